@@ -39,6 +39,12 @@ def _units():
         ("noalloc", "noalloc.hip", []),
     ]
     units.append(("gemm_lookup", "gemm_lookup.cpp", []))
+    # layer operators: the host side, the memory-bound kernels, and the products
+    # by operand type and layout
+    units += [("layers", "layers.cpp", []), ("layer_kernels", "layer_kernels.hip", []),
+              ("route", "route.hip", [])]
+    units += [(f"product_{dn}_{lay}", "product_inst.hip", [f"-DLP_DT={dt}", f"-DLP_LAY={lay}"])
+              for dt, dn in ((0, "f32"), (1, "bf16")) for lay in (0, 1, 2)]
     for dt, dn in ((0, "f32"), (1, "bf16")):
         for i in (16, 32):
             # CPR 0 is the generic path; the fast path needs CPR >= 64 / I

@@ -1,0 +1,90 @@
+// Launchers of the layer operators' helper kernels. dtype: gt_dtype of the
+// operands; ld*: elements between rows.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "gemmtune_layers.h"
+#include "product_args.h"
+
+namespace gt {
+
+// Sums the K slices of a product (a.e.part) in slice order and applies the linear
+// epilogue of a.e to every row (with groups along m: below the last offset).
+hipError_t launch_reduce(int dtype, const ProductArgs& a, hipStream_t s);
+
+// Rows a block of the gradient kernel sums into one row of its partial sums.
+constexpr int kActRows = 64;
+// dP = dY·act'(P) (gated: both halves), and each block's column sums of it into
+// part[block][wide] (part NULL: not wanted; dP NULL: only the sums).
+struct ActGradArgs {
+  int64_t M, N;
+  int act, gated;
+  const void* dY;
+  int64_t lddy;
+  const void* P;
+  int64_t ldp;
+  void* dP;
+  int64_t lddp;
+  float* part;
+  int vec;
+};
+hipError_t launch_act_grad(int dtype, const ActGradArgs& a, hipStream_t s);
+
+// out[g][n] = Σ of part's rows of group g, in order. Rows: with offsets, group
+// g's rows of tiles of `bm` rows, `per` partial rows each; without, all `rows`.
+hipError_t launch_join(const float* part, int64_t rows, int64_t wide, const int32_t* offsets,
+                       int groups, int64_t most, int bm, int per, float* out, hipStream_t s);
+
+// Rows of X and dY of the sorted entries: dst[p] = src[order[p] / k] for every
+// p below offsets[E] (either pair may be NULL).
+hipError_t launch_gather(int dtype, const void* a, int64_t lda, void* da, const void* b, int64_t ldb,
+                         void* db, int64_t ldd, int64_t cols, const int32_t* order,
+                         const int32_t* offsets, int E, int64_t entries, int k, int64_t T,
+                         hipStream_t s);
+
+// out[t] = R[t] + Σ_s w[t][s]·O[place[t][s]] (w NULL: 1; R NULL: 0), s ascending.
+struct CombineArgs {
+  int64_t T, D, entries;
+  int k, vec;
+  const float* O;
+  int64_t ldo;
+  const float* weights;
+  const int32_t* place;
+  const void* R;
+  int64_t ldr;
+  void* out;
+  int64_t ldout;
+};
+hipError_t launch_combine(int dtype, const CombineArgs& a, hipStream_t s);
+
+// part[chunk of kSumRows rows][D]: Σ w[order[p]]·rows[p] over the chunk's rows;
+// chunks counted per group.
+constexpr int kSumRows = 64;
+hipError_t launch_weighted_sums(int dtype, const void* rows, int64_t ld, int64_t D,
+                                const float* weights, const int32_t* order, int64_t entries,
+                                const int32_t* offsets, int E, float* part, hipStream_t s);
+
+// dweights[entry] = Σ of the ldot values at dot[place] (+ b2[e]·rows[place]), 0
+// for an entry without a place.
+struct WeightGradArgs {
+  int64_t entries, D;
+  int E;
+  const float* dot;
+  int64_t ldot;
+  const int32_t* place;
+  const int32_t* offsets;
+  const void* rows;   // dY of the sorted entries
+  int64_t ld;
+  const void* b2;     // or NULL
+  float* dweights;
+};
+hipError_t launch_weight_grad(int dtype, const WeightGradArgs& a, hipStream_t s);
+
+// Routing (gt_route): launches and scratch.
+int64_t route_scratch(int64_t T, int E, int k, int groups);
+hipError_t launch_route(const gt_route_args& a, void* ws, hipStream_t s);
+hipError_t launch_route_grad(const gt_route_grad_args& a, hipStream_t s);
+
+}  // namespace gt

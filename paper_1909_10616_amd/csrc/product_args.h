@@ -1,0 +1,82 @@
+// Arguments of the layer products and their launch.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace gt {
+
+// What becomes of the product's rows.
+enum EpiMode : int32_t {
+  kEpiLinear = 0,  // + bias, activation (gated or not), + residual, P kept
+  kEpiPart = 1,    // a K slice's sums, as they are, into `part`
+  kEpiSlope = 2,   // the product is dH of the experts: dP, w·H, Σ dH·H, column sums of dP
+};
+
+struct Epilogue {
+  int32_t mode;
+  int32_t act;       // gt_act
+  int32_t gated;     // columns n and N + n are a gate and its up value
+  int32_t out_f32;   // Y in fp32, else in the operands' type
+  int32_t vec;       // every row and pointer takes 4-element accesses
+  int32_t pad;
+  void* Y;           // [rows][ldy]; group g at Y + g·sY (groups along k)
+  int64_t ldy, sY;
+  void* P;           // kept pre-activations (kEpiLinear) or given ones (kEpiSlope), or null
+  int64_t ldp;
+  const void* bias;  // per group sbias apart
+  int64_t sbias;
+  const void* R;
+  int64_t ldr;
+  float* part;       // [slice][row][ldpart]: columns n, and ldpart/2 + n for up values
+  int64_t ldpart;
+  // kEpiSlope
+  void* Hw;               // [row][ldh]: w·act(P)
+  int64_t ldh;
+  const float* weights;   // of entry order[row]
+  const int32_t* order;
+  int64_t entries;        // entries of `order` and `weights`
+  float* dot;             // [row][ldot]: Σ over a wavefront's columns of dH·H
+  int64_t ldot;
+  float* colsum;          // [tile row·WAVES_M + wave row][wide]: sums of dP over its rows
+  int64_t wide;
+};
+
+struct ProductArgs {
+  const void* A;
+  const void* B;
+  int64_t lda, ldb;     // elements between stored rows
+  int64_t M, N, K;      // N: columns of Y (B has 2·N when gated)
+  const int32_t* offsets;  // group g: rows (or k) offsets[g] … offsets[g + 1] − 1
+  int32_t groups;       // 0: no groups
+  int32_t along_k;      // groups along k
+  int64_t sB;           // elements between the groups' B
+  const int32_t* gather;   // KC A: row r is A's row gather[r] / gather_div
+  int32_t gather_div;
+  int32_t splits;       // K slices (grid y)
+  int64_t a_rows;       // rows A has (gather)
+  int32_t tilesM, tilesN;
+  Epilogue e;
+};
+
+// How the operands lie: A and B along k or along their own index.
+enum Layout : int { kXW = 0, kPWt = 1, kXtP = 2 };  // KC·XC, KC·KC, XC·XC
+
+// The tiles that are built: rows, columns, wavefronts along each, ring slots.
+struct TileShape {
+  int BM, BN, NWM, NWN, NS;
+};
+constexpr int kTiles = 4;
+constexpr TileShape kTile[kTiles] = {
+    {256, 256, 2, 2, 2},  // 0: bf16, DMA only
+    {128, 128, 2, 2, 2},  // 1
+    {64, 64, 2, 2, 3},    // 2
+    {16, 128, 1, 4, 4},   // 3: not for kXtP
+};
+
+// Launches the product kernel of a tile (reg: the register path). The grid is
+// (tilesM·tilesN, splits, groups along k or 1).
+hipError_t launch_product(int dtype, int layout, int tile, bool reg, const ProductArgs& a,
+                          hipStream_t s);
+
+}  // namespace gt
