@@ -52,7 +52,10 @@ __global__ __launch_bounds__(256) void reduce_kernel(const ProductArgs a) {
       if (a.e.gated) u += *reinterpret_cast<const f32x4*>(p + z * slice + a.e.ldpart / 2);
     }
     const int group = a.groups > 0 ? group_of_row(a.offsets, a.groups, row) : 0;
-    linear_quad<T>(a.e, a.N, row, n, group, v, u);
+    const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
+    const f32x4 bv = bias_quad<T>(a.e, n, group, left);
+    const f32x4 bu = a.e.gated ? bias_quad<T>(a.e, n + a.N, group, left) : f32x4{};
+    linear_quad<T>(a.e, a.N, row, n, group, left, v, u, bv, bu, residual_quad<T>(a.e, row, n, left));
   }
 }
 

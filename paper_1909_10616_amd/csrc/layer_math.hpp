@@ -13,13 +13,37 @@ namespace gt {
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float sigmoid_of(float x) {
-  return __builtin_amdgcn_rcpf(1.0f + expf(-x));
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.4426950408889634f));
+}
+
+// Φ(x), the normal distribution function, and *e = exp(−x²/2). For x < 0, Φ = q·e with
+// q a polynomial in t = 1/(1 + 0.3·|x|), fitted by least squares to the scaled
+// complementary error function at 4500 points of [0, 14] with weights that even
+// out its relative error (1.5e-7; 5e-7 as evaluated here): a dozen instructions and
+// one exponential that the slope shares, where the library's error function
+// takes two branches of about fifty.
+__device__ __forceinline__ float normal_cdf(float x, float* e) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.3f, 1.0f));
+  float q = 0.03567453473806381f;
+  q = fmaf(q, t, -0.1572018563747406f);
+  q = fmaf(q, t, 0.20635104179382324f);
+  q = fmaf(q, t, -0.053681083023548126f);
+  q = fmaf(q, t, 0.1285601556301117f);
+  q = fmaf(q, t, 0.09991396218538284f);
+  q = fmaf(q, t, 0.12075387686491013f);
+  q = fmaf(q, t, 0.11962930113077164f);
+  *e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448171f);
+  const float tail = q * t * *e;
+  return x < 0.0f ? tail : 1.0f - tail;
 }
 
 // act(x)
 __device__ __forceinline__ float act_value(int act, float x) {
   if (act == GT_ACT_SILU) return x * sigmoid_of(x);
-  if (act == GT_ACT_GELU) return 0.5f * x * (1.0f + erff(x * 0.70710678118654752f));
+  if (act == GT_ACT_GELU) {
+    float e;
+    return x * normal_cdf(x, &e);
+  }
   if (act == GT_ACT_RELU) return x < 0.0f ? 0.0f : x;
   return x;
 }
@@ -31,9 +55,10 @@ __device__ __forceinline__ void act_both(int act, float x, float* value, float* 
     *value = x * s;
     *slope = s * (1.0f + x * (1.0f - s));
   } else if (act == GT_ACT_GELU) {
-    const float c = 0.5f * (1.0f + erff(x * 0.70710678118654752f));
+    float e;
+    const float c = normal_cdf(x, &e);
     *value = x * c;
-    *slope = c + x * 0.39894228040143268f * expf(-0.5f * x * x);
+    *slope = fmaf(x * 0.39894228040143268f, e, c);
   } else if (act == GT_ACT_RELU) {
     *value = x < 0.0f ? 0.0f : x;
     *slope = x > 0.0f ? 1.0f : 0.0f;

@@ -45,14 +45,13 @@ constexpr uint32_t kOutside = 0x80000000u;
 // Bytes one descriptor reaches (below kOutside).
 constexpr int64_t kReach = 0x7fffff00;
 
-// Raw buffer descriptor of [base, base + bytes): loads beyond it return zero.
-__device__ __forceinline__ i32x4 descriptor(const void* base, int64_t bytes) {
-  const uint64_t b = uniform_ptr(base);
+// Raw buffer descriptor of [b, b + bytes), both uniform: loads beyond it return zero.
+__device__ __forceinline__ i32x4 descriptor(uint64_t b, int64_t bytes) {
   const int64_t n = bytes < 0 ? 0 : bytes > kReach ? kReach : bytes;
   i32x4 d;
   d[0] = static_cast<int>(b);
   d[1] = static_cast<int>((b >> 32) & 0xffffu);
-  d[2] = uni(static_cast<int>(n));
+  d[2] = static_cast<int>(n);
   d[3] = 0x00020000;
   return d;
 }
@@ -120,30 +119,27 @@ __device__ __forceinline__ Span group_of_tile(const ProductArgs& a, int t, int64
 }
 
 // XOR of the 16-byte chunk index of an XC row k in LDS. bf16: the transposing
-// read's rows (bswz); fp32: the lane groups of a 4-byte read, 4 rows apart, go to the
-// four 64-byte quarters of 256 bytes.
-template <int DT>
+// read's rows (bswz); fp32: the 64/I lane groups of a 4-byte read, 4 rows apart, go to
+// distinct parts of 256 bytes.
+template <int DT, int I>
 __device__ __forceinline__ int xswz(int k, int chunks) {
   if constexpr (DT == 1)
     return bswz(k, chunks);
   else
-    return (((k >> 2) & 3) << 2) & (chunks - 1);
+    return (I == 16 ? ((k >> 2) & 3) << 2 : ((k >> 2) & 1) << 3) & (chunks - 1);
 }
 
 // ---- epilogue --------------------------------------------------------------
 
 // 4 outputs of a row from their sums v (and u, the up values, when gated): the
-// bias, the activation and the residual, every step in fp32.
+// bias (bv, bu), the activation and the residual r, every step in fp32.
 template <typename T>
 __device__ __forceinline__ void linear_quad(const Epilogue& e, int64_t N, int64_t row, int64_t n,
-                                            int group, f32x4 v, f32x4 u) {
+                                            int group, int left, f32x4 v, f32x4 u, f32x4 bv,
+                                            f32x4 bu, f32x4 r) {
   const bool vec = e.vec != 0;
-  const int left = N - n < 4 ? static_cast<int>(N - n) : 4;
-  if (e.bias) {
-    const T* b = static_cast<const T*>(e.bias) + group * e.sbias + n;
-    v += load4(b, left, vec);
-    if (e.gated) u += load4(b + N, left, vec);
-  }
+  v += bv;
+  u += bu;
   if (e.P) {
     T* p = static_cast<T*>(e.P) + row * e.ldp + n;
     store4(p, v, left, vec);
@@ -154,12 +150,21 @@ __device__ __forceinline__ void linear_quad(const Epilogue& e, int64_t N, int64_
     for (int i = 0; i < 4; ++i) v[i] = act_value(e.act, v[i]);
   }
   if (e.gated) v *= u;
-  if (e.R) v += load4(static_cast<const T*>(e.R) + row * e.ldr + n, left, vec);
+  v += r;
   const int64_t at = group * e.sY + row * e.ldy + n;
   if (e.out_f32)
     store4(static_cast<float*>(e.Y) + at, v, left, vec);
   else
     store4(static_cast<T*>(e.Y) + at, v, left, vec);
+}
+template <typename T>
+__device__ __forceinline__ f32x4 bias_quad(const Epilogue& e, int64_t n, int group, int left) {
+  return e.bias ? load4(static_cast<const T*>(e.bias) + group * e.sbias + n, left, e.vec != 0)
+                : f32x4{};
+}
+template <typename T>
+__device__ __forceinline__ f32x4 residual_quad(const Epilogue& e, int64_t row, int64_t n, int left) {
+  return e.R ? load4(static_cast<const T*>(e.R) + row * e.ldr + n, left, e.vec != 0) : f32x4{};
 }
 
 // Where a wavefront's tile lies.
@@ -174,7 +179,10 @@ struct EpiSums {
   f32x4 g, u;  // a lane's columns of dP, summed over its rows
 };
 
-// RP rows of a wavefront's tile, row h + r of it in LDS at mine + r·WN·4.
+// RP rows of a wavefront's tile, row h + r of it in LDS at mine + r·WN·4. A lane
+// keeps its column quad and takes U rows at a time: what they need from memory (the
+// residual, the pre-activations) is loaded for all of them before the first is
+// stored, since an output may be the residual itself.
 template <int DT, int WN, int XM, int RP, int BN>
 __device__ __forceinline__ void epilogue_rows(const ProductArgs& a, const EpiPlace& p, int h,
                                               const char* mine, int lane, EpiSums& sums) {
@@ -197,67 +205,100 @@ __device__ __forceinline__ void epilogue_rows(const ProductArgs& a, const EpiPla
       if (row < p.row_end && n < a.N) *reinterpret_cast<f32x4*>(base + row * e.ldpart) = chunk(r, c);
     }
   } else if (e.mode == kEpiLinear) {
-    if (e.gated) {
-      const int c = lane % (CH / 2);
-      const int64_t n = p.col + c * 4;
-      for (int r = lane / (CH / 2); r < RP; r += 128 / CH) {
-        const int64_t row = p.row + h + r;
-        if (row < p.row_end && n < a.N)
-          linear_quad<T>(e, a.N, row, n, p.group, chunk(r, c), chunk(r, c + CH / 2));
+    auto rows = [&](auto gated) __attribute__((always_inline)) {
+      constexpr bool G = decltype(gated)::value;
+      constexpr int LR = G ? CH / 2 : CH;      // lanes a row
+      constexpr int STEP = 64 / LR;
+      constexpr int U = RP / STEP >= 4 ? 4 : RP / STEP;
+      const int c = lane % LR;
+      const int64_t n = G ? p.col + c * 4 : col(c);
+      const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
+      f32x4 bv{}, bu{};
+      if (left > 0) {
+        bv = bias_quad<T>(e, n, p.group, left);
+        if constexpr (G) bu = bias_quad<T>(e, n + a.N, p.group, left);
       }
-    } else {
-      const int c = lane % CH;
-      const int64_t n = col(c);
-      for (int r = lane / CH; r < RP; r += 64 / CH) {
-        const int64_t row = p.row + h + r;
-        if (row < p.row_end && n < a.N)
-          linear_quad<T>(e, a.N, row, n, p.group, chunk(r, c), f32x4{});
+      for (int r0 = lane / LR; r0 < RP; r0 += U * STEP) {
+        f32x4 res[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int64_t row = p.row + h + r0 + i * STEP;
+          res[i] = f32x4{};
+          if (row < p.row_end && left > 0) res[i] = residual_quad<T>(e, row, n, left);
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int r = r0 + i * STEP;
+          const int64_t row = p.row + h + r;
+          if (row < p.row_end && left > 0)
+            linear_quad<T>(e, a.N, row, n, p.group, left, chunk(r, c),
+                           G ? chunk(r, c + CH / 2) : f32x4{}, bv, bu, res[i]);
+        }
       }
-    }
+    };
+    if (e.gated)
+      rows(std::true_type{});
+    else
+      rows(std::false_type{});
   } else {
     // dH arrived: H = act(P) (times up), w the row's weight;
     // dP = w·dH·act'(P) (gated: ·up, and w·dH·act(gate) for up), Hw = w·H
+    constexpr int STEP = 64 / CH;
+    constexpr int U = RP / STEP >= 4 ? 4 : RP / STEP;
     const int c = lane % CH;
     const int64_t n = col(c);
     const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
     const bool vec = e.vec != 0;
-    for (int r = lane / CH; r < RP; r += 64 / CH) {
-      const int64_t row = p.row + h + r;
-      const bool live = row < p.row_end && left > 0;
-      float dot = 0.0f;
-      if (live) {
-        const f32x4 v = chunk(r, c);
-        const int64_t entry = e.order[row];
-        const float w = entry >= 0 && entry < e.entries ? e.weights[entry] : 0.0f;
-        const T* pp = static_cast<const T*>(e.P) + row * e.ldp + n;
-        const f32x4 gate = load4(pp, left, vec);
-        f32x4 up = f32x4{1.0f, 1.0f, 1.0f, 1.0f};
-        if (e.gated) up = load4(pp + a.N, left, vec);
-        f32x4 val, slope;
+    for (int r0 = lane / CH; r0 < RP; r0 += U * STEP) {
+      f32x4 gate[U], up[U];
+      float w[U];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x, y;
-          act_both(e.act, gate[i], &x, &y);
-          val[i] = x;
-          slope[i] = y;
+      for (int i = 0; i < U; ++i) {
+        const int64_t row = p.row + h + r0 + i * STEP;
+        gate[i] = f32x4{};
+        up[i] = f32x4{1.0f, 1.0f, 1.0f, 1.0f};
+        w[i] = 0.0f;
+        if (row < p.row_end && left > 0) {
+          const int64_t entry = e.order[row];
+          if (entry >= 0 && entry < e.entries) w[i] = e.weights[entry];
+          const T* pp = static_cast<const T*>(e.P) + row * e.ldp + n;
+          gate[i] = load4(pp, left, vec);
+          if (e.gated) up[i] = load4(pp + a.N, left, vec);
         }
-        const f32x4 wv = v * w, H = val * up;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dot += i < left ? v[i] * H[i] : 0.0f;
-        const f32x4 dg = wv * up * slope;
-        T* out = static_cast<T*>(e.Y) + row * e.ldy + n;
-        store4(out, dg, left, vec);
-        sums.g += dg;
-        if (e.gated) {
-          const f32x4 du = wv * val;
-          store4(out + a.N, du, left, vec);
-          sums.u += du;
-        }
-        store4(static_cast<T*>(e.Hw) + row * e.ldh + n, H * w, left, vec);
       }
 #pragma unroll
-      for (int d = 1; d < CH; d <<= 1) dot += __shfl_xor(dot, d);
-      if (c == 0 && row < p.row_end) e.dot[row * e.ldot + p.pcol] = dot;
+      for (int i = 0; i < U; ++i) {
+        const int r = r0 + i * STEP;
+        const int64_t row = p.row + h + r;
+        float dot = 0.0f;
+        if (row < p.row_end && left > 0) {
+          const f32x4 v = chunk(r, c);
+          f32x4 val, slope;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float x, y;
+            act_both(e.act, gate[i][j], &x, &y);
+            val[j] = x;
+            slope[j] = y;
+          }
+          const f32x4 wv = v * w[i], H = val * up[i];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dot += j < left ? v[j] * H[j] : 0.0f;
+          const f32x4 dg = wv * up[i] * slope;
+          T* out = static_cast<T*>(e.Y) + row * e.ldy + n;
+          store4(out, dg, left, vec);
+          sums.g += dg;
+          if (e.gated) {
+            const f32x4 du = wv * val;
+            store4(out + a.N, du, left, vec);
+            sums.u += du;
+          }
+          store4(static_cast<T*>(e.Hw) + row * e.ldh + n, H * w[i], left, vec);
+        }
+#pragma unroll
+        for (int d = 1; d < CH; d <<= 1) dot += __shfl_xor(dot, d);
+        if (c == 0 && row < p.row_end) e.dot[row * e.ldot + p.pcol] = dot;
+      }
     }
   }
 }
@@ -289,7 +330,7 @@ __device__ __forceinline__ void epilogue_sums(const ProductArgs& a, const EpiPla
 // ---- the kernel ------------------------------------------------------------
 
 // Measured (bf16, one MI355X): see the instances' list in product_inst.hip.
-template <int DT, bool AX, bool BX, int BM, int BN, int NWM, int NWN, int NS, bool REG>
+template <int DT, int I, bool AX, bool BX, int BM, int BN, int NWM, int NWN, int NS, bool REG>
 __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductArgs a) {
   using T = typename Elem<DT>::T;
   constexpr int SZ = DT == 1 ? 2 : 4;
@@ -297,12 +338,16 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   constexpr int BK = 128 / SZ;           // k of a stage
   constexpr int NW = NWM * NWN;
   constexpr int WM = BM / NWM, WN = BN / NWN;
-  constexpr int TM = WM / 16, TN = WN / 16;
+  constexpr int TM = WM / I, TN = WN / I;
   constexpr int HN = WN / 2;             // a wavefront's columns in each half of the tile
+  constexpr int G = 64 / I;              // lane groups: 16-byte chunks of k a chunk-step
+  constexpr int NCS = 8 / G;             // chunk-steps of a stage
+  using acc_t = typename AccT<I>::type;
   static_assert(TM >= 1 && TN >= 2 && TN % 2 == 0, "tile too small for its wavefronts");
   static_assert(!REG || NS == 2, "the register path has two slots");
   constexpr int INA = BM / 8, INB = BN / 8;   // 1 KiB load instructions of a stage
   constexpr int NA = (INA + NW - 1) / NW, NB = (INB + NW - 1) / NW;  // of a wavefront
+  static_assert(NW % 2 == 0, "chunks of a lane");
   static_assert(INA % NW == 0 || NW % INA == 0, "loads of A");
   static_assert(INB % NW == 0 || NW % INB == 0, "loads of B");
   constexpr uint32_t STAGE = (BM + BN) * 128u;
@@ -312,7 +357,7 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   const int lane = threadIdx.x & 63;
   const int wave = uni(threadIdx.x >> 6);
   const int wm = wave % NWM, wn = wave / NWM;
-  const int l16 = lane & 15, g4 = lane >> 4;
+  const int lI = lane % I, grp = lane / I;
 
   // ---- which tile: XCD-contiguous runs, in groups of 4 tile rows
   int tm, tn;
@@ -321,9 +366,9 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
     int t = static_cast<int>(blockIdx.x);
     const int q = nt >> 3, r = nt & 7, x = t & 7;
     t = x * q + min(x, r) + (t >> 3);
-    constexpr int G = 4;
-    const int per = G * a.tilesN, grp = t / per, f = grp * G, gs = min(a.tilesM - f, G);
-    const int in = t - grp * per;
+    constexpr int ROWS = 4;
+    const int per = ROWS * a.tilesN, run = t / per, f = run * ROWS, gs = min(a.tilesM - f, ROWS);
+    const int in = t - run * per;
     tm = f + in % gs;
     tn = in / gs;
   }
@@ -363,6 +408,7 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   }
   const int nst = st1 - st0;
   k0 += static_cast<int64_t>(st0) * BK;
+  if (k0 + static_cast<int64_t>(nst) * BK < kend) kend = k0 + static_cast<int64_t>(nst) * BK;
 
   // ---- where each of this lane's chunks of a stage lies
   // Load instruction p fills the slots 64·p + lane of its operand's part. KC: 8
@@ -396,7 +442,7 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
         offA[i] = ok ? static_cast<uint32_t>(row) * static_cast<uint32_t>(a.lda * SZ) + c * 16u : kOutside;
       }
     } else {
-      const int k = s / CA, c = (s % CA) ^ xswz<DT>(k, CA);
+      const int k = s / CA, c = (s % CA) ^ xswz<DT, I>(k, CA);
       kA[i] = k;
       if constexpr (REG) {
         ptrA[i] = Ag + (k0 + k) * a.lda + m0 + c * VEC;
@@ -421,7 +467,7 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
         offB[i] = ok ? static_cast<uint32_t>(r) * static_cast<uint32_t>(a.ldb * SZ) + c * 16u : kOutside;
       }
     } else {
-      const int k = s / CB, c = (s % CB) ^ xswz<DT>(k, CB);
+      const int k = s / CB, c = (s % CB) ^ xswz<DT, I>(k, CB);
       const bool second = c * VEC >= BN / 2;
       const int64_t col = n0 + c * VEC + (second ? hoff : 0);
       const int64_t end = halves && !second ? a.N : wide;
@@ -441,41 +487,62 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   const uint32_t lds0 = static_cast<uint32_t>(uni(static_cast<int>(lds_off(smem))));
   u32x4 regA[REG ? NA : 1], regB[REG ? NB : 1];
 
-  // Stage st (from this slice's first) towards slot `slot`.
-  auto issue = [&](int st, int slot) __attribute__((always_inline)) {
-    const int64_t kk = static_cast<int64_t>(st) * BK;       // from k0
-    const int64_t left = kend - k0 - kk;                    // k left, > 0
+  // DMA: the next stage to load, as the operands' addresses at its first k, the bytes from
+  // there to each operand's last element, and the k left.
+  uint64_t ga = 0, gb = 0;
+  int64_t remA = 0, remB = 0, left = kend - k0;
+  const int64_t stepA = (AX ? BK * a.lda : BK) * SZ, stepB = (BX ? BK * a.ldb : BK) * SZ;
+  i32x4 da{}, db{};
+  int here = 0;   // k left, at most a stage's
+  if constexpr (!REG) {
+    ga = uniform_ptr(AX ? Ag + k0 * a.lda + m0 : Ag + (a.gather ? 0 : m0 * a.lda) + k0);
+    gb = uniform_ptr(BX ? Bg + k0 * a.ldb + n0 : Bg + n0 * a.ldb + k0);
+    remA = uni64((AX ? (left - 1) * a.lda + mend - m0 : (arem - 1) * a.lda + left) * SZ);
+    remB = uni64((BX ? (left - 1) * a.ldb + wide - n0 : (wide - n0 - 1) * a.ldb + left) * SZ);
+  }
+  auto next_stage = [&]() __attribute__((always_inline)) {
+    ga += stepA;
+    gb += stepB;
+    remA -= stepA;
+    remB -= stepB;
+    left -= BK;
+  };
+  // (A stage past the last reads nothing: its descriptors are empty.)
+  auto descriptors = [&]() __attribute__((always_inline)) {
+    da = descriptor(ga, left > 0 ? remA : 0);
+    db = descriptor(gb, left > 0 ? remB : 0);
+    settle(da, db);
+    here = left < BK ? static_cast<int>(left) : BK;
+  };
+  // Load instruction i of the stage (A's, then B's) into the slot at LDS address `base`.
+  // KC rows that end inside the stage are zero beyond.
+  auto dma = [&](uint32_t base, int i) __attribute__((always_inline)) {
+    // (a KC chunk has the same k in all of a lane's instructions: NW is even)
+    if (i < NA) {
+      const uint32_t off = !AX && kA[0] >= here ? kOutside : offA[i];
+      dma_buffer16(off, da, base + static_cast<uint32_t>((wave + NW * i) % INA) * 1024u);
+    } else {
+      const int j = i - NA;
+      const uint32_t off = !BX && kB[0] >= here ? kOutside : offB[j];
+      dma_buffer16(off, db, base + BOFF + static_cast<uint32_t>((wave + NW * j) % INB) * 1024u);
+    }
+  };
+  // REG: stage st (from this slice's first) into registers.
+  auto issue = [&](int st) __attribute__((always_inline)) {
     if constexpr (REG) {
+      const int64_t kk = static_cast<int64_t>(st) * BK;       // from k0
+      const int64_t rest = left - kk;                         // k left
 #pragma unroll
       for (int i = 0; i < NA; ++i) {
         const T* p = ptrA[i] + (AX ? kk * a.lda : kk);
-        const int64_t n = AX ? (kA[i] < left ? limA[i] : 0) : (limA[i] ? left - kA[i] : 0);
+        const int64_t n = AX ? (kA[i] < rest ? limA[i] : 0) : (limA[i] ? rest - kA[i] : 0);
         regA[i] = load_chunk<T, VEC>(p, n);
       }
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         const T* p = ptrB[i] + (BX ? kk * a.ldb : kk);
-        const int64_t n = BX ? (kB[i] < left ? limB[i] : 0) : (limB[i] ? left - kB[i] : 0);
+        const int64_t n = BX ? (kB[i] < rest ? limB[i] : 0) : (limB[i] ? rest - kB[i] : 0);
         regB[i] = load_chunk<T, VEC>(p, n);
-      }
-    } else {
-      // from the stage's origin to the operand's last element
-      const T* ga = AX ? Ag + (k0 + kk) * a.lda + m0 : Ag + (a.gather ? 0 : m0 * a.lda) + k0 + kk;
-      const T* gb = BX ? Bg + (k0 + kk) * a.ldb + n0 : Bg + n0 * a.ldb + k0 + kk;
-      i32x4 da = descriptor(ga, (AX ? (left - 1) * a.lda + mend - m0 : (arem - 1) * a.lda + left) * SZ);
-      i32x4 db = descriptor(gb, (BX ? (left - 1) * a.ldb + wide - n0 : (wide - n0 - 1) * a.ldb + left) * SZ);
-      settle(da, db);
-      const uint32_t base = lds0 + static_cast<uint32_t>(slot) * STAGE;
-      const bool tail = left < BK;   // KC rows end inside this stage: zero beyond
-#pragma unroll
-      for (int i = 0; i < NA; ++i) {
-        const uint32_t off = !AX && tail && kA[i] >= left ? kOutside : offA[i];
-        dma_buffer16(off, da, base + static_cast<uint32_t>((wave + NW * i) % INA) * 1024u);
-      }
-#pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const uint32_t off = !BX && tail && kB[i] >= left ? kOutside : offB[i];
-        dma_buffer16(off, db, base + BOFF + static_cast<uint32_t>((wave + NW * i) % INB) * 1024u);
       }
     }
   };
@@ -492,33 +559,36 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
     }
   };
 
-  // ---- fragments: 16 rows (columns) × 16 bytes of k a lane
+  // ---- fragments: I rows (columns) × 16 bytes of k a lane, chunk-step cs at k chunks cs·G …
   // tile column of fragment j: half j / (TN/2) of the tile
-  auto bcol = [&](int j) { return (j < TN / 2 ? 0 : BN / 2) + wn * HN + (j % (TN / 2)) * 16; };
-  const uint32_t sw = static_cast<uint32_t>(l16 >> 1);
-  uint32_t fa[AX ? TM : 2], fb[BX ? TN : 2];
-  // XC bf16: in lane group g4, lane i addresses row 8·g4 + (i >> 2), columns 4·(i & 3)
-  const int krow = DT == 1 ? 8 * g4 + (l16 >> 2) : 4 * g4;
-  const int kcol = DT == 1 ? 4 * (l16 & 3) : l16;
+  auto bcol = [&](int j) { return (j < TN / 2 ? 0 : BN / 2) + wn * HN + (j % (TN / 2)) * I; };
+  const uint32_t sw = static_cast<uint32_t>((lI >> 1) & 7);
+  uint32_t fa[AX ? TM : NCS], fb[BX ? TN : NCS];
+  // XC bf16: in a group of 16 lanes, lane i addresses row i >> 2, columns 4·(i & 3)
+  const int i16 = lane & 15, g16 = lane >> 4;
+  const int krow = DT == 1 ? 8 * grp + (i16 >> 2) : 4 * grp;
+  const int kcol = DT == 1 ? (I == 32 ? 16 * (g16 & 1) : 0) + 4 * (i16 & 3) : lI;
   if constexpr (AX) {
 #pragma unroll
     for (int t = 0; t < TM; ++t) {
-      const int x = wm * WM + t * 16 + kcol;
-      fa[t] = krow * (BM * SZ) + ((x / VEC) ^ xswz<DT>(krow, CA)) * 16 + (x % VEC) * SZ;
+      const int x = wm * WM + t * I + kcol;
+      fa[t] = krow * (BM * SZ) + ((x / VEC) ^ xswz<DT, I>(krow, CA)) * 16 + (x % VEC) * SZ;
     }
   } else {
-    fa[0] = (wm * WM + l16) * 128u + ((static_cast<uint32_t>(g4) ^ sw) << 4);
-    fa[1] = fa[0] ^ 64u;
+#pragma unroll
+    for (int c = 0; c < NCS; ++c)
+      fa[c] = (wm * WM + lI) * 128u + ((static_cast<uint32_t>(grp + c * G) ^ sw) << 4);
   }
   if constexpr (BX) {
 #pragma unroll
     for (int t = 0; t < TN; ++t) {
       const int x = bcol(t) + kcol;
-      fb[t] = BOFF + krow * (BN * SZ) + ((x / VEC) ^ xswz<DT>(krow, CB)) * 16 + (x % VEC) * SZ;
+      fb[t] = BOFF + krow * (BN * SZ) + ((x / VEC) ^ xswz<DT, I>(krow, CB)) * 16 + (x % VEC) * SZ;
     }
   } else {
-    fb[0] = BOFF + l16 * 128u + ((static_cast<uint32_t>(g4) ^ sw) << 4);
-    fb[1] = fb[0] ^ 64u;
+#pragma unroll
+    for (int c = 0; c < NCS; ++c)
+      fb[c] = BOFF + (wn * HN + lI) * 128u + ((static_cast<uint32_t>(grp + c * G) ^ sw) << 4);
   }
   auto read_x = [&](const char* st, uint32_t at, int cs, int rowb) __attribute__((always_inline)) {
     u32x4 v;
@@ -527,98 +597,123 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh)
         h[hh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(st + at + (cs * 32 + 4 * hh) * rowb));
+            (__attribute__((address_space(3))) s16x4*)(st + at + (cs * G * 8 + 4 * hh) * rowb));
       v = __builtin_bit_cast(u32x4, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        v[q] = *reinterpret_cast<const unsigned*>(st + at + (cs * 16 + q) * rowb);
+        v[q] = *reinterpret_cast<const unsigned*>(st + at + (cs * G * 4 + q) * rowb);
     }
     return v;
   };
   u32x4 va[2][TM], vb[2][TN];
-  auto frags = [&](int slot, int cs, int set) __attribute__((always_inline)) {
-    const char* st = smem + slot * STAGE;
-#pragma unroll
-    for (int t = 0; t < TN; ++t) {
+  // Fragment r of chunk-step cs (B's, then A's) of the slot at st.
+  auto frag = [&](const char* st, int cs, int set, int r) __attribute__((always_inline)) {
+    if (r < TN) {
       if constexpr (BX)
-        vb[set][t] = read_x(st, fb[t], cs, BN * SZ);
+        vb[set][r] = read_x(st, fb[r], cs, BN * SZ);
       else
-        vb[set][t] = *reinterpret_cast<const u32x4*>(st + fb[cs] + bcol(t) * 128);
-    }
-#pragma unroll
-    for (int t = 0; t < TM; ++t) {
+        vb[set][r] = *reinterpret_cast<const u32x4*>(st + fb[cs] + (bcol(r) - wn * HN) * 128);
+    } else {
+      const int t = r - TN;
       if constexpr (AX)
         va[set][t] = read_x(st, fa[t], cs, BM * SZ);
       else
-        va[set][t] = *reinterpret_cast<const u32x4*>(st + fa[cs] + t * 2048);
+        va[set][t] = *reinterpret_cast<const u32x4*>(st + fa[cs] + t * (I * 128));
     }
   };
 
-  f32x4 acc[TM][TN];
+  acc_t acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{};
-  auto mfmas = [&](int set) __attribute__((always_inline)) {
-#pragma unroll
-    for (int q = 0; q < (DT == 1 ? 1 : 4); ++q)
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          if constexpr (DT == 1)
-            acc[i][j] = mfma_bf16(__builtin_bit_cast(bf16x8, vb[set][j]),
-                                  __builtin_bit_cast(bf16x8, va[set][i]), acc[i][j]);
-          else
-            acc[i][j] = mfma_f32(__builtin_bit_cast(f32x4, vb[set][j])[q],
-                                 __builtin_bit_cast(f32x4, va[set][i])[q], acc[i][j]);
-        }
+    for (int j = 0; j < TN; ++j) acc[i][j] = acc_t{};
+  constexpr int CNT = NA + NB;                          // loads of a wavefront and stage
+  constexpr int FIRST = CNT / 2;                        // of them in the first window
+  constexpr int FR = TM + TN;                           // fragments of a chunk-step
+  constexpr int MF = (DT == 1 ? 1 : 4) * TM * TN;       // MFMAs of a chunk-step
+  auto mfma1 = [&](int set, int q) __attribute__((always_inline)) {
+    const int x = DT == 1 ? 0 : q / (TM * TN), i = q % (TM * TN) / TN, j = q % TN;
+    if constexpr (DT == 1)
+      acc[i][j] = mfma_bf16(__builtin_bit_cast(bf16x8, vb[set][j]),
+                            __builtin_bit_cast(bf16x8, va[set][i]), acc[i][j]);
+    else
+      acc[i][j] = mfma_f32(__builtin_bit_cast(f32x4, vb[set][j])[x],
+                           __builtin_bit_cast(f32x4, va[set][i])[x], acc[i][j]);
   };
+  // The MFMAs of one chunk-step (fragments `set`) with, between them, the reads of the other
+  // set (chunk-step cs of the slot at st) and loads LO … HI − 1 of a stage into
+  // the slot at `base`. A wavefront that waits for room in the memory pipeline issues
+  // no MFMAs, so both go out a few at a time.
+  auto chunk_step = [&](int set, const char* st, int cs, uint32_t base, auto lo, auto hi)
+      __attribute__((always_inline)) {
+    constexpr int LO = decltype(lo)::value, HI = REG ? LO : decltype(hi)::value;
+    constexpr int SPAN = MF >= 16 ? MF * 3 / 4 : MF >= 4 ? MF / 2 : 1;
+#pragma unroll
+    for (int q = 0; q < MF; ++q) {
+#pragma unroll
+      for (int r = 0; r < FR; ++r)
+        if (r * SPAN / FR == q) frag(st, cs, set ^ 1, r);
+      if constexpr (HI > LO) {
+#pragma unroll
+        for (int i = LO; i < HI; ++i)
+          if ((i - LO) * SPAN / (HI - LO) == q) dma(base, i);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      mfma1(set, q);
+    }
+  };
+  using i0 = std::integral_constant<int, 0>;
+  using iF = std::integral_constant<int, FIRST>;
+  using iC = std::integral_constant<int, CNT>;
 
-  // ---- the ring. Boundary of stage l, before its last MFMAs: stage l + 1 has
-  // landed and every wavefront has read all of stage l, whose slot stage l + NS takes.
-  constexpr int CNT = NA + NB;
+  // ---- the ring. Boundary of stage l, before its last chunk-step: stage l + 1 has
+  // landed and every wavefront has read all of stage l, whose slot stage l + NS takes:
+  // its first loads in that chunk-step, the others in the first of stage l + 1.
+  // One loop for all stages (stages past the last are loaded as nothing, and their
+  // fragments are not used): with loops of their own for the last ones the
+  // compiler moves 256 accumulators about between them, or spills them.
   if (nst > 0) {
     if constexpr (REG) {
-      issue(0, 0);
+      issue(0);
       commit(0);
-      if (nst > 1) issue(1, 1);
+      issue(1);
       __syncthreads();
     } else {
-      const int pro = min(NS, nst);
-      for (int s = 0; s < pro; ++s) issue(s, s);
-      if (pro == NS)
-        waitcnt_vm<(NS - 1) * CNT>();
-      else
-        waitcnt_vm<0>();
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        descriptors();
+#pragma unroll
+        for (int i = 0; i < (s == NS - 1 ? FIRST : CNT); ++i) dma(lds0 + s * STAGE, i);
+        if (s < NS - 1) next_stage();
+      }
+      waitcnt_vm<(NS - 2) * CNT + FIRST>();
       ring_barrier();
     }
-    frags(0, 0, 0);
-    int cur = 0;
+#pragma unroll
+    for (int r = 0; r < FR; ++r) frag(smem, 0, 0, r);
+    uint32_t cur = 0;   // byte offset of the stage's slot
     for (int l = 0; l < nst; ++l) {
-      frags(cur, 1, 1);
-      mfmas(0);
-      const int nx = cur + 1 == NS ? 0 : cur + 1;
-      if (l + 1 < nst) {
-        if constexpr (REG) {
-          commit(nx);
-          __syncthreads();
-          if (l + 2 < nst) issue(l + 2, cur);
-        } else {
-          if (l + NS <= nst)
-            waitcnt_vm<(NS - 2) * CNT>();
-          else
-            waitcnt_vm<0>();
-          waitcnt_lgkm0();
-          ring_barrier();
-          if (l + NS < nst) issue(l + NS, cur);
-        }
-        frags(nx, 0, 0);
+      const uint32_t nx = cur + STAGE == NS * STAGE ? 0 : cur + STAGE;
+      const uint32_t before = cur == 0 ? (NS - 1) * STAGE : cur - STAGE;
+      chunk_step(0, smem + cur, 1, lds0 + before, iF{}, iC{});
+#pragma unroll
+      for (int c = 1; c + 1 < NCS; ++c) chunk_step(c & 1, smem + cur, c + 1, 0, i0{}, i0{});
+      if constexpr (REG) {
+        commit(nx / STAGE);
+        __syncthreads();
+        issue(l + 2);
+      } else {
+        next_stage();
+        descriptors();
+        waitcnt_vm<(NS - 2) * CNT>();
+        waitcnt_lgkm0();
+        ring_barrier();
       }
-      mfmas(1);
+      chunk_step((NCS - 1) & 1, smem + nx, 0, lds0 + cur, i0{}, iF{});
       cur = nx;
     }
+    waitcnt_vm<0>();
   }
 
   // ---- epilogue: the wavefront's accumulators through its own share of LDS, RP
@@ -626,9 +721,9 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   constexpr int REGION = NS * STAGE / NW;
   constexpr int CH = WN / 4;                       // 16-byte fp32 chunks of a row
   constexpr int XM = (CH < 16 ? CH : 16) - 1;
-  constexpr int RPX = REGION / (WN * 4) / 16 * 16;
+  constexpr int RPX = REGION / (WN * 4) / I * I;
   constexpr int RP = RPX < WM ? RPX : WM;
-  static_assert(RP >= 16 && WM % RP == 0, "epilogue rows");
+  static_assert(RP >= I && WM % RP == 0, "epilogue rows");
   __syncthreads();
   char* mine = smem + wave * REGION;
   const EpiPlace place{m0 + wm * WM, mend, n0 + wn * HN, group, z,
@@ -637,12 +732,17 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
 #pragma unroll
   for (int h = 0; h < WM / RP; ++h) {
 #pragma unroll
-    for (int i = 0; i < RP / 16; ++i)
+    for (int i = 0; i < RP / I; ++i)
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int r = i * 16 + l16, c = j * 4 + g4;
-        *reinterpret_cast<f32x4*>(mine + r * (WN * 4) + ((c ^ (r & XM)) << 4)) = acc[h * (RP / 16) + i][j];
-      }
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < AccT<I>::N / 4; ++q) {
+          // accumulators 4q … 4q + 3: columns j·I + 8q + 4·grp … (I = 16: 4·grp …) of row lI
+          const int r = i * I + lI, c = (j * I + 8 * q) / 4 + grp;
+          const acc_t& v = acc[h * (RP / I) + i][j];
+          *reinterpret_cast<f32x4*>(mine + r * (WN * 4) + ((c ^ (r & XM)) << 4)) =
+              f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");

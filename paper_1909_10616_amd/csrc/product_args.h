@@ -62,16 +62,16 @@ struct ProductArgs {
 // How the operands lie: A and B along k or along their own index.
 enum Layout : int { kXW = 0, kPWt = 1, kXtP = 2 };  // KC·XC, KC·KC, XC·XC
 
-// The tiles that are built: rows, columns, wavefronts along each, ring slots.
+// The tiles that are built: rows, columns, wavefronts along each, ring slots, MFMA size.
 struct TileShape {
-  int BM, BN, NWM, NWN, NS;
+  int BM, BN, NWM, NWN, NS, I;
 };
 constexpr int kTiles = 4;
 constexpr TileShape kTile[kTiles] = {
-    {256, 256, 2, 2, 2},  // 0: bf16, DMA only
-    {128, 128, 2, 2, 2},  // 1
-    {64, 64, 2, 2, 3},    // 2
-    {16, 128, 1, 4, 4},   // 3: not for kXtP
+    {256, 256, 2, 2, 2, 32},  // 0: bf16, DMA only
+    {128, 128, 2, 2, 2, 32},  // 1
+    {64, 64, 2, 2, 3, 16},    // 2
+    {16, 128, 1, 4, 4, 16},   // 3: not for kXtP
 };
 
 // Launches the product kernel of a tile (reg: the register path). The grid is

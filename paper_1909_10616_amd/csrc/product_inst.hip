@@ -36,7 +36,7 @@ hipError_t go(const ProductArgs& a, hipStream_t s) {
   constexpr TileShape t = kTile[TILE];
   constexpr int NS = REG ? 2 : t.NS;
   constexpr auto* fn =
-      product_kernel<LP_DT, LP_LAY == kXtP, LP_LAY != kPWt, t.BM, t.BN, t.NWM, t.NWN, NS, REG>;
+      product_kernel<LP_DT, t.I, LP_LAY == kXtP, LP_LAY != kPWt, t.BM, t.BN, t.NWM, t.NWN, NS, REG>;
   const dim3 grid(static_cast<unsigned>(a.tilesM) * static_cast<unsigned>(a.tilesN),
                   static_cast<unsigned>(a.splits),
                   a.along_k ? static_cast<unsigned>(a.groups) : 1u);
