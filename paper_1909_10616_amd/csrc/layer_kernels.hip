@@ -55,7 +55,8 @@ __global__ __launch_bounds__(256) void reduce_kernel(const ProductArgs a) {
     const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
     const f32x4 bv = bias_quad<T>(a.e, n, group, left);
     const f32x4 bu = a.e.gated ? bias_quad<T>(a.e, n + a.N, group, left) : f32x4{};
-    linear_quad<T>(a.e, a.N, row, n, group, left, v, u, bv, bu, residual_quad<T>(a.e, row, n, left));
+    linear_quad<T>(a.e, a.N, row, n, group, left, a.e.gated != 0, v, u, bv, bu,
+                   residual_quad<T>(a.e, row, n, left));
   }
 }
 

@@ -117,6 +117,48 @@ __device__ __forceinline__ void store4(T* p, f32x4 v, int n, bool vec) {
   }
 }
 
+// 8 values at a 16-byte aligned p.
+struct oct {
+  f32x4 a, b;
+};
+template <typename T>
+__device__ __forceinline__ oct load8(const T* p) {
+  oct v;
+  if constexpr (sizeof(T) == 4) {
+    v.a = *reinterpret_cast<const f32x4*>(p);
+    v.b = *reinterpret_cast<const f32x4*>(p + 4);
+  } else {
+    const u32x4 u = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      v.a[2 * i] = __builtin_bit_cast(float, u[i] << 16);
+      v.a[2 * i + 1] = __builtin_bit_cast(float, u[i] & 0xffff0000u);
+      v.b[2 * i] = __builtin_bit_cast(float, u[i + 2] << 16);
+      v.b[2 * i + 1] = __builtin_bit_cast(float, u[i + 2] & 0xffff0000u);
+    }
+  }
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const oct& v) {
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<f32x4*>(p) = v.a;
+    *reinterpret_cast<f32x4*>(p + 4) = v.b;
+  } else {
+    const uint2 x = __builtin_bit_cast(uint2, __builtin_convertvector(v.a, bf16x4));
+    const uint2 y = __builtin_bit_cast(uint2, __builtin_convertvector(v.b, bf16x4));
+    *reinterpret_cast<u32x4*>(p) = u32x4{x.x, x.y, y.x, y.y};
+  }
+}
+template <int ACT>
+__device__ __forceinline__ void act8(oct& v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v.a[i] = act_value(ACT, v.a[i]);
+    v.b[i] = act_value(ACT, v.b[i]);
+  }
+}
+
 // The first n (≤ 0: none) of VEC values from p, at any alignment; zero beyond.
 template <typename T, int VEC>
 __device__ __forceinline__ u32x4 load_chunk(const T* p, int64_t n) {

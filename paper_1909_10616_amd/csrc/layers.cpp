@@ -64,7 +64,7 @@ bool chunks_serve(const Product& p) {
   const ProductArgs& a = p.a;
   const int64_t sz = size_of(p.dtype), vec = 16 / sz;
   const int64_t reach = int64_t{1} << 31;
-  const int64_t wide = a.e.gated && a.e.mode != kEpiSlope ? 2 * a.N : a.N;
+  const int64_t wide = a.e.epi == kEpiGated ? 2 * a.N : a.N;
   if (!aligned(a.A, 16) || !aligned(a.B, 16) || a.lda % vec || a.ldb % vec || a.sB % vec) return false;
   const bool ax = p.layout == kXtP, bx = p.layout != kPWt;
   if ((ax ? a.M : a.K) % vec || (bx ? wide : a.K) % vec || (wide != a.N && a.N % vec)) return false;
@@ -79,7 +79,7 @@ bool chunks_serve(const Product& p) {
 void choose(Product* p, bool may_split) {
   ProductArgs& a = p->a;
   const int64_t bk = 128 / size_of(p->dtype);
-  const int64_t wide = a.e.gated && a.e.mode != kEpiSlope ? 2 * a.N : a.N;
+  const int64_t wide = a.e.epi == kEpiGated ? 2 * a.N : a.N;
   p->reg = !chunks_serve(*p);
   const int64_t stages = std::max<int64_t>(1, (a.along_k ? a.K / std::max(1, a.groups) : a.K) / bk);
   double best = 0.0;
@@ -117,7 +117,9 @@ void choose(Product* p, bool may_split) {
       }
     }
   }
-  a.e.ldpart = up(a.N, 4) * (a.e.gated ? 2 : 1);
+  a.e.ldpart = up(a.N, 4) * (wide == a.N ? 1 : 2);
+  const int64_t all = (a.K + bk - 1) / bk;
+  a.per_slice = static_cast<int>((all + a.splits - 1) / std::max(1, a.splits));
   p->part = a.splits > 1 ? a.splits * a.M * a.e.ldpart * 4 : 0;
 }
 
@@ -126,7 +128,7 @@ int run(Product& p, float* part, hipStream_t s) {
   if (a.M == 0) return GT_OK;
   if (a.splits < 1) return fail("layer product: too many tiles");
   if (a.splits > 1) {
-    a.e.mode = kEpiPart;
+    a.e.epi = kEpiPart;
     a.e.part = part;
   }
   GT_TRY(launch_product(p.dtype, p.layout, p.tile, p.reg, a, s), "layer product");
@@ -134,12 +136,16 @@ int run(Product& p, float* part, hipStream_t s) {
   return GT_OK;
 }
 
-// Whether an output row (and what is added to it) takes 4-element accesses.
-bool quads(int64_t n, std::initializer_list<std::pair<const void*, int64_t>> rows, int64_t bytes) {
-  if (n % 4) return false;
-  for (const auto& r : rows)
-    if (r.first && (!aligned(r.first, bytes) || r.second % 4)) return false;
-  return true;
+// Rows of n elements of sz bytes (pointer and leading dimension; null: none): 2
+// if all take accesses of 8 elements, 1 of 4, 0 of one.
+int width(int64_t n, std::initializer_list<std::pair<const void*, int64_t>> rows, int64_t sz) {
+  for (int w = 2; w >= 1; --w) {
+    const int64_t e = 4 * w, bytes = std::min<int64_t>(16, e * sz);
+    bool ok = n % e == 0;
+    for (const auto& r : rows) ok = ok && (!r.first || (aligned(r.first, bytes) && r.second % e == 0));
+    if (ok) return w;
+  }
+  return 0;
 }
 
 int extent(int64_t v, int64_t least, const char* name) {
@@ -200,9 +206,9 @@ Product linear_product(const gt_linear_args& q) {
   a.N = q.N;
   a.K = q.K;
   Epilogue& e = a.e;
-  e.mode = kEpiLinear;
   e.act = q.act & ~GT_ACT_GATED;
   e.gated = q.act & GT_ACT_GATED ? 1 : 0;
+  e.epi = e.gated ? kEpiGated : kEpiLinear;
   e.out_f32 = q.out_dtype == GT_F32 ? 1 : 0;
   e.Y = q.Y;
   e.ldy = q.ldy;
@@ -211,11 +217,8 @@ Product linear_product(const gt_linear_args& q) {
   e.bias = q.bias;
   e.R = q.R;
   e.ldr = q.ldr;
-  const int64_t b = 4 * size_of(q.dtype);
-  e.vec = quads(q.N, {{q.P, q.ldp}, {q.bias, 0}, {q.R, q.ldr}}, b) &&
-                  quads(q.N, {{q.Y, q.ldy}}, 4 * size_of(q.out_dtype))
-              ? 1
-              : 0;
+  e.vec = std::min(width(q.N, {{q.P, q.ldp}, {q.bias, 0}, {q.R, q.ldr}}, size_of(q.dtype)),
+                   width(q.N, {{q.Y, q.ldy}}, size_of(q.out_dtype)));
   choose(&p, true);
   return p;
 }
@@ -256,11 +259,11 @@ struct LinearGrad {
 };
 
 void output(Epilogue* e, void* y, int64_t ldy, bool f32, int64_t n, int64_t sz) {
-  e->mode = kEpiLinear;
+  e->epi = kEpiPlain;
   e->Y = y;
   e->ldy = ldy;
   e->out_f32 = f32 ? 1 : 0;
-  e->vec = quads(n, {{y, ldy}}, 4 * (f32 ? 4 : sz)) ? 1 : 0;
+  e->vec = width(n, {{y, ldy}}, f32 ? 4 : sz);
 }
 
 LinearGrad linear_grad(const gt_linear_grad_args& q, void* ws) {
@@ -372,9 +375,9 @@ Experts experts(const gt_experts_args& q, void* ws) {
     a.gather_div = q.k;
     a.a_rows = q.T;
     Epilogue& e = a.e;
-    e.mode = kEpiLinear;
     e.act = q.act & ~GT_ACT_GATED;
     e.gated = q.act & GT_ACT_GATED ? 1 : 0;
+    e.epi = e.gated ? kEpiGated : kEpiLinear;
     e.out_f32 = q.dtype == GT_F32 ? 1 : 0;
     e.Y = x.H;
     e.ldy = ldh;
@@ -382,7 +385,7 @@ Experts experts(const gt_experts_args& q, void* ws) {
     e.ldp = q.ldp;
     e.bias = q.b1;
     e.sbias = wide;
-    e.vec = quads(q.H, {{q.P, q.ldp}, {q.b1, 0}}, 4 * sz) ? 1 : 0;
+    e.vec = width(q.H, {{q.P, q.ldp}, {q.b1, 0}, {x.H, ldh}}, sz);
     choose(&x.up, true);
   }
   {
@@ -400,13 +403,13 @@ Experts experts(const gt_experts_args& q, void* ws) {
     a.offsets = q.offsets;
     a.groups = q.E;
     Epilogue& e = a.e;
-    e.mode = kEpiLinear;
+    e.epi = kEpiLinear;
     e.out_f32 = 1;
     e.Y = x.O;
     e.ldy = x.ldo;
     e.bias = q.b2;
     e.sbias = q.D;
-    e.vec = quads(q.D, {{q.b2, 0}}, 4 * sz) ? 1 : 0;
+    e.vec = std::min(width(q.D, {{q.b2, 0}}, sz), width(q.D, {{x.O, x.ldo}}, 4));
     choose(&x.down, true);
   }
   const int64_t part = std::max(x.up.part, x.down.part);
@@ -479,7 +482,7 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     a.N = q.H;
     a.K = q.D;
     Epilogue& e = a.e;
-    e.mode = kEpiSlope;
+    e.epi = kEpiSlope;
     e.act = q.act & ~GT_ACT_GATED;
     e.gated = q.act & GT_ACT_GATED ? 1 : 0;
     e.Y = g.dP;
@@ -492,7 +495,7 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     e.order = q.order;
     e.entries = g.R;
     e.wide = g.wide;
-    e.vec = quads(q.H, {{q.P, q.ldp}}, 4 * sz) && g.ldp % 4 == 0 ? 1 : 0;
+    e.vec = width(q.H, {{q.P, q.ldp}, {g.dP, g.ldp}, {g.Hw, g.ldh}}, sz);
     choose(&g.dh, false);
     const TileShape& t = kTile[g.dh.tile];
     e.ldot = static_cast<int64_t>(a.tilesN) * t.NWN;
@@ -523,8 +526,7 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     a.N = q.D;
     a.K = g.wide;
     g.dXs = s.take<float>(g.R * g.ldo * 4);
-    output(&a.e, g.dXs, g.ldo, true, g.ldo, sz);
-    a.e.vec = q.D % 4 == 0 ? 1 : 0;
+    output(&a.e, g.dXs, g.ldo, true, q.D, sz);
     choose(&g.dx, false);
   }
   if (q.dW1) {
@@ -606,7 +608,7 @@ int gt_linear_backward(const gt_linear_grad_args* a, void* ws, int64_t ws_bytes,
     q.dP = g.dP;
     q.lddp = g.lddp;
     q.part = g.sums;
-    q.vec = quads(a->N, {{a->dY, a->lddy}, {q.P, a->ldp}, {g.dP, g.lddp}}, 4 * size_of(a->dtype)) ? 1 : 0;
+    q.vec = width(a->N, {{a->dY, a->lddy}, {q.P, a->ldp}, {g.dP, g.lddp}}, size_of(a->dtype));
     GT_TRY(launch_act_grad(a->dtype, q, s), "gradient of the activation");
     if (a->db)
       GT_TRY(launch_join(g.sums, (a->M + kActRows - 1) / kActRows, g.wide, nullptr, 1, 0, 1, 1, a->db, s),
@@ -688,7 +690,7 @@ int gt_experts(const gt_experts_args* a, void* ws, int64_t ws_bytes, void* strea
   c.ldr = a->ldr;
   c.out = a->Y;
   c.ldout = a->ldy;
-  c.vec = quads(a->D, {{a->R, a->ldr}, {a->Y, a->ldy}}, 4 * size_of(a->dtype)) ? 1 : 0;
+  c.vec = width(a->D, {{a->R, a->ldr}, {a->Y, a->ldy}}, size_of(a->dtype));
   GT_TRY(launch_combine(a->dtype, c, s), "summing the experts' outputs");
   return GT_OK;
 }
@@ -748,7 +750,7 @@ int gt_experts_backward(const gt_experts_grad_args* a, void* ws, int64_t ws_byte
     c.place = a->place;
     c.out = a->dX;
     c.ldout = a->lddx;
-    c.vec = quads(a->D, {{a->dX, a->lddx}}, 4 * size_of(a->dtype)) ? 1 : 0;
+    c.vec = width(a->D, {{a->dX, a->lddx}}, size_of(a->dtype));
     GT_TRY(launch_combine(a->dtype, c, s), "summing the experts' gradients");
   }
   if (a->dW1) GT_CHECK(run(g.dw1, nullptr, s));

@@ -135,21 +135,19 @@ __device__ __forceinline__ int xswz(int k, int chunks) {
 // bias (bv, bu), the activation and the residual r, every step in fp32.
 template <typename T>
 __device__ __forceinline__ void linear_quad(const Epilogue& e, int64_t N, int64_t row, int64_t n,
-                                            int group, int left, f32x4 v, f32x4 u, f32x4 bv,
-                                            f32x4 bu, f32x4 r) {
+                                            int group, int left, bool gated, f32x4 v, f32x4 u,
+                                            f32x4 bv, f32x4 bu, f32x4 r) {
   const bool vec = e.vec != 0;
   v += bv;
   u += bu;
   if (e.P) {
     T* p = static_cast<T*>(e.P) + row * e.ldp + n;
     store4(p, v, left, vec);
-    if (e.gated) store4(p + N, u, left, vec);
+    if (gated) store4(p + N, u, left, vec);
   }
-  if (e.act != GT_ACT_NONE) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = act_value(e.act, v[i]);
-  }
-  if (e.gated) v *= u;
+  for (int i = 0; i < 4; ++i) v[i] = act_value(e.act, v[i]);
+  if (gated) v *= u;
   v += r;
   const int64_t at = group * e.sY + row * e.ldy + n;
   if (e.out_f32)
@@ -179,76 +177,150 @@ struct EpiSums {
   f32x4 g, u;  // a lane's columns of dP, summed over its rows
 };
 
-// RP rows of a wavefront's tile, row h + r of it in LDS at mine + r·WN·4. A lane
-// keeps its column quad and takes U rows at a time: what they need from memory (the
-// residual, the pre-activations) is loaded for all of them before the first is
-// stored, since an output may be the residual itself.
-template <int DT, int WN, int XM, int RP, int BN>
-__device__ __forceinline__ void epilogue_rows(const ProductArgs& a, const EpiPlace& p, int h,
-                                              const char* mine, int lane, EpiSums& sums) {
+// RP rows of a wavefront's tile of WM×WN, row h + r of it in LDS at mine + r·WN·4.
+template <int DT, int EPI, int WM, int WN, int XM, int RP, int BN>
+struct EpiRows {
   using T = typename Elem<DT>::T;
-  const Epilogue& e = a.e;
-  constexpr int CH = WN / 4;
-  auto chunk = [&](int r, int c) {
+  static constexpr int CH = WN / 4;
+  static constexpr bool G = EPI == kEpiGated;
+  const ProductArgs& a;
+  const EpiPlace& p;
+  int h;
+  const char* mine;
+  int lane;
+
+  __device__ __forceinline__ f32x4 chunk(int r, int c) const {
     return *reinterpret_cast<const f32x4*>(mine + r * (WN * 4) + ((c ^ (r & XM)) << 4));
-  };
-  // the column of chunk c (not gated)
-  auto col = [&](int c) { return p.col + (c < CH / 2 ? 0 : BN / 2 - WN / 2) + c * 4; };
-  if (e.mode == kEpiPart) {
+  }
+  // the column of chunk c (gated: of the gate's)
+  __device__ __forceinline__ int64_t col(int c) const {
+    return p.col + (G || c < CH / 2 ? 0 : BN / 2 - WN / 2) + c * 4;
+  }
+
+  // A whole tile of aligned rows of whole octets: 16-byte accesses, nothing checked.
+  // The residuals of U rows are loaded before the first of them is stored (an output may
+  // be the residual itself) and while the U rows before them are worked on.
+  template <int ACT>
+  __device__ __forceinline__ void whole() const {
+    const Epilogue& e = a.e;
+    constexpr int LR = (G ? CH / 2 : CH) / 2;   // lanes a row
+    constexpr int STEP = 64 / LR;
+    constexpr int U = EPI == kEpiPlain ? 1 : RP / STEP >= 4 ? 4 : RP / STEP >= 1 ? RP / STEP : 1;
+    const int c = lane % LR * 2, first = lane / LR;
+    const int64_t n = col(c), row0 = p.row + h + first;
+    oct bv{}, bu{};
+    const T* R = nullptr;
+    T* P = nullptr;
+    if constexpr (EPI != kEpiPlain) {
+      if (e.bias) {
+        const T* b = static_cast<const T*>(e.bias) + p.group * e.sbias + n;
+        bv = load8(b);
+        if constexpr (G) bu = load8(b + a.N);
+      }
+      if (e.R) R = static_cast<const T*>(e.R) + row0 * e.ldr + n;
+      if (e.P) P = static_cast<T*>(e.P) + row0 * e.ldp + n;
+    }
+    char* Y = static_cast<char*>(e.Y) + (p.group * e.sY + row0 * e.ldy + n) * (e.out_f32 ? 4 : sizeof(T));
+    const int64_t ystep = STEP * e.ldy * (e.out_f32 ? 4 : sizeof(T));
+    oct res[U], next[U];
+    if (R) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) next[i] = load8(R + i * STEP * e.ldr);
+    }
+#pragma unroll 1
+    for (int r0 = first; r0 < RP; r0 += U * STEP) {
+      if (R) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) res[i] = next[i];
+        R += U * STEP * e.ldr;
+        if (r0 + U * STEP < RP) {
+#pragma unroll
+          for (int i = 0; i < U; ++i) next[i] = load8(R + i * STEP * e.ldr);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int r = r0 + i * STEP;
+        oct v{chunk(r, c) + bv.a, chunk(r, c + 1) + bv.b};
+        oct u{};
+        if constexpr (G) u = oct{chunk(r, c + CH / 2) + bu.a, chunk(r, c + CH / 2 + 1) + bu.b};
+        if (P) {
+          store8(P, v);
+          if constexpr (G) store8(P + a.N, u);
+          P += STEP * e.ldp;
+        }
+        if constexpr (ACT != GT_ACT_NONE) act8<ACT>(v);
+        if constexpr (G) {
+          v.a *= u.a;
+          v.b *= u.b;
+        }
+        if (R) {
+          v.a += res[i].a;
+          v.b += res[i].b;
+        }
+        if (e.out_f32)
+          store8(reinterpret_cast<float*>(Y), v);
+        else
+          store8(reinterpret_cast<T*>(Y), v);
+        Y += ystep;
+      }
+    }
+  }
+
+  // Any tile: a quad a lane, every row checked.
+  __device__ __forceinline__ void edge() const {
+    constexpr int LR = G ? CH / 2 : CH;
+    constexpr int STEP = 64 / LR;
+    constexpr int U = RP / STEP >= 2 ? 2 : 1;
+    const int c = lane % LR;
+    const int64_t n = col(c);
+    const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
+    if (left <= 0) return;
+    const f32x4 bv = bias_quad<T>(a.e, n, p.group, left);
+    const f32x4 bu = G ? bias_quad<T>(a.e, n + a.N, p.group, left) : f32x4{};
+#pragma unroll 1
+    for (int r0 = lane / LR; r0 < RP; r0 += U * STEP) {
+      f32x4 res[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int64_t row = p.row + h + r0 + i * STEP;
+        res[i] = row < p.row_end ? residual_quad<T>(a.e, row, n, left) : f32x4{};
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int r = r0 + i * STEP;
+        const int64_t row = p.row + h + r;
+        if (row < p.row_end)
+          linear_quad<T>(a.e, a.N, row, n, p.group, left, G, chunk(r, c),
+                         G ? chunk(r, c + CH / 2) : f32x4{}, bv, bu, res[i]);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void part() const {
+    const Epilogue& e = a.e;
     const int c = lane % CH;
     const bool up = e.gated && c >= CH / 2;
     const int64_t n = up ? p.col + (c - CH / 2) * 4 : e.gated ? p.col + c * 4 : col(c);
-    float* const base = e.part + static_cast<int64_t>(p.slice) * a.M * e.ldpart + n +
-                        (up ? e.ldpart / 2 : 0);
-    for (int r = lane / CH; r < RP; r += 64 / CH) {
-      const int64_t row = p.row + h + r;
-      if (row < p.row_end && n < a.N) *reinterpret_cast<f32x4*>(base + row * e.ldpart) = chunk(r, c);
-    }
-  } else if (e.mode == kEpiLinear) {
-    auto rows = [&](auto gated) __attribute__((always_inline)) {
-      constexpr bool G = decltype(gated)::value;
-      constexpr int LR = G ? CH / 2 : CH;      // lanes a row
-      constexpr int STEP = 64 / LR;
-      constexpr int U = RP / STEP >= 4 ? 4 : RP / STEP;
-      const int c = lane % LR;
-      const int64_t n = G ? p.col + c * 4 : col(c);
-      const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
-      f32x4 bv{}, bu{};
-      if (left > 0) {
-        bv = bias_quad<T>(e, n, p.group, left);
-        if constexpr (G) bu = bias_quad<T>(e, n + a.N, p.group, left);
-      }
-      for (int r0 = lane / LR; r0 < RP; r0 += U * STEP) {
-        f32x4 res[U];
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const int64_t row = p.row + h + r0 + i * STEP;
-          res[i] = f32x4{};
-          if (row < p.row_end && left > 0) res[i] = residual_quad<T>(e, row, n, left);
-        }
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const int r = r0 + i * STEP;
-          const int64_t row = p.row + h + r;
-          if (row < p.row_end && left > 0)
-            linear_quad<T>(e, a.N, row, n, p.group, left, chunk(r, c),
-                           G ? chunk(r, c + CH / 2) : f32x4{}, bv, bu, res[i]);
-        }
-      }
-    };
-    if (e.gated)
-      rows(std::true_type{});
-    else
-      rows(std::false_type{});
-  } else {
-    // dH arrived: H = act(P) (times up), w the row's weight;
-    // dP = w·dH·act'(P) (gated: ·up, and w·dH·act(gate) for up), Hw = w·H
+    if (n >= a.N) return;
+    float* out = e.part + (static_cast<int64_t>(p.slice) * a.M + p.row + h) * e.ldpart + n +
+                 (up ? e.ldpart / 2 : 0);
+#pragma unroll 1
+    for (int r = lane / CH; r < RP; r += 64 / CH)
+      if (p.row + h + r < p.row_end) *reinterpret_cast<f32x4*>(out + r * e.ldpart) = chunk(r, c);
+  }
+
+  // dH arrived: H = act(P) (times up), w the row's weight;
+  // dP = w·dH·act'(P) (gated: ·up, and w·dH·act(gate) for up), Hw = w·H
+  __device__ __forceinline__ void slope(EpiSums& sums) const {
+    const Epilogue& e = a.e;
     constexpr int STEP = 64 / CH;
     constexpr int U = RP / STEP >= 4 ? 4 : RP / STEP;
     const int c = lane % CH;
     const int64_t n = col(c);
     const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
     const bool vec = e.vec != 0;
+#pragma unroll 1
     for (int r0 = lane / CH; r0 < RP; r0 += U * STEP) {
       f32x4 gate[U], up[U];
       float w[U];
@@ -301,7 +373,29 @@ __device__ __forceinline__ void epilogue_rows(const ProductArgs& a, const EpiPla
       }
     }
   }
-}
+
+  __device__ __forceinline__ void run(EpiSums& sums) const {
+    const Epilogue& e = a.e;
+    if constexpr (EPI == kEpiPart) {
+      part();
+    } else if constexpr (EPI == kEpiSlope) {
+      slope(sums);
+    } else {
+      const bool all = e.vec == 2 && p.row + WM <= p.row_end &&
+                       p.col + (G ? WN / 2 : BN / 2 + WN / 2) <= a.N;
+      if (!all)
+        edge();
+      else if (EPI == kEpiPlain || e.act == GT_ACT_NONE)
+        whole<GT_ACT_NONE>();
+      else if (e.act == GT_ACT_SILU)
+        whole<GT_ACT_SILU>();
+      else if (e.act == GT_ACT_GELU)
+        whole<GT_ACT_GELU>();
+      else
+        whole<GT_ACT_RELU>();
+    }
+  }
+};
 
 // The column sums of a wavefront's rows, joined over its lanes.
 template <int WN, int BN>
@@ -330,28 +424,34 @@ __device__ __forceinline__ void epilogue_sums(const ProductArgs& a, const EpiPla
 // ---- the kernel ------------------------------------------------------------
 
 // Measured (bf16, one MI355X): see the instances' list in product_inst.hip.
-template <int DT, int I, bool AX, bool BX, int BM, int BN, int NWM, int NWN, int NS, bool REG>
+template <int DT, int I, bool AX, bool BX, int BM, int BN, int NWM, int NWN, int KB, int NS, bool REG, int EPI>
 __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductArgs a) {
   using T = typename Elem<DT>::T;
   constexpr int SZ = DT == 1 ? 2 : 4;
   constexpr int VEC = 16 / SZ;
-  constexpr int BK = 128 / SZ;           // k of a stage
+  constexpr int BK = KB / SZ;            // k of a stage, KB bytes of it
+  constexpr int CPK = KB / 16;           // 16-byte chunks of a KC row
   constexpr int NW = NWM * NWN;
   constexpr int WM = BM / NWM, WN = BN / NWN;
   constexpr int TM = WM / I, TN = WN / I;
   constexpr int HN = WN / 2;             // a wavefront's columns in each half of the tile
   constexpr int G = 64 / I;              // lane groups: 16-byte chunks of k a chunk-step
-  constexpr int NCS = 8 / G;             // chunk-steps of a stage
+  constexpr int NCS = CPK / G;           // chunk-steps of a stage
   using acc_t = typename AccT<I>::type;
   static_assert(TM >= 1 && TN >= 2 && TN % 2 == 0, "tile too small for its wavefronts");
   static_assert(!REG || NS == 2, "the register path has two slots");
-  constexpr int INA = BM / 8, INB = BN / 8;   // 1 KiB load instructions of a stage
+  static_assert((CPK == 8 || CPK == 4) && NCS >= 2, "stage depth");
+  constexpr int INA = BM * CPK / 64, INB = BN * CPK / 64;   // 1 KiB load instructions of a stage
   constexpr int NA = (INA + NW - 1) / NW, NB = (INB + NW - 1) / NW;  // of a wavefront
   static_assert(NW % 2 == 0, "chunks of a lane");
   static_assert(INA % NW == 0 || NW % INA == 0, "loads of A");
   static_assert(INB % NW == 0 || NW % INB == 0, "loads of B");
-  constexpr uint32_t STAGE = (BM + BN) * 128u;
-  constexpr uint32_t BOFF = BM * 128u;        // B inside a slot
+  constexpr uint32_t KBu = KB;
+  constexpr uint32_t STAGE = (BM + BN) * KBu;
+  constexpr uint32_t BOFF = BM * KBu;         // B inside a slot
+  // XOR of a KC row's chunks: the 16 rows of a fragment read lie in distinct 16-byte
+  // banks of 256 bytes
+  auto kswz = [](int r) { return CPK == 8 ? (r >> 1) & 7 : (r >> 2) & 3; };
 
   extern __shared__ char smem[];
   const int lane = threadIdx.x & 63;
@@ -389,9 +489,9 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
       mend = s.hi;
     }
   }
-  const bool gated = a.e.gated != 0;
-  const int64_t wide = (gated && a.e.mode != kEpiSlope) ? 2 * a.N : a.N;  // B's columns
-  const bool halves = wide != a.N;
+  // whether the tile's second half holds up values, B's columns N on
+  const bool halves = EPI == kEpiGated || (EPI == kEpiPart && BX && !AX && a.e.gated != 0);
+  const int64_t wide = halves ? 2 * a.N : a.N;   // B's columns
   const int64_t n0 = static_cast<int64_t>(tn) * (halves ? BN / 2 : BN);
   // stored column of tile column c is n0 + c, plus this for the second half
   const int64_t hoff = halves ? a.N - BN / 2 : 0;
@@ -402,19 +502,18 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   // ---- the stages of this K slice
   int st0, st1;
   {
-    const int64_t all = (kend - k0 + BK - 1) / BK;
-    st0 = uni(static_cast<int>(all * z / a.splits));
-    st1 = uni(static_cast<int>(all * (z + 1) / a.splits));
+    const int all = uni(static_cast<int>((kend - k0 + BK - 1) / BK));
+    st0 = EPI == kEpiPart ? min(all, z * a.per_slice) : 0;
+    st1 = EPI == kEpiPart ? min(all, st0 + a.per_slice) : all;
   }
   const int nst = st1 - st0;
   k0 += static_cast<int64_t>(st0) * BK;
   if (k0 + static_cast<int64_t>(nst) * BK < kend) kend = k0 + static_cast<int64_t>(nst) * BK;
 
   // ---- where each of this lane's chunks of a stage lies
-  // Load instruction p fills the slots 64·p + lane of its operand's part. KC: 8
-  // chunks a row r, chunk c in slot c ^ ((r >> 1) & 7), so that the 16 rows of a
-  // fragment read lie in distinct 16-byte banks of 256 bytes. XC: rows k of
-  // chunks of x, chunk c in slot c ^ xswz(k).
+  // Load instruction p fills the slots 64·p + lane of its operand's part. KC: CPK
+  // chunks a row r, chunk c in slot c ^ kswz(r). XC: rows k of chunks of x, chunk c in
+  // slot c ^ xswz(k).
   constexpr int CA = BM / VEC, CB = BN / VEC;   // chunks of an XC row
   uint32_t offA[NA], offB[NB];
   const T* ptrA[REG ? NA : 1];
@@ -426,7 +525,7 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   for (int i = 0; i < NA; ++i) {
     const int s = (((wave + NW * i) % INA) << 6) + lane;
     if constexpr (!AX) {
-      const int r = s >> 3, c = (s & 7) ^ ((r >> 1) & 7);
+      const int r = s / CPK, c = (s % CPK) ^ kswz(r);
       kA[i] = c * VEC;
       int64_t row = r;
       bool ok = m0 + r < mend;
@@ -457,7 +556,7 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   for (int i = 0; i < NB; ++i) {
     const int s = (((wave + NW * i) % INB) << 6) + lane;
     if constexpr (!BX) {
-      const int r = s >> 3, c = (s & 7) ^ ((r >> 1) & 7);
+      const int r = s / CPK, c = (s % CPK) ^ kswz(r);
       kB[i] = c * VEC;
       const bool ok = n0 + r < wide;
       if constexpr (REG) {
@@ -562,7 +661,7 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   // ---- fragments: I rows (columns) × 16 bytes of k a lane, chunk-step cs at k chunks cs·G …
   // tile column of fragment j: half j / (TN/2) of the tile
   auto bcol = [&](int j) { return (j < TN / 2 ? 0 : BN / 2) + wn * HN + (j % (TN / 2)) * I; };
-  const uint32_t sw = static_cast<uint32_t>((lI >> 1) & 7);
+  const uint32_t sw = static_cast<uint32_t>(kswz(lI));
   uint32_t fa[AX ? TM : NCS], fb[BX ? TN : NCS];
   // XC bf16: in a group of 16 lanes, lane i addresses row i >> 2, columns 4·(i & 3)
   const int i16 = lane & 15, g16 = lane >> 4;
@@ -577,7 +676,7 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   } else {
 #pragma unroll
     for (int c = 0; c < NCS; ++c)
-      fa[c] = (wm * WM + lI) * 128u + ((static_cast<uint32_t>(grp + c * G) ^ sw) << 4);
+      fa[c] = (wm * WM + lI) * KBu + ((static_cast<uint32_t>(grp + c * G) ^ sw) << 4);
   }
   if constexpr (BX) {
 #pragma unroll
@@ -588,7 +687,7 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   } else {
 #pragma unroll
     for (int c = 0; c < NCS; ++c)
-      fb[c] = BOFF + (wn * HN + lI) * 128u + ((static_cast<uint32_t>(grp + c * G) ^ sw) << 4);
+      fb[c] = BOFF + (wn * HN + lI) * KBu + ((static_cast<uint32_t>(grp + c * G) ^ sw) << 4);
   }
   auto read_x = [&](const char* st, uint32_t at, int cs, int rowb) __attribute__((always_inline)) {
     u32x4 v;
@@ -613,13 +712,13 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
       if constexpr (BX)
         vb[set][r] = read_x(st, fb[r], cs, BN * SZ);
       else
-        vb[set][r] = *reinterpret_cast<const u32x4*>(st + fb[cs] + (bcol(r) - wn * HN) * 128);
+        vb[set][r] = *reinterpret_cast<const u32x4*>(st + fb[cs] + (bcol(r) - wn * HN) * KB);
     } else {
       const int t = r - TN;
       if constexpr (AX)
         va[set][t] = read_x(st, fa[t], cs, BM * SZ);
       else
-        va[set][t] = *reinterpret_cast<const u32x4*>(st + fa[cs] + t * (I * 128));
+        va[set][t] = *reinterpret_cast<const u32x4*>(st + fa[cs] + t * (I * KB));
     }
   };
 
@@ -746,10 +845,12 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    epilogue_rows<DT, WN, XM, RP, BN>(a, place, h * RP, mine, lane, sums);
+    EpiRows<DT, EPI, WM, WN, XM, RP, BN>{a, place, h * RP, mine, lane}.run(sums);
     __builtin_amdgcn_wave_barrier();
   }
-  if (a.e.mode == kEpiSlope && a.e.colsum) epilogue_sums<WN, BN>(a, place, lane, sums);
+  if constexpr (EPI == kEpiSlope) {
+    if (a.e.colsum) epilogue_sums<WN, BN>(a, place, lane, sums);
+  }
 }
 
 }  // namespace gt

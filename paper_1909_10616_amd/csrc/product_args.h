@@ -6,23 +6,27 @@
 
 namespace gt {
 
-// What becomes of the product's rows.
-enum EpiMode : int32_t {
-  kEpiLinear = 0,  // + bias, activation (gated or not), + residual, P kept
+// What becomes of the product's rows; each is a kernel of its own, so that none carries
+// the others' code (a launch fetches its instructions cold).
+enum Epi : int {
+  kEpiPlain = 0,   // Y alone
   kEpiPart = 1,    // a K slice's sums, as they are, into `part`
-  kEpiSlope = 2,   // the product is dH of the experts: dP, w·H, Σ dH·H, column sums of dP
+  kEpiLinear = 2,  // + bias, activation, + residual, P kept
+  kEpiGated = 3,   // the same with a gate and an up half
+  kEpiSlope = 4,   // the product is dH of the experts: dP, w·H, Σ dH·H, column sums of dP
 };
 
 struct Epilogue {
-  int32_t mode;
+  int32_t epi;
   int32_t act;       // gt_act
   int32_t gated;     // columns n and N + n are a gate and its up value
   int32_t out_f32;   // Y in fp32, else in the operands' type
-  int32_t vec;       // every row and pointer takes 4-element accesses
+  int32_t vec;       // every row and pointer takes accesses of: 1: 4 elements, 2: 8 (16 bytes
+                     // at least), 0: one
   int32_t pad;
   void* Y;           // [rows][ldy]; group g at Y + g·sY (groups along k)
   int64_t ldy, sY;
-  void* P;           // kept pre-activations (kEpiLinear) or given ones (kEpiSlope), or null
+  void* P;           // kept pre-activations or the given ones (kEpiSlope), or null
   int64_t ldp;
   const void* bias;  // per group sbias apart
   int64_t sbias;
@@ -54,6 +58,7 @@ struct ProductArgs {
   const int32_t* gather;   // KC A: row r is A's row gather[r] / gather_div
   int32_t gather_div;
   int32_t splits;       // K slices (grid y)
+  int32_t per_slice;    // stages of a slice
   int64_t a_rows;       // rows A has (gather)
   int32_t tilesM, tilesN;
   Epilogue e;
@@ -62,20 +67,23 @@ struct ProductArgs {
 // How the operands lie: A and B along k or along their own index.
 enum Layout : int { kXW = 0, kPWt = 1, kXtP = 2 };  // KC·XC, KC·KC, XC·XC
 
-// The tiles that are built: rows, columns, wavefronts along each, ring slots, MFMA size.
+// The tiles that are built: rows, columns, wavefronts along each, bytes of k in a stage,
+// ring slots, MFMA size.
 struct TileShape {
-  int BM, BN, NWM, NWN, NS, I;
+  int BM, BN, NWM, NWN, KB, NS, I;
 };
 constexpr int kTiles = 4;
 constexpr TileShape kTile[kTiles] = {
-    {256, 256, 2, 2, 2, 32},  // 0: bf16, DMA only
-    {128, 128, 2, 2, 2, 32},  // 1
-    {64, 64, 2, 2, 3, 16},    // 2
-    {16, 128, 1, 4, 4, 16},   // 3: not for kXtP
+    {256, 256, 2, 4, 128, 2, 32},  // 0: bf16, DMA only
+    {128, 128, 2, 2, 128, 2, 32},  // 1
+    {64, 64, 2, 2, 128, 3, 16},    // 2
+    {16, 128, 1, 4, 128, 4, 16},   // 3: not for kXtP
 };
 
-// Launches the product kernel of a tile (reg: the register path). The grid is
-// (tilesM·tilesN, splits, groups along k or 1).
+// Launches the product kernel of a tile (reg: the register path) with the epilogue
+// a.e.epi: kXW has kEpiPart, kEpiLinear and kEpiGated, kPWt kEpiPlain, kEpiPart and
+// kEpiSlope, kXtP kEpiPlain and kEpiPart. The grid is (tilesM·tilesN, splits, groups
+// along k or 1).
 hipError_t launch_product(int dtype, int layout, int tile, bool reg, const ProductArgs& a,
                           hipStream_t s);
 

@@ -31,30 +31,45 @@ hipError_t launch_with_lds(F fn, std::atomic<uint64_t>& attr, const ProductArgs&
   return hipGetLastError();
 }
 
-template <int TILE, bool REG>
+template <int TILE, bool REG, int EPI>
 hipError_t go(const ProductArgs& a, hipStream_t s) {
   constexpr TileShape t = kTile[TILE];
-  constexpr int NS = REG ? 2 : t.NS;
-  constexpr auto* fn =
-      product_kernel<LP_DT, t.I, LP_LAY == kXtP, LP_LAY != kPWt, t.BM, t.BN, t.NWM, t.NWN, NS, REG>;
+  constexpr int KB = REG ? 128 : t.KB, NS = REG ? 2 : t.NS;
+  constexpr auto* fn = product_kernel<LP_DT, t.I, LP_LAY == kXtP, LP_LAY != kPWt, t.BM, t.BN, t.NWM,
+                                      t.NWN, KB, NS, REG, EPI>;
   const dim3 grid(static_cast<unsigned>(a.tilesM) * static_cast<unsigned>(a.tilesN),
                   static_cast<unsigned>(a.splits),
                   a.along_k ? static_cast<unsigned>(a.groups) : 1u);
   static std::atomic<uint64_t> attr{0};
   return launch_with_lds(fn, attr, a, grid, dim3(64 * t.NWM * t.NWN),
-                         static_cast<size_t>(NS) * (t.BM + t.BN) * 128, s);
+                         static_cast<size_t>(NS) * (t.BM + t.BN) * KB, s);
+}
+
+template <int TILE, bool REG>
+hipError_t by_epilogue(const ProductArgs& a, hipStream_t s) {
+  if (a.e.epi == kEpiPart) return go<TILE, REG, kEpiPart>(a, s);
+#if LP_LAY == 0
+  if (a.e.epi == kEpiLinear) return go<TILE, REG, kEpiLinear>(a, s);
+  if (a.e.epi == kEpiGated) return go<TILE, REG, kEpiGated>(a, s);
+#else
+  if (a.e.epi == kEpiPlain) return go<TILE, REG, kEpiPlain>(a, s);
+#endif
+#if LP_LAY == 1
+  if (a.e.epi == kEpiSlope) return go<TILE, REG, kEpiSlope>(a, s);
+#endif
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
 
 hipError_t LP_NAME(LP_DT, LP_LAY)(int tile, bool reg, const ProductArgs& a, hipStream_t s) {
 #if LP_DT == 1
-  if (tile == 0 && !reg) return go<0, false>(a, s);
+  if (tile == 0 && !reg) return by_epilogue<0, false>(a, s);
 #endif
-  if (tile == 1) return reg ? go<1, true>(a, s) : go<1, false>(a, s);
-  if (tile == 2) return reg ? go<2, true>(a, s) : go<2, false>(a, s);
+  if (tile == 1) return reg ? by_epilogue<1, true>(a, s) : by_epilogue<1, false>(a, s);
+  if (tile == 2) return reg ? by_epilogue<2, true>(a, s) : by_epilogue<2, false>(a, s);
 #if LP_LAY != 2
-  if (tile == 3) return reg ? go<3, true>(a, s) : go<3, false>(a, s);
+  if (tile == 3) return reg ? by_epilogue<3, true>(a, s) : by_epilogue<3, false>(a, s);
 #endif
   return hipErrorInvalidValue;
 }
