@@ -14,8 +14,24 @@ namespace gt {
 // epilogue of a.e to every row (with groups along m: below the last offset).
 hipError_t launch_reduce(int dtype, const ProductArgs& a, hipStream_t s);
 
+// A matrix (or `groups` of them) copied to rows of whole 16-byte chunks, zero beyond its
+// columns; half > 0: its two halves of cols / 2 columns each begin at 0 and half.
+struct PadJob {
+  const void* src;
+  void* dst;
+  int64_t groups, rows, cols;
+  int64_t ld, sgroup;     // of src
+  int64_t ldd, half;      // of dst, groups one after the other
+};
+constexpr int kPadJobs = 3;
+struct PadJobs {
+  PadJob job[kPadJobs];
+  int n;
+};
+hipError_t launch_pad(int dtype, const PadJobs& jobs, hipStream_t s);
+
 // Rows a block of the gradient kernel sums into one row of its partial sums.
-constexpr int kActRows = 64;
+constexpr int kActRows = 16;
 // dP = dY·act'(P) (gated: both halves), and each block's column sums of it into
 // part[block][wide] (part NULL: not wanted; dP NULL: only the sums).
 struct ActGradArgs {
@@ -29,6 +45,7 @@ struct ActGradArgs {
   int64_t lddp;
   float* part;
   int vec;
+  int pad;   // columns of dP beyond its last that are written as zero
 };
 hipError_t launch_act_grad(int dtype, const ActGradArgs& a, hipStream_t s);
 

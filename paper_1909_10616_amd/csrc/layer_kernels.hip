@@ -35,11 +35,33 @@ __device__ __forceinline__ int group_of_row(const int32_t* offsets, int groups, 
   return lo;
 }
 
+// ---- copies to aligned rows
+
+// One wavefront a row, a 16-byte chunk a lane. Bound by memory.
+template <typename T>
+__global__ __launch_bounds__(256) void pad_kernel(const PadJobs jobs) {
+  constexpr int VEC = 16 / sizeof(T);
+  const PadJob& j = jobs.job[blockIdx.y];
+  const int lane = threadIdx.x & 63;
+  const int64_t n = j.half > 0 ? j.cols / 2 : j.cols;   // columns of a half
+  for (int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); r < j.groups * j.rows;
+       r += static_cast<int64_t>(gridDim.x) * 4) {
+    const int64_t g = j.groups > 1 ? r / j.rows : 0, row = r - g * j.rows;
+    const T* src = static_cast<const T*>(j.src) + g * j.sgroup + row * j.ld;
+    T* dst = static_cast<T*>(j.dst) + r * j.ldd;
+    for (int64_t c = static_cast<int64_t>(lane) * VEC; c < j.ldd; c += 64 * VEC) {
+      const bool second = j.half > 0 && c >= j.half;
+      const int64_t col = second ? c - j.half : c;
+      *reinterpret_cast<u32x4*>(dst + c) = load_chunk<T, VEC>(src + (second ? n : 0) + col, n - col);
+    }
+  }
+}
+
 // ---- the join of K slices
 
 template <typename T>
 __global__ __launch_bounds__(256) void reduce_kernel(const ProductArgs a) {
-  const int64_t quads = (a.N + 3) / 4;
+  const int64_t quads = (written<T>(a.e, a.N) + 3) / 4;
   const int64_t rows = a.groups > 0 ? clamp_offset(a.offsets[a.groups], a.M) : a.M;
   const int64_t slice = a.M * a.e.ldpart;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < rows * quads;
@@ -47,9 +69,12 @@ __global__ __launch_bounds__(256) void reduce_kernel(const ProductArgs a) {
     const int64_t row = i / quads, n = (i - row * quads) * 4;
     const float* p = a.e.part + row * a.e.ldpart + n;
     f32x4 v{}, u{};
-    for (int z = 0; z < a.splits; ++z) {
-      v += *reinterpret_cast<const f32x4*>(p + z * slice);
-      if (a.e.gated) u += *reinterpret_cast<const f32x4*>(p + z * slice + a.e.ldpart / 2);
+    if (n < a.N) {
+#pragma unroll 4
+      for (int z = 0; z < a.splits; ++z) {
+        v += *reinterpret_cast<const f32x4*>(p + z * slice);
+        if (a.e.gated) u += *reinterpret_cast<const f32x4*>(p + z * slice + a.e.ldpart / 2);
+      }
     }
     const int group = a.groups > 0 ? group_of_row(a.offsets, a.groups, row) : 0;
     const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
@@ -62,65 +87,112 @@ __global__ __launch_bounds__(256) void reduce_kernel(const ProductArgs a) {
 
 // ---- the activation's gradient
 
-// 256 threads: 64 quads of columns, kActRows rows, a quarter of them a thread.
-template <typename T>
+// 256 threads: 64 column quads (octets, WIDE), kActRows rows, four of them a thread: all its
+// loads are out before the first is used. Bound by memory.
+template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void act_grad_kernel(const ActGradArgs a) {
-  __shared__ f32x4 sums[2][4][64];
+  constexpr int U = kActRows / 4, Q = WIDE ? 2 : 1;
+  __shared__ f32x4 sums[2][Q][4][64];
   const int q = threadIdx.x & 63, part = threadIdx.x >> 6;
-  const int64_t n = (static_cast<int64_t>(blockIdx.y) * 64 + q) * 4;
-  const int64_t r0 = static_cast<int64_t>(blockIdx.x) * kActRows;
-  const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
+  const int64_t n = (static_cast<int64_t>(blockIdx.y) * 64 + q) * 4 * Q;
+  const int64_t r0 = static_cast<int64_t>(blockIdx.x) * kActRows + part;
+  const int64_t left64 = a.N - n;
+  const int left = left64 < 4 ? static_cast<int>(left64) : 4;
   const bool vec = a.vec != 0;
-  f32x4 sg{}, su{};
-  if (left > 0) {
-    for (int r = part; r < kActRows; r += 4) {
-      const int64_t row = r0 + r;
-      if (row >= a.M) break;
-      const f32x4 dy = load4(static_cast<const T*>(a.dY) + row * a.lddy + n, left, vec);
-      f32x4 g = dy, u{};
-      if (a.P) {
-        const T* p = static_cast<const T*>(a.P) + row * a.ldp + n;
-        const f32x4 gate = load4(p, left, vec);
-        f32x4 up = f32x4{1.0f, 1.0f, 1.0f, 1.0f};
-        if (a.gated) up = load4(p + a.N, left, vec);
+  f32x4 dy[U][Q], gate[U][Q], up[U][Q];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float val, slope;
-          act_both(a.act, gate[i], &val, &slope);
-          g[i] = dy[i] * up[i] * slope;
-          u[i] = dy[i] * val;
+  for (int i = 0; i < U; ++i) {
+    const int64_t row = r0 + 4 * i;
+#pragma unroll
+    for (int j = 0; j < Q; ++j) dy[i][j] = gate[i][j] = up[i][j] = f32x4{};
+    if (left <= 0 || row >= a.M) continue;
+    const T* d = static_cast<const T*>(a.dY) + row * a.lddy + n;
+    const T* p = a.P ? static_cast<const T*>(a.P) + row * a.ldp + n : nullptr;
+    if constexpr (WIDE) {
+      const oct v = load8(d);
+      dy[i][0] = v.a;
+      dy[i][1] = v.b;
+      if (a.P) {
+        const oct g = load8(p);
+        gate[i][0] = g.a;
+        gate[i][1] = g.b;
+        if (a.gated) {
+          const oct u = load8(p + a.N);
+          up[i][0] = u.a;
+          up[i][1] = u.b;
         }
       }
-      if (a.dP) {
-        T* out = static_cast<T*>(a.dP) + row * a.lddp + n;
-        store4(out, g, left, vec);
-        if (a.gated) store4(out + a.N, u, left, vec);
+    } else {
+      dy[i][0] = load4(d, left, vec);
+      if (a.P) {
+        gate[i][0] = load4(p, left, vec);
+        if (a.gated) up[i][0] = load4(p + a.N, left, vec);
       }
-      sg += g;
-      su += u;
+    }
+  }
+  f32x4 sg[Q] = {}, su[Q] = {};
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int64_t row = r0 + 4 * i;
+    f32x4 g[Q], u[Q];
+#pragma unroll
+    for (int j = 0; j < Q; ++j) {
+      g[j] = dy[i][j];
+      u[j] = f32x4{};
+      if (a.P) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float val, slope;
+          act_both(a.act, gate[i][j][c], &val, &slope);
+          g[j][c] = dy[i][j][c] * slope;
+          u[j][c] = dy[i][j][c] * val;
+        }
+        if (a.gated) g[j] *= up[i][j];
+      }
+      sg[j] += g[j];
+      su[j] += u[j];
+    }
+    if (a.dP && left > 0 && row < a.M) {
+      T* out = static_cast<T*>(a.dP) + row * a.lddp + n;
+      if constexpr (WIDE) {
+        store8(out, oct{g[0], g[1]});
+        if (a.gated) store8(out + a.N, oct{u[0], u[1]});
+      } else {
+        store4(out, g[0], left, vec);
+        if (a.gated) store4(out + a.N, u[0], left, vec);
+        if (n + left == a.N)
+          for (int z = 0; z < a.pad; ++z) out[(a.gated ? a.N : 0) + left + z] = T(0);
+      }
     }
   }
   if (!a.part) return;
-  sums[0][part][q] = sg;
-  sums[1][part][q] = su;
+#pragma unroll
+  for (int j = 0; j < Q; ++j) {
+    sums[0][j][part][q] = sg[j];
+    sums[1][j][part][q] = su[j];
+  }
   __syncthreads();
   const int half = threadIdx.x >> 6;
   if (half >= (a.gated ? 2 : 1) || left <= 0) return;
-  const f32x4 t = (sums[half][0][q] + sums[half][1][q]) + (sums[half][2][q] + sums[half][3][q]);
   const int64_t wide = a.gated ? 2 * a.N : a.N;
   float* out = a.part + blockIdx.x * wide + half * a.N + n;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (i < left) out[i] = t[i];
+  for (int j = 0; j < Q; ++j) {
+    const f32x4* s = &sums[half][j][0][q];
+    const f32x4 t = (s[0] + s[64]) + (s[128] + s[192]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < left) out[4 * j + i] = t[i];
+  }
 }
 
 // ---- the join of column sums
 
-// 256 threads: 64 columns of a group, a quarter of the partial rows each.
-__global__ __launch_bounds__(256) void join_kernel(const float* part, int64_t rows, int64_t wide,
+// 1024 threads: 64 columns of a group, a sixteenth of the partial rows each.
+__global__ __launch_bounds__(1024) void join_kernel(const float* part, int64_t rows, int64_t wide,
                                                    const int32_t* offsets, int64_t most, int bm,
                                                    int per, float* out) {
-  __shared__ float sums[4][64];
+  __shared__ float sums[16][64];
   __shared__ int64_t span[2];
   const int g = static_cast<int>(blockIdx.y);
   int64_t r0 = 0, r1 = rows;
@@ -143,27 +215,35 @@ __global__ __launch_bounds__(256) void join_kernel(const float* part, int64_t ro
     r0 = span[0];
     r1 = span[1];
   }
-  const int c = threadIdx.x & 63, quarter = threadIdx.x >> 6;
+  const int c = threadIdx.x & 63, part16 = threadIdx.x >> 6;
   const int64_t n = static_cast<int64_t>(blockIdx.x) * 64 + c;
   float s = 0.0f;
-  if (n < wide)
-    for (int64_t r = r0 + quarter; r < r1; r += 4) s += part[r * wide + n];
-  sums[quarter][c] = s;
+  if (n < wide) {
+#pragma unroll 4
+    for (int64_t r = r0 + part16; r < r1; r += 16) s += part[r * wide + n];
+  }
+  sums[part16][c] = s;
   __syncthreads();
-  if (quarter == 0 && n < wide)
-    out[g * wide + n] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
+  if (part16 == 0 && n < wide) {
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t += sums[i][c];
+    out[g * wide + n] = t;
+  }
 }
 
 // ---- sorted copies of rows
 
-// One wavefront a row; VEC elements a lane where rows and pointers allow it.
-template <typename T, int VEC>
+// One wavefront a row, a 16-byte chunk a lane (WIDE: of the source too).
+template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void gather_kernel(const T* a, int64_t lda, T* da, const T* b,
                                                      int64_t ldb, T* db, int64_t ldd, int64_t cols,
                                                      const int32_t* order, const int32_t* offsets,
                                                      int E, int64_t entries, int k, int64_t tokens) {
+  constexpr int VEC = 16 / sizeof(T);
   const int lane = threadIdx.x & 63;
   const int64_t rows = clamp_offset(offsets[E], entries);
+  // (rows of ldd elements: zero beyond the columns)
   const T* src = blockIdx.y == 0 ? a : b;
   const int64_t lds = blockIdx.y == 0 ? lda : ldb;
   T* dst = blockIdx.y == 0 ? da : db;
@@ -172,39 +252,74 @@ __global__ __launch_bounds__(256) void gather_kernel(const T* a, int64_t lda, T*
        p += static_cast<int64_t>(gridDim.x) * 4) {
     const int32_t entry = order[p];
     const int64_t t = entry < 0 ? tokens : entry / k;
-    for (int64_t c = static_cast<int64_t>(lane) * VEC; c < cols; c += 64 * VEC) {
-      if constexpr (VEC > 1) {
-        u32x4 v{};
-        if (t < tokens) v = *reinterpret_cast<const u32x4*>(src + t * lds + c);
-        *reinterpret_cast<u32x4*>(dst + p * ldd + c) = v;
-      } else {
-        dst[p * ldd + c] = t < tokens ? src[t * lds + c] : T(0);
+    for (int64_t c = static_cast<int64_t>(lane) * VEC; c < ldd; c += 64 * VEC) {
+      u32x4 v{};
+      if (t < tokens) {
+        if constexpr (WIDE)
+          v = *reinterpret_cast<const u32x4*>(src + t * lds + c);
+        else
+          v = load_chunk<T, VEC>(src + t * lds + c, cols - c);
       }
+      *reinterpret_cast<u32x4*>(dst + p * ldd + c) = v;
     }
   }
 }
 
 // ---- sums back into the tokens' order
 
-template <typename T>
+// A quad (octet, WIDE) of a token's columns a thread; the rows of four slots at a time.
+template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
-  const int64_t quads = (a.D + 3) / 4;
+  constexpr int Q = WIDE ? 2 : 1;
+  const uint32_t per = static_cast<uint32_t>((a.D + 4 * Q - 1) / (4 * Q));
   const bool vec = a.vec != 0;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < a.T * quads;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < a.T * per;
        i += static_cast<int64_t>(gridDim.x) * 256) {
-    const int64_t t = i / quads, n = (i - t * quads) * 4;
+    const int64_t t = i / per, n = (i - t * per) * 4 * Q;
     const int left = a.D - n < 4 ? static_cast<int>(a.D - n) : 4;
-    f32x4 v{};
-    for (int s = 0; s < a.k; ++s) {
-      const int64_t p = a.place[t * a.k + s];
-      if (p < 0 || p >= a.entries) continue;
-      const f32x4 o = *reinterpret_cast<const f32x4*>(a.O + p * a.ldo + n);   // rows of whole quads
-      const float w = a.weights ? a.weights[t * a.k + s] : 1.0f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = fmaf(w, o[j], v[j]);
+    f32x4 v[Q] = {}, r[Q] = {};
+    if (a.R) {
+      const T* p = static_cast<const T*>(a.R) + t * a.ldr + n;
+      if constexpr (WIDE) {
+        const oct o = load8(p);
+        r[0] = o.a;
+        r[1] = o.b;
+      } else {
+        r[0] = load4(p, left, vec);
+      }
     }
-    if (a.R) v += load4(static_cast<const T*>(a.R) + t * a.ldr + n, left, vec);
-    store4(static_cast<T*>(a.out) + t * a.ldout + n, v, left, vec);
+    for (int s0 = 0; s0 < a.k; s0 += 4) {
+      f32x4 o[4][Q];
+      float w[4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        w[s] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < Q; ++j) o[s][j] = f32x4{};
+        if (s0 + s >= a.k) continue;
+        const int64_t p = a.place[t * a.k + s0 + s];
+        if (p < 0 || p >= a.entries) continue;
+        w[s] = a.weights ? a.weights[t * a.k + s0 + s] : 1.0f;
+#pragma unroll
+        for (int j = 0; j < Q; ++j)   // (rows of whole quads)
+          o[s][j] = *reinterpret_cast<const f32x4*>(a.O + p * a.ldo + n + 4 * j);
+      }
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        if (s0 + s < a.k) {
+#pragma unroll
+          for (int j = 0; j < Q; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[j][c] = fmaf(w[s], o[s][j][c], v[j][c]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < Q; ++j) v[j] += r[j];
+    T* out = static_cast<T*>(a.out) + t * a.ldout + n;
+    if constexpr (WIDE)
+      store8(out, oct{v[0], v[1]});
+    else
+      store4(out, v[0], left, vec);
   }
 }
 
@@ -271,8 +386,20 @@ bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p
 
 }  // namespace
 
+hipError_t launch_pad(int dtype, const PadJobs& jobs, hipStream_t s) {
+  int64_t rows = 0;
+  for (int i = 0; i < jobs.n; ++i) rows = std::max(rows, jobs.job[i].groups * jobs.job[i].rows);
+  if (rows == 0) return hipSuccess;
+  const dim3 grid(blocks_for(rows, 4), static_cast<unsigned>(jobs.n));
+  if (dtype == GT_BF16)
+    pad_kernel<uint16_t><<<grid, 256, 0, s>>>(jobs);
+  else
+    pad_kernel<float><<<grid, 256, 0, s>>>(jobs);
+  return hipGetLastError();
+}
+
 hipError_t launch_reduce(int dtype, const ProductArgs& a, hipStream_t s) {
-  const int64_t n = a.M * ((a.N + 3) / 4);
+  const int64_t n = a.M * ((a.N + 7) / 4);
   if (n == 0) return hipSuccess;
   const dim3 grid(blocks_for(n, 256));
   if (dtype == GT_BF16)
@@ -284,19 +411,27 @@ hipError_t launch_reduce(int dtype, const ProductArgs& a, hipStream_t s) {
 
 hipError_t launch_act_grad(int dtype, const ActGradArgs& a, hipStream_t s) {
   if (a.M == 0) return hipSuccess;
+  const int cols = a.vec == 2 ? 512 : 256;
   const dim3 grid(static_cast<unsigned>((a.M + kActRows - 1) / kActRows),
-                  static_cast<unsigned>((a.N + 255) / 256));
-  if (dtype == GT_BF16)
-    act_grad_kernel<uint16_t><<<grid, 256, 0, s>>>(a);
-  else
-    act_grad_kernel<float><<<grid, 256, 0, s>>>(a);
+                  static_cast<unsigned>((a.N + cols - 1) / cols));
+  if (dtype == GT_BF16) {
+    if (a.vec == 2)
+      act_grad_kernel<uint16_t, true><<<grid, 256, 0, s>>>(a);
+    else
+      act_grad_kernel<uint16_t, false><<<grid, 256, 0, s>>>(a);
+  } else {
+    if (a.vec == 2)
+      act_grad_kernel<float, true><<<grid, 256, 0, s>>>(a);
+    else
+      act_grad_kernel<float, false><<<grid, 256, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 
 hipError_t launch_join(const float* part, int64_t rows, int64_t wide, const int32_t* offsets,
                        int groups, int64_t most, int bm, int per, float* out, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>((wide + 63) / 64), static_cast<unsigned>(groups));
-  join_kernel<<<grid, 256, 0, s>>>(part, rows, wide, offsets, most, bm, per, out);
+  join_kernel<<<grid, 1024, 0, s>>>(part, rows, wide, offsets, most, bm, per, out);
   return hipGetLastError();
 }
 
@@ -315,27 +450,35 @@ hipError_t launch_gather(int dtype, const void* a, int64_t lda, void* da, const 
                                              ldd, cols, order, offsets, E, entries, k, T)
   if (dtype == GT_BF16) {
     if (wide)
-      GT_GATHER(uint16_t, 8);
+      GT_GATHER(uint16_t, true);
     else
-      GT_GATHER(uint16_t, 1);
+      GT_GATHER(uint16_t, false);
   } else {
     if (wide)
-      GT_GATHER(float, 4);
+      GT_GATHER(float, true);
     else
-      GT_GATHER(float, 1);
+      GT_GATHER(float, false);
   }
 #undef GT_GATHER
   return hipGetLastError();
 }
 
 hipError_t launch_combine(int dtype, const CombineArgs& a, hipStream_t s) {
-  const int64_t n = a.T * ((a.D + 3) / 4);
+  const int cols = a.vec == 2 ? 8 : 4;
+  const int64_t n = a.T * ((a.D + cols - 1) / cols);
   if (n == 0) return hipSuccess;
   const dim3 grid(blocks_for(n, 256));
-  if (dtype == GT_BF16)
-    combine_kernel<uint16_t><<<grid, 256, 0, s>>>(a);
-  else
-    combine_kernel<float><<<grid, 256, 0, s>>>(a);
+  if (dtype == GT_BF16) {
+    if (a.vec == 2)
+      combine_kernel<uint16_t, true><<<grid, 256, 0, s>>>(a);
+    else
+      combine_kernel<uint16_t, false><<<grid, 256, 0, s>>>(a);
+  } else {
+    if (a.vec == 2)
+      combine_kernel<float, true><<<grid, 256, 0, s>>>(a);
+    else
+      combine_kernel<float, false><<<grid, 256, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 

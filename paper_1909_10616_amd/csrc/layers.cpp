@@ -53,39 +53,78 @@ struct Scratch {
 struct Product {
   ProductArgs a{};
   int dtype = GT_F32, layout = kXW;
+  // the operands are this library's own arrays: 16-byte aligned rows of whole chunks,
+  // and, where k runs along them, zero beyond the last
+  bool own_a = false, own_b = false;
   int tile = 1;
   bool reg = false;
-  int64_t part = 0;      // bytes of partial sums
+  PadJobs pad{};          // operands copied to aligned rows first …
+  int64_t pad_a = 0, pad_b = 0, part = 0;   // … and the bytes of that and of partial sums
+
+  int64_t scratch() const { return up(pad_a, 256) + up(pad_b, 256) + up(part, 256); }
 };
 
-// Whether the 16-byte loads serve both operands: rows of whole aligned chunks,
-// and what one descriptor must reach of them within its range.
-bool chunks_serve(const Product& p) {
-  const ProductArgs& a = p.a;
-  const int64_t sz = size_of(p.dtype), vec = 16 / sz;
-  const int64_t reach = int64_t{1} << 31;
-  const int64_t wide = a.e.epi == kEpiGated ? 2 * a.N : a.N;
-  if (!aligned(a.A, 16) || !aligned(a.B, 16) || a.lda % vec || a.ldb % vec || a.sB % vec) return false;
-  const bool ax = p.layout == kXtP, bx = p.layout != kPWt;
-  if ((ax ? a.M : a.K) % vec || (bx ? wide : a.K) % vec || (wide != a.N && a.N % vec)) return false;
-  if ((ax ? 64 : a.gather ? a.a_rows : 256) * a.lda * sz >= reach) return false;
-  return (bx ? 64 : 256) * a.ldb * sz < reach;
+// One operand as it is stored: whether 16-byte loads serve it (aligned rows of whole
+// chunks, what one descriptor must reach within its range), and as the copy that they
+// do serve.
+struct Stored {
+  bool ok;
+  PadJob job;
+  int64_t bytes;
+};
+Stored stored(const void* ptr, int64_t ld, int64_t sgroup, int64_t groups, int64_t rows, int64_t cols,
+              int64_t half, int64_t reach_rows, bool own, int64_t sz) {
+  const int64_t vec = 16 / sz, reach = int64_t{1} << 31;
+  Stored s{};
+  s.ok = aligned(ptr, 16) && ld % vec == 0 && (groups == 1 || sgroup % vec == 0) &&
+         (own || (cols % vec == 0 && half % vec == 0)) && reach_rows * ld * sz < reach;
+  PadJob& j = s.job;
+  j.src = ptr;
+  j.groups = groups;
+  j.rows = rows;
+  j.cols = cols;
+  j.ld = ld;
+  j.sgroup = sgroup;
+  j.half = half ? up(half, vec) : 0;
+  j.ldd = half ? 2 * j.half : up(cols, vec);
+  s.bytes = groups * rows * j.ldd * sz;
+  if (reach_rows * j.ldd * sz >= reach) s.bytes = -1;   // no copy of it would do
+  return s;
 }
 
-// Tile and K slices by the time they should take. A stage of a tile (128 bytes
-// of k) costs a compute unit the larger of its MFMAs and of its operands' way
-// into LDS; workgroups beyond one per compute unit queue up; a K slice adds its
-// partial sums' way through memory and the launch that joins them.
+// What a stage (128 bytes of k) of a tile takes a compute unit, in µs: alone, and
+// when others share the unit.
+struct StageCost {
+  double alone, shared;
+};
+constexpr StageCost kStage[2][kTiles] = {
+    {{0, 0}, {1.9, 1.75}, {0.75, 0.5}, {0.5, 0.3}},       // fp32
+    {{1.6, 1.6}, {0.62, 0.53}, {0.4, 0.25}, {0.4, 0.15}}  // bf16
+};
+
+// Tile, K slices and copies by the time they should take: stages of the tiles that a
+// compute unit gets (256 of them), a K slice's partial sums through memory and the
+// launch that joins them, the copies of operands that 16-byte loads do not serve
+// and their launch; the register path takes those as they are, at twice the time of a
+// stage.
 void choose(Product* p, bool may_split) {
   ProductArgs& a = p->a;
-  const int64_t bk = 128 / size_of(p->dtype);
-  const int64_t wide = a.e.epi == kEpiGated ? 2 * a.N : a.N;
-  p->reg = !chunks_serve(*p);
-  const int64_t stages = std::max<int64_t>(1, (a.along_k ? a.K / std::max(1, a.groups) : a.K) / bk);
+  const int64_t sz = size_of(p->dtype), bk = 128 / sz;
+  const bool gated = a.e.epi == kEpiGated;
+  const int64_t wide = gated ? 2 * a.N : a.N;
+  const bool ax = p->layout == kXtP, bx = p->layout != kPWt;
+  const int64_t bgroups = a.groups > 0 && !a.along_k ? a.groups : 1;
+  const Stored sa = stored(a.A, a.lda, 0, 1, ax ? a.K : a.gather ? a.a_rows : a.M, ax ? a.M : a.K, 0,
+                           ax ? 64 : a.gather ? a.a_rows : 256, p->own_a, sz);
+  const Stored sb = stored(a.B, a.ldb, a.sB, bgroups, bx ? a.K : a.N, bx ? wide : a.K,
+                           bx && gated ? a.N : 0, bx ? 64 : 256, p->own_b, sz);
+  const bool copies = (!sa.ok && sa.bytes > 0) || (!sb.ok && sb.bytes > 0);
+  const bool can_dma = (sa.ok || sa.bytes >= 0) && (sb.ok || sb.bytes >= 0);
+  const int64_t stages = std::max<int64_t>(1, ((a.along_k ? a.K / std::max(1, a.groups) : a.K) + bk - 1) / bk);
   double best = 0.0;
   for (int t = 0; t < kTiles; ++t) {
     const TileShape& s = kTile[t];
-    if (t == 0 && (p->dtype != GT_BF16 || p->reg)) continue;
+    if (t == 0 && p->dtype != GT_BF16) continue;
     if (t == 3 && p->layout == kXtP) continue;
     const int64_t tn = (wide + s.BN - 1) / s.BN;
     int64_t tm = (a.M + s.BM - 1) / s.BM;
@@ -93,46 +132,79 @@ void choose(Product* p, bool may_split) {
     if (a.groups > 0 && !a.along_k) {
       const int64_t g = std::min<int64_t>(a.groups, a.M);
       most = a.M / s.BM + g;
-      const int64_t each = (a.M + g - 1) / std::max<int64_t>(1, g);
-      tm = g * ((each + s.BM - 1) / s.BM);
+      // rows spread over the groups: half a tile lost in each, one tile at least
+      tm = std::max<int64_t>(g, a.M / s.BM + g / 2);
     }
     const int64_t tiles = tm * tn * (a.along_k ? a.groups : 1);
     if (most * tn >= kMaxExtent) continue;
-    // cycles of a stage: 4096 (bf16) or 256 (fp32) operations a cycle at 60 %,
-    // 24 operand bytes a cycle
-    const double ops = 2.0 * s.BM * s.BN * bk;
-    const double stage = std::max(ops / (p->dtype == GT_BF16 ? 4096 * 0.6 : 256 * 0.8),
-                                  (s.BM + s.BN) * 128.0 / 24);
-    for (int64_t z = 1; z <= 64; z *= 2) {
-      if (z > 1 && (!may_split || stages / z < 4)) break;
-      const int64_t queue = (tiles * z + 255) / 256;
-      double cost = queue * (((stages + z - 1) / z + 2) * stage) + 2000;
-      if (z > 1) cost += 6000 + 2.0 * z * a.M * wide * 4 / 1700;   // bytes at 4 TB/s, in cycles
-      if (best == 0.0 || cost < best) {
-        best = cost;
-        p->tile = t;
-        a.splits = static_cast<int>(z);
-        a.tilesM = static_cast<int>(most);
-        a.tilesN = static_cast<int>(tn);
+    const StageCost& c = kStage[p->dtype == GT_BF16 ? 1 : 0][t];
+    for (int reg = 0; reg < 2; ++reg) {
+      if (reg ? (t < 2 || (sa.ok && sb.ok)) : !can_dma) continue;
+      const double copy = !reg && copies ? 5.0 + 2.0 * ((sa.ok ? 0 : sa.bytes) + (sb.ok ? 0 : sb.bytes)) / 4.5e6 : 0.0;
+      for (int64_t z = 1; z <= 64; z *= 2) {
+        if (z > 1 && (!may_split || stages / z < 4)) break;
+        const double each = static_cast<double>((stages + z - 1) / z) * (reg ? 2.0 : 1.0);
+        const double queue = std::max(c.alone, c.shared * ((tiles * z + 255) / 256));
+        double cost = copy + each * queue + 4.0;
+        if (z > 1) cost += 4.0 + 2.0 * z * a.M * wide * 4 / 4.0e6;
+        if (best == 0.0 || cost < best) {
+          best = cost;
+          p->tile = t;
+          p->reg = reg != 0;
+          a.splits = static_cast<int>(z);
+          a.tilesM = static_cast<int>(most);
+          a.tilesN = static_cast<int>(tn);
+        }
       }
     }
   }
-  a.e.ldpart = up(a.N, 4) * (wide == a.N ? 1 : 2);
-  const int64_t all = (a.K + bk - 1) / bk;
+  a.half = a.N;
+  if (!p->reg) {
+    if (!sa.ok) {
+      p->pad.job[p->pad.n++] = sa.job;
+      p->pad_a = sa.bytes;
+      a.lda = sa.job.ldd;
+    }
+    if (!sb.ok) {
+      p->pad.job[p->pad.n++] = sb.job;
+      p->pad_b = sb.bytes;
+      a.ldb = sb.job.ldd;
+      a.sB = sb.job.rows * sb.job.ldd;
+      if (sb.job.half) a.half = sb.job.half;
+    }
+  }
+  a.e.ldpart = up(a.N, 4) * (gated ? 2 : 1);
+  const TileShape& s = kTile[p->tile];
+  const int64_t kb = (p->reg ? 128 : s.KB) / sz, all = (a.K + kb - 1) / kb;
   a.per_slice = static_cast<int>((all + a.splits - 1) / std::max(1, a.splits));
   p->part = a.splits > 1 ? a.splits * a.M * a.e.ldpart * 4 : 0;
 }
 
-int run(Product& p, float* part, hipStream_t s) {
+// Launches a product; ws: its scratch() bytes.
+int run(const Product& p, void* ws, hipStream_t s) {
   ProductArgs a = p.a;
   if (a.M == 0) return GT_OK;
   if (a.splits < 1) return fail("layer product: too many tiles");
+  char* at = static_cast<char*>(ws);
+  if (p.pad.n > 0) {
+    PadJobs jobs = p.pad;
+    int n = 0;
+    if (p.pad_a) a.A = jobs.job[n++].dst = at;
+    at += up(p.pad_a, 256);
+    if (p.pad_b) a.B = jobs.job[n++].dst = at;
+    at += up(p.pad_b, 256);
+    GT_TRY(launch_pad(p.dtype, jobs, s), "copy to aligned rows");
+  }
   if (a.splits > 1) {
+    a.e.part = reinterpret_cast<float*>(at);
+    const int epi = a.e.epi;
     a.e.epi = kEpiPart;
-    a.e.part = part;
+    GT_TRY(launch_product(p.dtype, p.layout, p.tile, p.reg, a, s), "layer product");
+    a.e.epi = epi;
+    GT_TRY(launch_reduce(p.dtype, a, s), "joining the K slices");
+    return GT_OK;
   }
   GT_TRY(launch_product(p.dtype, p.layout, p.tile, p.reg, a, s), "layer product");
-  if (a.splits > 1) GT_TRY(launch_reduce(p.dtype, a, s), "joining the K slices");
   return GT_OK;
 }
 
@@ -253,8 +325,8 @@ struct LinearGrad {
   int64_t lddp = 0, wide = 0;
   Product dx, dw;
   // scratch
-  void* dP = nullptr;
-  float *part = nullptr, *sums = nullptr;
+  void *dP = nullptr, *rest = nullptr;   // rest: the products' own, one after the other
+  float* sums = nullptr;
   int64_t bytes = 0;
 };
 
@@ -277,7 +349,7 @@ LinearGrad linear_grad(const gt_linear_grad_args& q, void* ws) {
   if (g.own_dP && products) g.dP = s.take(q.M * g.lddp * sz);
   const void* dP = g.own_dP ? g.dP : q.dY;
   if (q.db) g.sums = s.take<float>((q.M + kActRows - 1) / kActRows * g.wide * 4);
-  int64_t part = 0;
+  int64_t rest = 0;
   if (q.dX) {   // dP (M×wide) · Wᵀ
     g.dx.dtype = q.dtype;
     g.dx.layout = kPWt;
@@ -290,8 +362,9 @@ LinearGrad linear_grad(const gt_linear_grad_args& q, void* ws) {
     a.N = q.K;
     a.K = g.wide;
     output(&a.e, q.dX, q.lddx, q.dtype == GT_F32, q.K, sz);
+    g.dx.own_a = g.own_dP;
     choose(&g.dx, true);
-    part = std::max(part, g.dx.part);
+    rest = std::max(rest, g.dx.scratch());
   }
   if (q.dW) {   // Xᵀ · dP
     g.dw.dtype = q.dtype;
@@ -305,10 +378,11 @@ LinearGrad linear_grad(const gt_linear_grad_args& q, void* ws) {
     a.N = g.wide;
     a.K = q.M;
     output(&a.e, q.dW, q.lddw, q.dw_dtype == GT_F32, g.wide, sz);
+    g.dw.own_b = g.own_dP;
     choose(&g.dw, true);
-    part = std::max(part, g.dw.part);
+    rest = std::max(rest, g.dw.scratch());
   }
-  if (part) g.part = s.take<float>(part);
+  if (rest) g.rest = s.take(rest);
   g.bytes = s.used;
   return g;
 }
@@ -343,8 +417,8 @@ int experts_args_checks(const gt_experts_args* a, bool pointers) {
 
 struct Experts {
   Product up, down;
-  void* H = nullptr;
-  float *O = nullptr, *part = nullptr;
+  void *H = nullptr, *rest = nullptr;
+  float* O = nullptr;
   int64_t bytes = 0, ldo = 0;
 };
 
@@ -386,6 +460,7 @@ Experts experts(const gt_experts_args& q, void* ws) {
     e.bias = q.b1;
     e.sbias = wide;
     e.vec = width(q.H, {{q.P, q.ldp}, {q.b1, 0}, {x.H, ldh}}, sz);
+    e.zero_pad = 1;
     choose(&x.up, true);
   }
   {
@@ -410,10 +485,11 @@ Experts experts(const gt_experts_args& q, void* ws) {
     e.bias = q.b2;
     e.sbias = q.D;
     e.vec = std::min(width(q.D, {{q.b2, 0}}, sz), width(q.D, {{x.O, x.ldo}}, 4));
+    x.down.own_a = true;
     choose(&x.down, true);
   }
-  const int64_t part = std::max(x.up.part, x.down.part);
-  if (part) x.part = s.take<float>(part);
+  const int64_t rest = std::max(x.up.scratch(), x.down.scratch());
+  if (rest) x.rest = s.take(rest);
   x.bytes = s.used;
   return x;
 }
@@ -441,7 +517,7 @@ int experts_grad_checks(const gt_experts_grad_args* a, bool pointers) {
 struct ExpertsGrad {
   int64_t R, wide, ldd, ldp, ldh, ldo;
   Product dh, dw2, dx, dw1;
-  void *Xs = nullptr, *dYs = nullptr, *dP = nullptr, *Hw = nullptr;
+  void *Xs = nullptr, *dYs = nullptr, *dP = nullptr, *Hw = nullptr, *rest = nullptr;
   float *dXs = nullptr, *dot = nullptr, *colsum = nullptr, *sums = nullptr;
   int64_t bytes = 0;
 };
@@ -495,6 +571,8 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     e.order = q.order;
     e.entries = g.R;
     e.wide = g.wide;
+    e.zero_pad = 1;
+    g.dh.own_a = true;
     e.vec = width(q.H, {{q.P, q.ldp}, {g.dP, g.ldp}, {g.Hw, g.ldh}}, sz);
     choose(&g.dh, false);
     const TileShape& t = kTile[g.dh.tile];
@@ -513,6 +591,7 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     a.K = g.R;
     output(&a.e, q.dW2, q.D, q.dtype == GT_F32, q.D, sz);
     a.e.sY = q.H * q.D;
+    g.dw2.own_a = g.dw2.own_b = true;
     choose(&g.dw2, false);
   }
   if (q.dX) {
@@ -527,6 +606,7 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     a.K = g.wide;
     g.dXs = s.take<float>(g.R * g.ldo * 4);
     output(&a.e, g.dXs, g.ldo, true, q.D, sz);
+    g.dx.own_a = true;
     choose(&g.dx, false);
   }
   if (q.dW1) {
@@ -540,8 +620,11 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     a.K = g.R;
     output(&a.e, q.dW1, g.wide, q.dtype == GT_F32, g.wide, sz);
     a.e.sY = q.D * g.wide;
+    g.dw1.own_a = g.dw1.own_b = true;
     choose(&g.dw1, false);
   }
+  const int64_t rest = std::max({g.dh.scratch(), g.dw2.scratch(), g.dx.scratch(), g.dw1.scratch()});
+  if (rest) g.rest = s.take(rest);
   if (q.db2) g.sums = s.take<float>((g.R / kSumRows + std::min<int64_t>(q.E, g.R)) * q.D * 4);
   g.bytes = s.used;
   return g;
@@ -572,15 +655,15 @@ extern "C" {
 int gt_linear_workspace(const gt_linear_args* a, int64_t* bytes) {
   if (!bytes) return fail("gt_linear_workspace: null argument");
   GT_CHECK(linear_checks(a, false));
-  *bytes = linear_product(*a).part;
+  *bytes = linear_product(*a).scratch();
   return GT_OK;
 }
 
 int gt_linear(const gt_linear_args* a, void* ws, int64_t ws_bytes, void* stream) {
   GT_CHECK(linear_checks(a, true));
   Product p = linear_product(*a);
-  GT_CHECK(scratch_ok(ws, ws_bytes, p.part));
-  return run(p, static_cast<float*>(ws), static_cast<hipStream_t>(stream));
+  GT_CHECK(scratch_ok(ws, ws_bytes, p.scratch()));
+  return run(p, ws, static_cast<hipStream_t>(stream));
 }
 
 int gt_linear_backward_workspace(const gt_linear_grad_args* a, int64_t* bytes) {
@@ -608,14 +691,15 @@ int gt_linear_backward(const gt_linear_grad_args* a, void* ws, int64_t ws_bytes,
     q.dP = g.dP;
     q.lddp = g.lddp;
     q.part = g.sums;
+    q.pad = static_cast<int>(g.lddp - g.wide);
     q.vec = width(a->N, {{a->dY, a->lddy}, {q.P, a->ldp}, {g.dP, g.lddp}}, size_of(a->dtype));
     GT_TRY(launch_act_grad(a->dtype, q, s), "gradient of the activation");
     if (a->db)
       GT_TRY(launch_join(g.sums, (a->M + kActRows - 1) / kActRows, g.wide, nullptr, 1, 0, 1, 1, a->db, s),
              "gradient of the bias");
   }
-  if (a->dX) GT_CHECK(run(g.dx, g.part, s));
-  if (a->dW) GT_CHECK(run(g.dw, g.part, s));
+  if (a->dX) GT_CHECK(run(g.dx, g.rest, s));
+  if (a->dW) GT_CHECK(run(g.dw, g.rest, s));
   return GT_OK;
 }
 
@@ -675,8 +759,8 @@ int gt_experts(const gt_experts_args* a, void* ws, int64_t ws_bytes, void* strea
   const hipStream_t s = static_cast<hipStream_t>(stream);
   Experts x = experts(*a, ws);
   GT_CHECK(scratch_ok(ws, ws_bytes, x.bytes));
-  GT_CHECK(run(x.up, x.part, s));
-  GT_CHECK(run(x.down, x.part, s));
+  GT_CHECK(run(x.up, x.rest, s));
+  GT_CHECK(run(x.down, x.rest, s));
   CombineArgs c{};
   c.T = a->T;
   c.D = a->D;
@@ -710,7 +794,7 @@ int gt_experts_backward(const gt_experts_grad_args* a, void* ws, int64_t ws_byte
   GT_TRY(launch_gather(a->dtype, a->dW1 ? a->X : nullptr, a->ldx, g.Xs, a->dY, a->lddy, g.dYs, g.ldd,
                        a->D, a->order, a->offsets, a->E, g.R, a->k, a->T, s),
          "sorting the rows");
-  if (g.dP) GT_CHECK(run(g.dh, nullptr, s));
+  if (g.dP) GT_CHECK(run(g.dh, g.rest, s));
   if (a->db1)
     GT_TRY(launch_join(g.colsum, 0, g.wide, a->offsets, a->E, g.R, kTile[g.dh.tile].BM,
                        kTile[g.dh.tile].NWM, a->db1, s),
@@ -737,9 +821,9 @@ int gt_experts_backward(const gt_experts_grad_args* a, void* ws, int64_t ws_byte
     w.dweights = a->dweights;
     GT_TRY(launch_weight_grad(a->dtype, w, s), "gradient of the weights");
   }
-  if (a->dW2) GT_CHECK(run(g.dw2, nullptr, s));
+  if (a->dW2) GT_CHECK(run(g.dw2, g.rest, s));
   if (a->dX) {
-    GT_CHECK(run(g.dx, nullptr, s));
+    GT_CHECK(run(g.dx, g.rest, s));
     CombineArgs c{};
     c.T = a->T;
     c.D = a->D;
@@ -753,7 +837,7 @@ int gt_experts_backward(const gt_experts_grad_args* a, void* ws, int64_t ws_byte
     c.vec = width(a->D, {{a->dX, a->lddx}}, size_of(a->dtype));
     GT_TRY(launch_combine(a->dtype, c, s), "summing the experts' gradients");
   }
-  if (a->dW1) GT_CHECK(run(g.dw1, nullptr, s));
+  if (a->dW1) GT_CHECK(run(g.dw1, g.rest, s));
   return GT_OK;
 }
 

@@ -150,10 +150,19 @@ __device__ __forceinline__ void linear_quad(const Epilogue& e, int64_t N, int64_
   if (gated) v *= u;
   v += r;
   const int64_t at = group * e.sY + row * e.ldy + n;
+  const bool pad = e.zero_pad != 0;   // rows of whole aligned quads
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = i < left ? v[i] : 0.0f;
   if (e.out_f32)
-    store4(static_cast<float*>(e.Y) + at, v, left, vec);
+    store4(static_cast<float*>(e.Y) + at, v, pad ? 4 : left, vec || pad);
   else
-    store4(static_cast<T*>(e.Y) + at, v, left, vec);
+    store4(static_cast<T*>(e.Y) + at, v, pad ? 4 : left, vec || pad);
+}
+// Columns that an epilogue writes: N, or up to the next 16 bytes.
+template <typename T>
+__device__ __forceinline__ int64_t written(const Epilogue& e, int64_t N) {
+  constexpr int64_t VEC = 16 / sizeof(T);
+  return e.zero_pad ? (N + VEC - 1) / VEC * VEC : N;
 }
 template <typename T>
 __device__ __forceinline__ f32x4 bias_quad(const Epilogue& e, int64_t n, int group, int left) {
@@ -195,6 +204,11 @@ struct EpiRows {
   // the column of chunk c (gated: of the gate's)
   __device__ __forceinline__ int64_t col(int c) const {
     return p.col + (G || c < CH / 2 ? 0 : BN / 2 - WN / 2) + c * 4;
+  }
+
+  // Whether the slope epilogue takes octets: columns that all exist.
+  __device__ static __forceinline__ bool whole_slope(const ProductArgs& a, const EpiPlace& p) {
+    return a.e.vec == 2 && p.col + BN / 2 + WN / 2 <= a.N;
   }
 
   // A whole tile of aligned rows of whole octets: 16-byte accesses, nothing checked.
@@ -275,7 +289,7 @@ struct EpiRows {
     const int c = lane % LR;
     const int64_t n = col(c);
     const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
-    if (left <= 0) return;
+    if (n >= written<T>(a.e, a.N)) return;
     const f32x4 bv = bias_quad<T>(a.e, n, p.group, left);
     const f32x4 bu = G ? bias_quad<T>(a.e, n + a.N, p.group, left) : f32x4{};
 #pragma unroll 1
@@ -311,75 +325,112 @@ struct EpiRows {
   }
 
   // dH arrived: H = act(P) (times up), w the row's weight;
-  // dP = w·dH·act'(P) (gated: ·up, and w·dH·act(gate) for up), Hw = w·H
-  __device__ __forceinline__ void slope(EpiSums& sums) const {
+  // dP = w·dH·act'(P) (gated: ·up, and w·dH·act(gate) for up), Hw = w·H.
+  // Every lane holds the weight of one row of 64; Q quads of columns a lane, U rows at a
+  // time with their pre-activations loaded first.
+  template <bool WHOLE>
+  __device__ __forceinline__ void slope(EpiSums* sums) const {
     const Epilogue& e = a.e;
-    constexpr int STEP = 64 / CH;
-    constexpr int U = RP / STEP >= 4 ? 4 : RP / STEP;
-    const int c = lane % CH;
+    constexpr int Q = WHOLE ? 2 : 1, LR = CH / Q, STEP = 64 / LR;
+    constexpr int U = RP / STEP >= 2 ? 2 : 1;
+    static_assert(RP <= 64, "a row's weight in each lane");
+    const int c = lane % LR * Q;
     const int64_t n = col(c);
     const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
     const bool vec = e.vec != 0;
+    float mine_w = 0.0f;
+    if (lane < RP && p.row + h + lane < p.row_end) {
+      const int64_t entry = e.order[p.row + h + lane];
+      if (entry >= 0 && entry < e.entries) mine_w = e.weights[entry];
+    }
 #pragma unroll 1
-    for (int r0 = lane / CH; r0 < RP; r0 += U * STEP) {
-      f32x4 gate[U], up[U];
-      float w[U];
+    for (int r0 = lane / LR; r0 < RP; r0 += U * STEP) {
+      f32x4 gate[U][Q], up[U][Q];
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int64_t row = p.row + h + r0 + i * STEP;
-        gate[i] = f32x4{};
-        up[i] = f32x4{1.0f, 1.0f, 1.0f, 1.0f};
-        w[i] = 0.0f;
-        if (row < p.row_end && left > 0) {
-          const int64_t entry = e.order[row];
-          if (entry >= 0 && entry < e.entries) w[i] = e.weights[entry];
-          const T* pp = static_cast<const T*>(e.P) + row * e.ldp + n;
-          gate[i] = load4(pp, left, vec);
-          if (e.gated) up[i] = load4(pp + a.N, left, vec);
+        const T* pp = static_cast<const T*>(e.P) + row * e.ldp + n;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+          gate[i][q] = f32x4{};
+          up[i][q] = f32x4{1.0f, 1.0f, 1.0f, 1.0f};
+        }
+        if (row >= p.row_end || (!WHOLE && left <= 0)) continue;
+        if constexpr (WHOLE) {
+          const oct g = load8(pp);
+          gate[i][0] = g.a;
+          gate[i][Q - 1] = g.b;
+          if (e.gated) {
+            const oct u = load8(pp + a.N);
+            up[i][0] = u.a;
+            up[i][Q - 1] = u.b;
+          }
+        } else {
+          gate[i][0] = load4(pp, left, vec);
+          if (e.gated) up[i][0] = load4(pp + a.N, left, vec);
         }
       }
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int r = r0 + i * STEP;
         const int64_t row = p.row + h + r;
+        const float w = __shfl(mine_w, r);
+        const bool live = row < p.row_end && (WHOLE || left > 0);
         float dot = 0.0f;
-        if (row < p.row_end && left > 0) {
-          const f32x4 v = chunk(r, c);
-          f32x4 val, slope;
+        f32x4 dg[Q], du[Q], hw[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+          const f32x4 v = chunk(r, c + q);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            float x, y;
-            act_both(e.act, gate[i][j], &x, &y);
-            val[j] = x;
-            slope[j] = y;
+            float val, sl;
+            act_both(e.act, gate[i][q][j], &val, &sl);
+            const float wv = w * v[j], H = val * up[i][q][j];
+            const bool in = live && (WHOLE || j < left);
+            dot += in ? v[j] * H : 0.0f;
+            dg[q][j] = in ? wv * up[i][q][j] * sl : 0.0f;
+            du[q][j] = in ? wv * val : 0.0f;
+            hw[q][j] = in ? w * H : 0.0f;
           }
-          const f32x4 wv = v * w[i], H = val * up[i];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) dot += j < left ? v[j] * H[j] : 0.0f;
-          const f32x4 dg = wv * up[i] * slope;
+          sums[q].g += dg[q];
+          sums[q].u += du[q];
+        }
+        if (live || (row < p.row_end && n < written<T>(e, a.N))) {
           T* out = static_cast<T*>(e.Y) + row * e.ldy + n;
-          store4(out, dg, left, vec);
-          sums.g += dg;
-          if (e.gated) {
-            const f32x4 du = wv * val;
-            store4(out + a.N, du, left, vec);
-            sums.u += du;
+          T* hout = static_cast<T*>(e.Hw) + row * e.ldh + n;
+          if constexpr (WHOLE) {
+            store8(out, oct{dg[0], dg[Q - 1]});
+            if (e.gated) store8(out + a.N, oct{du[0], du[Q - 1]});
+            store8(hout, oct{hw[0], hw[Q - 1]});
+          } else {
+            // (rows padded with zeros: dP's end with the up half when gated)
+            store4(out, dg[0], e.gated ? left : e.zero_pad ? 4 : left, vec);
+            if (e.gated) {
+              store4(out + a.N, du[0], left, vec);
+              constexpr int64_t VEC = 16 / sizeof(T);
+              const int64_t pad = (2 * a.N + VEC - 1) / VEC * VEC - 2 * a.N;
+              if (e.zero_pad && left > 0 && n + left == a.N)
+                for (int64_t z = 0; z < pad; ++z) (out + a.N)[left + z] = T(0);
+            }
+            store4(hout, hw[0], left, vec);
           }
-          store4(static_cast<T*>(e.Hw) + row * e.ldh + n, H * w[i], left, vec);
         }
 #pragma unroll
-        for (int d = 1; d < CH; d <<= 1) dot += __shfl_xor(dot, d);
+        for (int d = 1; d < LR; d <<= 1) dot += __shfl_xor(dot, d);
         if (c == 0 && row < p.row_end) e.dot[row * e.ldot + p.pcol] = dot;
       }
     }
   }
 
-  __device__ __forceinline__ void run(EpiSums& sums) const {
+  __device__ __forceinline__ void run(EpiSums* sums) const {
     const Epilogue& e = a.e;
     if constexpr (EPI == kEpiPart) {
       part();
     } else if constexpr (EPI == kEpiSlope) {
-      slope(sums);
+      if (whole_slope(a, p))
+        slope<true>(sums);
+      else
+        slope<false>(sums);
     } else {
       const bool all = e.vec == 2 && p.row + WM <= p.row_end &&
                        p.col + (G ? WN / 2 : BN / 2 + WN / 2) <= a.N;
@@ -397,28 +448,31 @@ struct EpiRows {
   }
 };
 
-// The column sums of a wavefront's rows, joined over its lanes.
-template <int WN, int BN>
+// The column sums of a wavefront's rows, joined over its lanes (octets: of Q quads
+// a lane, as the rows were).
+template <int WN, int BN, int Q>
 __device__ __forceinline__ void epilogue_sums(const ProductArgs& a, const EpiPlace& p, int lane,
-                                              EpiSums& s) {
-  constexpr int CH = WN / 4;
-#pragma unroll
-  for (int d = CH; d < 64; d <<= 1)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      s.g[i] += __shfl_xor(s.g[i], d);
-      s.u[i] += __shfl_xor(s.u[i], d);
-    }
-  const int c = lane % CH;
+                                              EpiSums* s) {
+  constexpr int CH = WN / 4, LR = CH / Q;
+  const int c = lane % LR * Q;
   const int64_t n = p.col + (c < CH / 2 ? 0 : BN / 2 - WN / 2) + c * 4;
-  if (lane >= CH) return;
   float* out = a.e.colsum + p.prow * a.e.wide + n;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (n + i < a.N) {
-      out[i] = s.g[i];
-      if (a.e.gated) out[a.N + i] = s.u[i];
-    }
+  for (int q = 0; q < Q; ++q) {
+#pragma unroll
+    for (int d = LR; d < 64; d <<= 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[q].g[i] += __shfl_xor(s[q].g[i], d);
+        s[q].u[i] += __shfl_xor(s[q].u[i], d);
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (lane < LR && n + 4 * q + i < a.N) {
+        out[4 * q + i] = s[q].g[i];
+        if (a.e.gated) out[a.N + 4 * q + i] = s[q].u[i];
+      }
+  }
 }
 
 // ---- the kernel ------------------------------------------------------------
@@ -491,10 +545,10 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   }
   // whether the tile's second half holds up values, B's columns N on
   const bool halves = EPI == kEpiGated || (EPI == kEpiPart && BX && !AX && a.e.gated != 0);
-  const int64_t wide = halves ? 2 * a.N : a.N;   // B's columns
+  const int64_t wide = halves ? a.half + a.N : a.N;   // B's columns
   const int64_t n0 = static_cast<int64_t>(tn) * (halves ? BN / 2 : BN);
   // stored column of tile column c is n0 + c, plus this for the second half
-  const int64_t hoff = halves ? a.N - BN / 2 : 0;
+  const int64_t hoff = halves ? a.half - BN / 2 : 0;
 
   const T* Ag = static_cast<const T*>(a.A);
   const T* Bg = static_cast<const T*>(a.B) + (a.along_k ? 0 : group * a.sB);
@@ -596,8 +650,10 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   if constexpr (!REG) {
     ga = uniform_ptr(AX ? Ag + k0 * a.lda + m0 : Ag + (a.gather ? 0 : m0 * a.lda) + k0);
     gb = uniform_ptr(BX ? Bg + k0 * a.ldb + n0 : Bg + n0 * a.ldb + k0);
-    remA = uni64((AX ? (left - 1) * a.lda + mend - m0 : (arem - 1) * a.lda + left) * SZ);
-    remB = uni64((BX ? (left - 1) * a.ldb + wide - n0 : (wide - n0 - 1) * a.ldb + left) * SZ);
+    // (rows end on whole chunks: what pads an operand's last one is its own)
+    auto whole = [](int64_t v) { return (v + VEC - 1) / VEC * VEC; };
+    remA = uni64((AX ? (left - 1) * a.lda + whole(mend) - m0 : (arem - 1) * a.lda + whole(left)) * SZ);
+    remB = uni64((BX ? (left - 1) * a.ldb + whole(wide) - n0 : (wide - n0 - 1) * a.ldb + whole(left)) * SZ);
   }
   auto next_stage = [&]() __attribute__((always_inline)) {
     ga += stepA;
@@ -821,13 +877,14 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   constexpr int CH = WN / 4;                       // 16-byte fp32 chunks of a row
   constexpr int XM = (CH < 16 ? CH : 16) - 1;
   constexpr int RPX = REGION / (WN * 4) / I * I;
-  constexpr int RP = RPX < WM ? RPX : WM;
+  constexpr int RPM = RPX < WM ? RPX : WM;
+  constexpr int RP = RPM < 64 ? RPM : 64;
   static_assert(RP >= I && WM % RP == 0, "epilogue rows");
   __syncthreads();
   char* mine = smem + wave * REGION;
   const EpiPlace place{m0 + wm * WM, mend, n0 + wn * HN, group, z,
                        tm * NWM + wm, tn * NWN + wn};
-  EpiSums sums{};
+  EpiSums sums[2] = {};
 #pragma unroll
   for (int h = 0; h < WM / RP; ++h) {
 #pragma unroll
@@ -849,7 +906,12 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
     __builtin_amdgcn_wave_barrier();
   }
   if constexpr (EPI == kEpiSlope) {
-    if (a.e.colsum) epilogue_sums<WN, BN>(a, place, lane, sums);
+    if (a.e.colsum) {
+      if (EpiRows<DT, EPI, WM, WN, XM, RP, BN>::whole_slope(a, place))
+        epilogue_sums<WN, BN, 2>(a, place, lane, sums);
+      else
+        epilogue_sums<WN, BN, 1>(a, place, lane, sums);
+    }
   }
 }
 

@@ -23,7 +23,7 @@ struct Epilogue {
   int32_t out_f32;   // Y in fp32, else in the operands' type
   int32_t vec;       // every row and pointer takes accesses of: 1: 4 elements, 2: 8 (16 bytes
                      // at least), 0: one
-  int32_t pad;
+  int32_t zero_pad;  // columns of Y from N to the next 16 bytes are written as zero
   void* Y;           // [rows][ldy]; group g at Y + g·sY (groups along k)
   int64_t ldy, sY;
   void* P;           // kept pre-activations or the given ones (kEpiSlope), or null
@@ -50,7 +50,8 @@ struct ProductArgs {
   const void* A;
   const void* B;
   int64_t lda, ldb;     // elements between stored rows
-  int64_t M, N, K;      // N: columns of Y (B has 2·N when gated)
+  int64_t M, N, K;      // N: columns of Y
+  int64_t half;         // gated: columns of B before the up half's first
   const int32_t* offsets;  // group g: rows (or k) offsets[g] … offsets[g + 1] − 1
   int32_t groups;       // 0: no groups
   int32_t along_k;      // groups along k
@@ -75,7 +76,7 @@ struct TileShape {
 constexpr int kTiles = 4;
 constexpr TileShape kTile[kTiles] = {
     {256, 256, 2, 4, 128, 2, 32},  // 0: bf16, DMA only
-    {128, 128, 2, 2, 128, 2, 32},  // 1
+    {128, 128, 2, 2, 128, 2, 32},  // 1: DMA only
     {64, 64, 2, 2, 128, 3, 16},    // 2
     {16, 128, 1, 4, 128, 4, 16},   // 3: not for kXtP
 };

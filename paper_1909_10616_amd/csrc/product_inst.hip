@@ -66,7 +66,7 @@ hipError_t LP_NAME(LP_DT, LP_LAY)(int tile, bool reg, const ProductArgs& a, hipS
 #if LP_DT == 1
   if (tile == 0 && !reg) return by_epilogue<0, false>(a, s);
 #endif
-  if (tile == 1) return reg ? by_epilogue<1, true>(a, s) : by_epilogue<1, false>(a, s);
+  if (tile == 1 && !reg) return by_epilogue<1, false>(a, s);
   if (tile == 2) return reg ? by_epilogue<2, true>(a, s) : by_epilogue<2, false>(a, s);
 #if LP_LAY != 2
   if (tile == 3) return reg ? by_epilogue<3, true>(a, s) : by_epilogue<3, false>(a, s);

@@ -2,12 +2,16 @@
 // and the gradient of the weights.
 //
 // One wavefront a token. Lane l holds the logits of experts l, l + 64, …; the
-// choice is k times the largest key, as one 64-bit maximum over the wavefront
-// of (the key made unsigned in its order, the index inverted), so that equals
-// go to the lowest index. The lists are a counting sort in fixed blocks of
-// entries: every block's counts per expert, their running sums, and each
-// entry's rank among its block's entries of the same expert, so that an
-// expert's entries keep their order.
+// choice is k times the largest key over the wavefront (lane moves within rows of 16,
+// then four scalars), whose lowest index the lanes' votes give, register by
+// register. The lists are a counting sort over at most kMaxBlocks blocks of tokens:
+// the block that routes its tokens counts them per expert; then each block sums
+// what the blocks before it counted and ranks its entries, 64 at a time, by the
+// votes on their experts' bits, so that an expert's entries keep their order.
+// Two launches; one for a few tokens.
+//
+// Bound by the latency of the choice's chain of maxima: 16384 tokens, 8 of 256 experts
+// in 8 groups, with their lists.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -20,39 +24,41 @@ namespace gt {
 namespace {
 
 constexpr int kMaxE = 1024;
-constexpr int kMaxK = 64;
-constexpr int kEntries = 512;     // entries of a sort block
+constexpr int kMaxBlocks = 256;
+constexpr int kWaves = 16;       // of a routing block, a token each at a time
+constexpr int kEntries = 512;    // entries ranked at a time; the most of one block that does all
 
 struct RouteArgs {
   gt_route_args a;
-  int32_t* counts;   // [block][E], then made the blocks' first positions
-  int64_t blocks;
+  int32_t* counts;   // [block][E]
+  int32_t blocks;
+  int32_t tokens;    // of a block
 };
 
-// Unsigned integers in the order of the floats (NaN taken as −inf before; −0 and 0
-// are equal).
-__device__ __forceinline__ uint32_t ordered(float v) {
-  const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.0f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+// The value of the lane that a move within 16 lanes names.
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+  const int b = __builtin_bit_cast(int, v);
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, CTRL, 0xf, 0xf, false));
 }
-
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t o = __shfl_xor(static_cast<unsigned long long>(v), d);
-    v = o > v ? o : v;
-  }
-  return v;
+__device__ __forceinline__ float lane_of(float v, int lane) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
+// Reductions over the wavefront, all lanes active, the result in every lane.
+// (0xb1, 0x4e: neighbours and pairs swapped; 0x141, 0x140: 8 and 16 lanes mirrored.)
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+  v = fmaxf(v, moved<0xb1>(v));
+  v = fmaxf(v, moved<0x4e>(v));
+  v = fmaxf(v, moved<0x141>(v));
+  v = fmaxf(v, moved<0x140>(v));
+  return fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
 }
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-  return v;
+  v += moved<0xb1>(v);
+  v += moved<0x4e>(v);
+  v += moved<0x141>(v);
+  v += moved<0x140>(v);
+  return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
 
 // exp(x − m) where m is the largest of the values: 1 for the largest, +inf included.
@@ -122,30 +128,48 @@ __device__ __forceinline__ void load_logits(const void* logits, int64_t at, int 
   }
 }
 
+// The two largest of a run's keys.
+struct Best {
+  float a, b;
+  __device__ __forceinline__ void add(float v) {
+    b = fmaxf(b, fminf(a, v));
+    a = fmaxf(a, v);
+  }
+};
+
 // The keys of experts outside the kept groups become −inf. keys, runs: this
-// wavefront's LDS (E keys, `groups` scores).
+// wavefront's LDS (E keys, 128 + groups values). Up to 32 groups are scored by 64 / groups
+// lanes each.
 template <int EPL>
 __device__ __forceinline__ void keep_groups(int E, int groups, int keep, int lane, float* keys,
                                             float* runs, float (&key)[EPL]) {
+  const float ninf = -__builtin_inff();
   const int size = E / groups;
+  float* const score = runs + 128;
 #pragma unroll
   for (int i = 0; i < EPL; ++i)
     if (i * 64 + lane < E) keys[i * 64 + lane] = key[i];
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  for (int g = lane; g < groups; g += 64) {
-    float a = -__builtin_inff(), b = a;
-    for (int j = 0; j < size; ++j) {
-      const float v = keys[g * size + j];
-      if (v > a) {
-        b = a;
-        a = v;
-      } else if (v > b) {
-        b = v;
-      }
+  const int parts = groups > 32 ? 1 : 64 / groups;
+  for (int g0 = 0; g0 < groups; g0 += 64) {
+    const int g = g0 + (parts > 1 ? lane % groups : lane), part = parts > 1 ? lane / groups : 0;
+    Best best{ninf, ninf};
+    if (g < groups && part < parts)
+      for (int j = part; j < size; j += parts) best.add(keys[g * size + j]);
+    if (parts > 1) {
+      runs[2 * lane] = best.a;
+      runs[2 * lane + 1] = best.b;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (part == 0)
+        for (int j = 1; j < parts; ++j) {
+          best.add(runs[2 * (lane + j * groups)]);
+          best.add(runs[2 * (lane + j * groups) + 1]);
+        }
     }
-    float s = size > 1 ? a + b : a;
-    if (!(s == s)) s = -__builtin_inff();   // +inf and −inf in one run
-    runs[g] = s;
+    if (g < groups && part == 0) {
+      const float s = size > 1 ? best.a + best.b : best.a;
+      score[g] = s == s ? s : ninf;   // (+inf and −inf in one run)
+    }
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   // an expert's run stays if fewer than `keep` runs beat it
@@ -154,20 +178,25 @@ __device__ __forceinline__ void keep_groups(int E, int groups, int keep, int lan
     const int e = i * 64 + lane;
     if (e >= E) continue;
     const int g = e / size;
-    const float mine = runs[g];
+    const float mine = score[g];
     int better = 0;
     for (int o = 0; o < groups; ++o) {
-      const float v = runs[o];
+      const float v = score[o];
       better += v > mine || (v == mine && o < g) ? 1 : 0;
     }
-    if (better >= keep) key[i] = -__builtin_inff();
+    if (better >= keep) key[i] = ninf;
   }
 }
 
-// Scores and choice of one token.
+// LDS floats a wavefront needs to keep groups.
+__host__ __device__ constexpr int group_floats(int E, int groups) {
+  return groups > 1 ? E + 128 + groups : 0;
+}
+
+// Scores and choice of one token; lane s returns the expert of slot s (−1: none).
 template <typename T, int EPL>
-__device__ __forceinline__ int route_row(const gt_route_args& a, int64_t t, int lane, float* keys,
-                                         float* runs) {
+__device__ __forceinline__ int route_row(const gt_route_args& a, int64_t t, int lane, float* lds) {
+  const float ninf = -__builtin_inff();
   const int E = a.E, k = a.k;
   float x[EPL], key[EPL];
   load_logits<T, EPL>(a.logits, t * a.ldl, E, lane, x);
@@ -177,31 +206,30 @@ __device__ __forceinline__ int route_row(const gt_route_args& a, int64_t t, int 
     const int e = i * 64 + lane;
     if (a.bias && e < E) {
       key[i] = x[i] + a.bias[e];
-      if (!(key[i] == key[i])) key[i] = -__builtin_inff();
+      if (!(key[i] == key[i])) key[i] = ninf;
     }
   }
-  if (a.groups > 1) keep_groups<EPL>(E, a.groups, a.keep, lane, keys, runs, key);
-  int mine = -1;       // lane s: the expert of slot s
-  float chosen = 0.0f; // and its logit
-  const uint32_t none = ordered(-__builtin_inff());
+  if (a.groups > 1) keep_groups<EPL>(E, a.groups, a.keep, lane, lds, lds + E, key);
+  int mine = -1;
   for (int s = 0; s < k; ++s) {
-    uint64_t best = 0;
+    float m = key[0];
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      const uint64_t c = static_cast<uint64_t>(ordered(key[i])) << 32 |
-                         static_cast<uint32_t>(~(i * 64 + lane));
-      best = c > best ? c : best;
+    for (int i = 1; i < EPL; ++i) m = fmaxf(m, key[i]);
+    m = wave_max(m);
+    if (!(m > ninf)) break;
+    int e = 0;
+#pragma unroll
+    for (int i = EPL - 1; i >= 0; --i) {
+      const uint64_t has = __ballot(key[i] == m);
+      if (has) e = i * 64 + __builtin_ctzll(has);
     }
-    best = wave_max(best);
-    if (static_cast<uint32_t>(best >> 32) <= none) break;
-    const int e = static_cast<int>(~static_cast<uint32_t>(best));
     if (lane == s) mine = e;
 #pragma unroll
     for (int i = 0; i < EPL; ++i)
-      if (i * 64 + lane == e) key[i] = -__builtin_inff();
+      if (i * 64 + lane == e) key[i] = ninf;
   }
   const bool live = mine >= 0;
-  if (live) chosen = to_float(static_cast<const T*>(a.logits)[t * a.ldl + mine]);
+  const float chosen = live ? to_float(static_cast<const T*>(a.logits)[t * a.ldl + mine]) : 0.0f;
   const Shares sh = shares_of<EPL>(a.score, a.renormalise, x, chosen, live);
   if (lane < k) {
     a.experts[t * k + lane] = mine;
@@ -210,35 +238,28 @@ __device__ __forceinline__ int route_row(const gt_route_args& a, int64_t t, int 
   return mine;
 }
 
-// Scores and choice; one wavefront a token.
+// Scores and choice of a block's tokens, and their counts per expert.
 template <typename T, int EPL>
-__global__ __launch_bounds__(256) void route_kernel(const RouteArgs r) {
+__global__ __launch_bounds__(64 * kWaves) void route_kernel(const RouteArgs r) {
   extern __shared__ float lds[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * 4 + wave;
-  if (t >= r.a.T) return;
-  float* keys = lds + wave * (r.a.E + r.a.groups);
-  route_row<T, EPL>(r.a, t, lane, keys, keys + r.a.E);
-}
-
-// Counts per expert of each block of entries.
-__global__ __launch_bounds__(kEntries) void count_kernel(const RouteArgs r) {
   __shared__ int hist[kMaxE];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int E = r.a.E;
-  for (int e = threadIdx.x; e < E; e += kEntries) hist[e] = 0;
+  for (int e = threadIdx.x; e < E; e += 64 * kWaves) hist[e] = 0;
   __syncthreads();
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kEntries + threadIdx.x;
-  if (i < r.a.T * r.a.k) {
-    const int e = r.a.experts[i];
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * r.tokens;
+  const int64_t t1 = t0 + r.tokens < r.a.T ? t0 + r.tokens : r.a.T;
+  for (int64_t t = t0 + wave; t < t1; t += kWaves) {
+    const int e = route_row<T, EPL>(r.a, t, lane, lds + wave * group_floats(E, r.a.groups));
     if (e >= 0) atomicAdd(&hist[e], 1);   // whole numbers: any order gives the same
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < E; e += kEntries) r.counts[blockIdx.x * static_cast<int64_t>(E) + e] = hist[e];
+  for (int e = threadIdx.x; e < E; e += 64 * kWaves)
+    r.counts[static_cast<int64_t>(blockIdx.x) * E + e] = hist[e];
 }
 
-// The exclusive prefix over the wavefront-held totals of up to kMaxE experts.
-__device__ __forceinline__ void scan_experts(int* total, int E, int* first) {
-  // total[E] in LDS → first[0 … E]; called by the first wavefront
+// total[E] in LDS → first[0 … E], the sums before each; called by the first wavefront.
+__device__ __forceinline__ void scan_experts(const int* total, int E, int* first) {
   const int lane = threadIdx.x & 63;
   int before = 0;
   for (int e0 = 0; e0 < E; e0 += 64) {
@@ -255,82 +276,99 @@ __device__ __forceinline__ void scan_experts(int* total, int E, int* first) {
   if (lane == 0) first[E] = before;
 }
 
-// counts[block][e] → the first position of block's entries of expert e; offsets.
-__global__ __launch_bounds__(1024) void scan_kernel(const RouteArgs r) {
-  __shared__ int total[kMaxE], first[kMaxE + 1];
-  const int E = r.a.E;
-  for (int e = threadIdx.x; e < E; e += 1024) {
-    int sum = 0;
-    for (int64_t b = 0; b < r.blocks; ++b) sum += r.counts[b * E + e];
-    total[e] = sum;
+// The lanes that hold the same expert as this one (all lanes active; −1 too).
+__device__ __forceinline__ uint64_t same_expert(int e) {
+  uint64_t same = ~uint64_t{0};
+#pragma unroll
+  for (int b = 0; b < 11; ++b) {   // an expert's ten bits, and that of −1
+    const bool set = (e >> b) & 1;
+    const uint64_t v = __ballot(set);
+    same &= set ? v : ~v;
+  }
+  return same;
+}
+
+// Gives each of up to kEntries entries (thread i's expert e, −1: none) its place; at[e]
+// is the next place of expert e and moves on. The wavefronts take turns.
+__device__ __forceinline__ int place_entry(int e, int* at) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t same = same_expert(e);
+  const int rank = __popcll(same & ((uint64_t{1} << lane) - 1));
+  int p = -1;
+  for (int w = 0; w < kEntries / 64; ++w) {
+    if (wave == w && e >= 0) {
+      p = at[e] + rank;
+      __builtin_amdgcn_wave_barrier();
+      if (rank == 0) at[e] += __popcll(same);
+    }
+    __syncthreads();
+  }
+  return p;
+}
+
+// Each entry of a block's tokens to its place; the order after the last entry to −1; the
+// offsets.
+__global__ __launch_bounds__(kEntries) void place_kernel(const RouteArgs r) {
+  __shared__ int total[kMaxE], before[kMaxE], first[kMaxE + 1];
+  const int E = r.a.E, k = r.a.k, b = static_cast<int>(blockIdx.x);
+  for (int e = threadIdx.x; e < E; e += kEntries) {
+    int mine = 0, all = 0;
+#pragma unroll 8
+    for (int i = 0; i < r.blocks; ++i) {
+      const int c = r.counts[static_cast<int64_t>(i) * E + e];
+      all += c;
+      mine += i < b ? c : 0;
+    }
+    total[e] = all;
+    before[e] = mine;
   }
   __syncthreads();
   if (threadIdx.x < 64) scan_experts(total, E, first);
   __syncthreads();
-  for (int e = threadIdx.x; e <= E; e += 1024) r.a.offsets[e] = first[e];
-  for (int e = threadIdx.x; e < E; e += 1024) {
-    int at = first[e];
-    for (int64_t b = 0; b < r.blocks; ++b) {
-      const int c = r.counts[b * E + e];
-      r.counts[b * E + e] = at;
-      at += c;
-    }
-  }
-}
-
-// Each entry of a block to its place; the order after the last entry to −1.
-__global__ __launch_bounds__(kEntries) void place_kernel(const RouteArgs r) {
-  __shared__ __align__(16) int ids[kEntries];
-  const int64_t n = r.a.T * r.a.k;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kEntries + threadIdx.x;
-  const int e = i < n ? r.a.experts[i] : -1;
-  ids[threadIdx.x] = e;
+  for (int e = threadIdx.x; e < E; e += kEntries) before[e] += first[e];
+  if (b == 0)
+    for (int e = threadIdx.x; e <= E; e += kEntries) r.a.offsets[e] = first[e];
   __syncthreads();
-  int rank = 0;
-  for (int j = 0; j < static_cast<int>(threadIdx.x); ++j) rank += ids[j] == e ? 1 : 0;
-  if (i < n) {
-    int p = -1;
-    if (e >= 0) {
-      p = r.counts[blockIdx.x * static_cast<int64_t>(r.a.E) + e] + rank;
-      r.a.order[p] = static_cast<int32_t>(i);
+  const int64_t n = r.a.T * k, i0 = static_cast<int64_t>(b) * r.tokens * k;
+  const int64_t i1 = i0 + static_cast<int64_t>(r.tokens) * k < n ? i0 + static_cast<int64_t>(r.tokens) * k : n;
+  for (int64_t at = i0; at < i1; at += kEntries) {
+    const int64_t i = at + threadIdx.x;
+    const int p = place_entry(i < i1 ? r.a.experts[i] : -1, before);
+    if (i < i1) {
+      if (p >= 0) r.a.order[p] = static_cast<int32_t>(i);
+      r.a.place[i] = p;
+      if (i >= first[E]) r.a.order[i] = -1;
     }
-    r.a.place[i] = p;
-    if (i >= r.a.offsets[r.a.E]) r.a.order[i] = -1;
   }
 }
 
 // A few tokens: everything in one block.
 template <typename T, int EPL>
-__global__ __launch_bounds__(1024) void route_few_kernel(const RouteArgs r) {
+__global__ __launch_bounds__(64 * kWaves) void route_few_kernel(const RouteArgs r) {
   extern __shared__ float lds[];
-  __shared__ __align__(16) int ids[kEntries];
+  __shared__ int ids[kEntries];
   __shared__ int total[kMaxE], first[kMaxE + 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int E = r.a.E, k = r.a.k;
-  for (int e = threadIdx.x; e < E; e += 1024) total[e] = 0;
-  float* keys = lds + wave * (E + r.a.groups);
-  for (int64_t t = wave; t < r.a.T; t += 16) {
-    const int mine = route_row<T, EPL>(r.a, t, lane, keys, keys + E);
-    if (lane < k) ids[t * k + lane] = mine;
-  }
+  for (int e = threadIdx.x; e < E; e += 64 * kWaves) total[e] = 0;
   __syncthreads();
-  const int n = static_cast<int>(r.a.T) * k;
-  const int i = threadIdx.x;
-  const int e = i < n ? ids[i] : -1;
-  int rank = 0;
-  if (e >= 0) {
-    atomicAdd(&total[e], 1);
-    for (int j = 0; j < i; ++j) rank += ids[j] == e ? 1 : 0;
+  for (int64_t t = wave; t < r.a.T; t += kWaves) {
+    const int e = route_row<T, EPL>(r.a, t, lane, lds + wave * group_floats(E, r.a.groups));
+    if (lane < k) ids[t * k + lane] = e;
+    if (e >= 0) atomicAdd(&total[e], 1);
   }
   __syncthreads();
   if (wave == 0) scan_experts(total, E, first);
   __syncthreads();
-  for (int x = threadIdx.x; x <= E; x += 1024) r.a.offsets[x] = first[x];
+  for (int x = threadIdx.x; x <= E; x += 64 * kWaves) r.a.offsets[x] = first[x];
+  const int n = static_cast<int>(r.a.T) * k, all = first[E];
+  __syncthreads();
+  const int i = threadIdx.x;
+  const int p = place_entry(i < n ? ids[i < kEntries ? i : 0] : -1, first);
   if (i < n) {
-    const int p = e >= 0 ? first[e] + rank : -1;
     if (p >= 0) r.a.order[p] = i;
     r.a.place[i] = p;
-    if (i >= first[E]) r.a.order[i] = -1;
+    if (i >= all) r.a.order[i] = -1;
   }
 }
 
@@ -376,27 +414,37 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const gt_route_grad_arg
   }
 }
 
-// Whether one block does all: one launch, no scratch, and the keys of 16 tokens
-// in its LDS.
+// Tokens of a block: whole rounds of its wavefronts, at most kMaxBlocks blocks.
+int32_t block_tokens(int64_t T) {
+  const int64_t each = (T + kMaxBlocks - 1) / kMaxBlocks;
+  return static_cast<int32_t>((each + kWaves - 1) / kWaves * kWaves);
+}
+
+// Whether one block does all: one launch, no scratch, and the keys of its wavefronts'
+// tokens in 64 KiB of LDS.
 bool few(int64_t T, int E, int k, int groups) {
-  return T <= 64 && T * k <= kEntries && E + groups <= 640;
+  return T == 0 || (T <= 64 && T * k <= kEntries && group_floats(E, groups) * kWaves * 4 <= 48 * 1024);
 }
 
 template <typename T, int EPL>
 hipError_t route_by(const gt_route_args& a, void* ws, hipStream_t s) {
-  const RouteArgs r{a, static_cast<int32_t*>(ws), (a.T * a.k + kEntries - 1) / kEntries};
+  RouteArgs r{a, static_cast<int32_t*>(ws), 0, 0};
+  const size_t lds = a.T == 0 ? 0 : group_floats(a.E, a.groups) * kWaves * sizeof(float);
   if (few(a.T, a.E, a.k, a.groups)) {
-    route_few_kernel<T, EPL><<<1, 1024, 16 * (a.E + a.groups) * sizeof(float), s>>>(r);
+    route_few_kernel<T, EPL><<<1, 64 * kWaves, lds, s>>>(r);
     return hipGetLastError();
   }
-  route_kernel<T, EPL><<<static_cast<unsigned>((a.T + 3) / 4), 256,
-                         4 * (a.E + a.groups) * sizeof(float), s>>>(r);
-  hipError_t e = hipGetLastError();
+  if (lds > 48 * 1024) {   // E + groups beyond 640: a launch may use more than its default LDS
+    const hipError_t e =
+        hipFuncSetAttribute(reinterpret_cast<const void*>(route_kernel<T, EPL>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+    if (e != hipSuccess) return e;
+  }
+  r.tokens = block_tokens(a.T);
+  r.blocks = static_cast<int32_t>((a.T + r.tokens - 1) / r.tokens);
+  route_kernel<T, EPL><<<static_cast<unsigned>(r.blocks), 64 * kWaves, lds, s>>>(r);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  count_kernel<<<static_cast<unsigned>(r.blocks), kEntries, 0, s>>>(r);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  scan_kernel<<<1, 1024, 0, s>>>(r);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
   place_kernel<<<static_cast<unsigned>(r.blocks), kEntries, 0, s>>>(r);
   return hipGetLastError();
 }
@@ -419,7 +467,8 @@ hipError_t grad_by(const gt_route_grad_args& a, hipStream_t s) {
 
 int64_t route_scratch(int64_t T, int E, int k, int groups) {
   if (few(T, E, k, groups)) return 0;
-  return (T * k + kEntries - 1) / kEntries * E * static_cast<int64_t>(sizeof(int32_t));
+  const int64_t tokens = block_tokens(T);
+  return (T + tokens - 1) / tokens * E * static_cast<int64_t>(sizeof(int32_t));
 }
 
 hipError_t launch_route(const gt_route_args& a, void* ws, hipStream_t s) {
