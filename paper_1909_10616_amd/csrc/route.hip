@@ -35,6 +35,30 @@ struct RouteArgs {
   int32_t tokens;    // of a block
 };
 
+// Keys are compared as signed integers in the order of the floats (−0 and 0 equal; no NaN
+// comes here): whole-number maxima take one instruction where a float's take
+// three, the scalar unit joins the rows of 16, and no key needs its NaN quieted.
+constexpr int32_t kNone = static_cast<int32_t>(0x807fffffu);   // of −inf
+__device__ __forceinline__ int32_t ordered(float v) {
+  const int32_t b = __builtin_bit_cast(int32_t, v + 0.0f);
+  return b ^ ((b >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float unordered(int32_t v) {
+  return __builtin_bit_cast(float, v ^ ((v >> 31) & 0x7fffffff));
+}
+template <int CTRL>
+__device__ __forceinline__ int32_t moved(int32_t v) {
+  return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
+}
+__device__ __forceinline__ int32_t wave_max(int32_t v) {
+  v = max(v, moved<0xb1>(v));
+  v = max(v, moved<0x4e>(v));
+  v = max(v, moved<0x141>(v));
+  v = max(v, moved<0x140>(v));
+  return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+             max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+
 // The value of the lane that a move within 16 lanes names.
 template <int CTRL>
 __device__ __forceinline__ float moved(float v) {
@@ -130,112 +154,158 @@ __device__ __forceinline__ void load_logits(const void* logits, int64_t at, int 
 
 // The two largest of a run's keys.
 struct Best {
-  float a, b;
-  __device__ __forceinline__ void add(float v) {
-    b = fmaxf(b, fminf(a, v));
-    a = fmaxf(a, v);
+  int32_t a, b;
+  __device__ __forceinline__ void add(int32_t v) {
+    b = max(b, min(a, v));
+    a = max(a, v);
+  }
+  __device__ __forceinline__ void add(int32_t x, int32_t y) {   // x ≥ y, of other keys
+    add(x);
+    b = max(b, y);
   }
 };
 
-// The keys of experts outside the kept groups become −inf. keys, runs: this
-// wavefront's LDS (E keys, 128 + groups values). Up to 32 groups are scored by 64 / groups
-// lanes each.
+// What does not change from token to token: the lanes of a run and the runs of this
+// lane's experts.
 template <int EPL>
-__device__ __forceinline__ void keep_groups(int E, int groups, int keep, int lane, float* keys,
-                                            float* runs, float (&key)[EPL]) {
-  const float ninf = -__builtin_inff();
-  const int size = E / groups;
-  float* const score = runs + 128;
+struct Runs {
+  int size, parts, part, first;   // keys of a run, lanes a run (a power of two), this lane's part, its first run
+  int mine[EPL];                  // the run of expert i·64 + lane
+  float bias[EPL];
+  __device__ __forceinline__ Runs(const gt_route_args& a, int lane) {
+    size = a.E / a.groups;
+    parts = 1;
+    while (parts < 64 && 2 * parts * a.groups <= 64) parts *= 2;
+    part = lane & (parts - 1);
+    first = lane / parts;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      const int e = i * 64 + lane;
+      mine[i] = e / size;
+      bias[i] = a.bias && e < a.E ? a.bias[e] : 0.0f;
+    }
+  }
+};
+
+// The keys of experts outside the kept groups become −inf. keys, score: this wavefront's LDS
+// (E keys, `groups` scores). A run's two largest keys by `parts` lanes each; a run
+// stays if fewer than `keep` runs beat it.
+template <int EPL>
+__device__ __forceinline__ void keep_groups(const Runs<EPL>& runs, int E, int groups, int keep,
+                                            int lane, int32_t* keys, int32_t* score,
+                                            int32_t (&key)[EPL]) {
 #pragma unroll
   for (int i = 0; i < EPL; ++i)
     if (i * 64 + lane < E) keys[i * 64 + lane] = key[i];
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  const int parts = groups > 32 ? 1 : 64 / groups;
   for (int g0 = 0; g0 < groups; g0 += 64) {
-    const int g = g0 + (parts > 1 ? lane % groups : lane), part = parts > 1 ? lane / groups : 0;
-    Best best{ninf, ninf};
-    if (g < groups && part < parts)
-      for (int j = part; j < size; j += parts) best.add(keys[g * size + j]);
-    if (parts > 1) {
-      runs[2 * lane] = best.a;
-      runs[2 * lane + 1] = best.b;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      if (part == 0)
-        for (int j = 1; j < parts; ++j) {
-          best.add(runs[2 * (lane + j * groups)]);
-          best.add(runs[2 * (lane + j * groups) + 1]);
-        }
-    }
-    if (g < groups && part == 0) {
-      const float s = size > 1 ? best.a + best.b : best.a;
-      score[g] = s == s ? s : ninf;   // (+inf and −inf in one run)
-    }
+    const int g = g0 + runs.first;
+    Best best{kNone, kNone};
+    if (g < groups)
+      for (int j = runs.part; j < runs.size; j += runs.parts) best.add(keys[g * runs.size + j]);
+    if (runs.parts > 1) best.add(moved<0xb1>(best.a), moved<0xb1>(best.b));
+    if (runs.parts > 2) best.add(moved<0x4e>(best.a), moved<0x4e>(best.b));
+    if (runs.parts > 4) best.add(moved<0x141>(best.a), moved<0x141>(best.b));
+    if (runs.parts > 8) best.add(moved<0x140>(best.a), moved<0x140>(best.b));
+    if (runs.parts > 16) best.add(__shfl_xor(best.a, 16), __shfl_xor(best.b, 16));
+    const float s = unordered(best.a) + unordered(best.b);   // (NaN: +inf and −inf in one run)
+    if (g < groups && runs.part == 0)
+      score[g] = runs.size == 1 ? best.a : s == s ? ordered(s) : kNone;
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  // an expert's run stays if fewer than `keep` runs beat it
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    const int e = i * 64 + lane;
-    if (e >= E) continue;
-    const int g = e / size;
-    const float mine = score[g];
+  if (groups <= 64) {
+    const int32_t own = lane < groups ? score[lane] : kNone;
     int better = 0;
     for (int o = 0; o < groups; ++o) {
-      const float v = score[o];
-      better += v > mine || (v == mine && o < g) ? 1 : 0;
+      const int32_t v = __builtin_amdgcn_readlane(own, o);
+      better += v > own || (v == own && o < lane) ? 1 : 0;
     }
-    if (better >= keep) key[i] = ninf;
+    const uint64_t kept = __ballot(lane < groups && better < keep);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i)
+      if (!((kept >> (runs.mine[i] & 63)) & 1)) key[i] = kNone;
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      if (i * 64 + lane >= E) continue;
+      const int g = runs.mine[i];
+      const int32_t mine = score[g];
+      int better = 0;
+      for (int o = 0; o < groups; ++o) {
+        const int32_t v = score[o];
+        better += v > mine || (v == mine && o < g) ? 1 : 0;
+      }
+      if (better >= keep) key[i] = kNone;
+    }
   }
 }
 
 // LDS floats a wavefront needs to keep groups.
 __host__ __device__ constexpr int group_floats(int E, int groups) {
-  return groups > 1 ? E + 128 + groups : 0;
+  return groups > 1 ? E + groups : 0;
 }
 
-// Scores and choice of one token; lane s returns the expert of slot s (−1: none).
-template <typename T, int EPL>
-__device__ __forceinline__ int route_row(const gt_route_args& a, int64_t t, int lane, float* lds) {
-  const float ninf = -__builtin_inff();
+// Scores and choice of token t, whose logits x are; lane s returns the expert of slot s
+// (−1: none).
+template <int EPL>
+__device__ __forceinline__ int route_row(const gt_route_args& a, const Runs<EPL>& runs, int64_t t,
+                                         int lane, float* lds, const float (&x)[EPL]) {
   const int E = a.E, k = a.k;
-  float x[EPL], key[EPL];
-  load_logits<T, EPL>(a.logits, t * a.ldl, E, lane, x);
+  int32_t key[EPL];
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
-    key[i] = x[i];
-    const int e = i * 64 + lane;
-    if (a.bias && e < E) {
-      key[i] = x[i] + a.bias[e];
-      if (!(key[i] == key[i])) key[i] = ninf;
-    }
+    const float v = x[i] + runs.bias[i];
+    key[i] = v == v ? ordered(v) : kNone;
   }
-  if (a.groups > 1) keep_groups<EPL>(E, a.groups, a.keep, lane, lds, lds + E, key);
+  if (a.groups > 1)
+    keep_groups<EPL>(runs, E, a.groups, a.keep, lane, reinterpret_cast<int32_t*>(lds),
+                     reinterpret_cast<int32_t*>(lds) + E, key);
   int mine = -1;
+  float chosen = 0.0f;
   for (int s = 0; s < k; ++s) {
-    float m = key[0];
+    int32_t m = key[0];
 #pragma unroll
-    for (int i = 1; i < EPL; ++i) m = fmaxf(m, key[i]);
+    for (int i = 1; i < EPL; ++i) m = max(m, key[i]);
     m = wave_max(m);
-    if (!(m > ninf)) break;
-    int e = 0;
+    if (m == kNone) break;
+    bool found = false;
 #pragma unroll
-    for (int i = EPL - 1; i >= 0; --i) {
+    for (int i = 0; i < EPL; ++i) {
       const uint64_t has = __ballot(key[i] == m);
-      if (has) e = i * 64 + __builtin_ctzll(has);
+      if (!found && has != 0) {
+        found = true;
+        const int at = __builtin_ctzll(has);
+        const float logit = lane_of(x[i], at);
+        if (lane == s) {
+          mine = i * 64 + at;
+          chosen = logit;
+        }
+        if (lane == at) key[i] = kNone;
+      }
     }
-    if (lane == s) mine = e;
-#pragma unroll
-    for (int i = 0; i < EPL; ++i)
-      if (i * 64 + lane == e) key[i] = ninf;
   }
-  const bool live = mine >= 0;
-  const float chosen = live ? to_float(static_cast<const T*>(a.logits)[t * a.ldl + mine]) : 0.0f;
-  const Shares sh = shares_of<EPL>(a.score, a.renormalise, x, chosen, live);
+  const Shares sh = shares_of<EPL>(a.score, a.renormalise, x, chosen, mine >= 0);
   if (lane < k) {
     a.experts[t * k + lane] = mine;
     a.weights[t * k + lane] = a.scale * sh.part;
   }
   return mine;
+}
+
+// A wavefront's tokens t, t + kWaves, … below t1, the next one's logits loaded while the
+// choice of one goes on; then(t, expert of the lane's slot).
+template <typename T, int EPL, typename F>
+__device__ __forceinline__ void route_rows(const gt_route_args& a, int64_t t, int64_t t1, int lane,
+                                           float* lds, F then) {
+  const Runs<EPL> runs(a, lane);
+  float x[EPL], next[EPL];
+  if (t < t1) load_logits<T, EPL>(a.logits, t * a.ldl, a.E, lane, next);
+  for (; t < t1; t += kWaves) {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) x[i] = next[i];
+    if (t + kWaves < t1) load_logits<T, EPL>(a.logits, (t + kWaves) * a.ldl, a.E, lane, next);
+    then(t, route_row<EPL>(a, runs, t, lane, lds, x));
+  }
 }
 
 // Scores and choice of a block's tokens, and their counts per expert.
@@ -249,10 +319,10 @@ __global__ __launch_bounds__(64 * kWaves) void route_kernel(const RouteArgs r) {
   __syncthreads();
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * r.tokens;
   const int64_t t1 = t0 + r.tokens < r.a.T ? t0 + r.tokens : r.a.T;
-  for (int64_t t = t0 + wave; t < t1; t += kWaves) {
-    const int e = route_row<T, EPL>(r.a, t, lane, lds + wave * group_floats(E, r.a.groups));
-    if (e >= 0) atomicAdd(&hist[e], 1);   // whole numbers: any order gives the same
-  }
+  route_rows<T, EPL>(r.a, t0 + wave, t1, lane, lds + wave * group_floats(E, r.a.groups),
+                     [&](int64_t, int e) {
+                       if (e >= 0) atomicAdd(&hist[e], 1);   // whole numbers: any order gives the same
+                     });
   __syncthreads();
   for (int e = threadIdx.x; e < E; e += 64 * kWaves)
     r.counts[static_cast<int64_t>(blockIdx.x) * E + e] = hist[e];
@@ -311,16 +381,21 @@ __device__ __forceinline__ int place_entry(int e, int* at) {
 __global__ __launch_bounds__(kEntries) void place_kernel(const RouteArgs r) {
   __shared__ int total[kMaxE], before[kMaxE], first[kMaxE + 1];
   const int E = r.a.E, k = r.a.k, b = static_cast<int>(blockIdx.x);
-  for (int e = threadIdx.x; e < E; e += kEntries) {
+  for (int e = threadIdx.x; e < E; e += kEntries) total[e] = before[e] = 0;
+  __syncthreads();
+  // the blocks' counts, by as many threads an expert as there are
+  const int parts = E < kEntries ? kEntries / E : 1;
+  for (int x = threadIdx.x; x < E * parts; x += kEntries) {
+    const int e = x % E, part = x / E;
     int mine = 0, all = 0;
-#pragma unroll 8
-    for (int i = 0; i < r.blocks; ++i) {
+#pragma unroll 16
+    for (int i = part; i < r.blocks; i += parts) {
       const int c = r.counts[static_cast<int64_t>(i) * E + e];
       all += c;
       mine += i < b ? c : 0;
     }
-    total[e] = all;
-    before[e] = mine;
+    atomicAdd(&total[e], all);
+    atomicAdd(&before[e], mine);
   }
   __syncthreads();
   if (threadIdx.x < 64) scan_experts(total, E, first);
@@ -352,11 +427,11 @@ __global__ __launch_bounds__(64 * kWaves) void route_few_kernel(const RouteArgs 
   const int E = r.a.E, k = r.a.k;
   for (int e = threadIdx.x; e < E; e += 64 * kWaves) total[e] = 0;
   __syncthreads();
-  for (int64_t t = wave; t < r.a.T; t += kWaves) {
-    const int e = route_row<T, EPL>(r.a, t, lane, lds + wave * group_floats(E, r.a.groups));
-    if (lane < k) ids[t * k + lane] = e;
-    if (e >= 0) atomicAdd(&total[e], 1);
-  }
+  route_rows<T, EPL>(r.a, wave, r.a.T, lane, lds + wave * group_floats(E, r.a.groups),
+                     [&](int64_t t, int e) {
+                       if (lane < k) ids[t * k + lane] = e;
+                       if (e >= 0) atomicAdd(&total[e], 1);
+                     });
   __syncthreads();
   if (wave == 0) scan_experts(total, E, first);
   __syncthreads();

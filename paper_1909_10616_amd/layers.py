@@ -305,10 +305,10 @@ def gt_route(logits, k, bias=None, score="softmax", groups=1, keep=1, renormalis
     if not 1 <= k <= E:
         raise ValueError(f"k is {k}, with {E} experts")
     n = T * k
-    weights = _empty((T, k), torch.float32, logits.device, stream)
-    ints = _empty((3 * n + E + 1,), torch.int32, logits.device, stream)
-    experts, place = ints[:n].view(T, k), ints[n:2 * n].view(T, k)
-    order, offsets = ints[2 * n:3 * n], ints[3 * n:]
+    dev = logits.device
+    weights = _empty((T, k), torch.float32, dev, stream)
+    experts, place = _empty((2, T, k), torch.int32, dev, stream).unbind(0)
+    order, offsets = _empty((n,), torch.int32, dev, stream), _empty((E + 1,), torch.int32, dev, stream)
     _call("gt_route", gt_route_args(T, E, k, groups, keep, dt, SCORES[score], int(bool(renormalise)),
                                     scale, x, ldl, b, weights.data_ptr(), experts.data_ptr(),
                                     offsets.data_ptr(), order.data_ptr(), place.data_ptr()),
