@@ -58,6 +58,7 @@ struct Product {
   bool own_a = false, own_b = false;
   int tile = 1;
   bool reg = false;
+  int rows = 0;           // > 0: the kernel for a few rows, so many a workgroup
   PadJobs pad{};          // operands copied to aligned rows first …
   int64_t pad_a = 0, pad_b = 0, part = 0;   // … and the bytes of that and of partial sums
 
@@ -92,23 +93,54 @@ Stored stored(const void* ptr, int64_t ld, int64_t sgroup, int64_t groups, int64
   return s;
 }
 
-// What a stage (128 bytes of k) of a tile takes a compute unit, in µs: alone, and
-// when others share the unit.
-struct StageCost {
-  double alone, shared;
+// Rows a workgroup of the kernel for a few rows takes, 0 where it does not serve: up to 4
+// rows, or up to 4 a group on average (the groups that get a row, were the rows
+// spread evenly), that fit its LDS.
+int few_rows(const Product& p) {
+  const ProductArgs& a = p.a;
+  if (p.layout != kXW || a.M < 1) return 0;
+  double each = static_cast<double>(a.M);
+  if (a.groups > 0) {
+    if (a.M > 4 * a.groups) return 0;
+    double none = 1.0;   // that a group gets no row
+    for (int64_t i = 0; i < a.M; ++i) none *= 1.0 - 1.0 / a.groups;
+    each = a.M / (a.groups * (1.0 - none));
+  }
+  const int rows = each <= 1.3 ? 1 : each <= 2.3 ? 2 : each <= 4.0 ? 4 : 0;
+  if (rows == 0 || rows_lds(a.K, rows, p.a.e.epi == kEpiGated) > 128 * 1024) return 0;
+  return a.M / rows + a.groups < 65536 ? rows : 0;
+}
+
+// What a tile takes a compute unit, in µs: a stage (128 bytes of k) alone and
+// when others share the unit, its launch and epilogue, and how many share it. Fitted to
+// 21 shapes from 1×4096×4096 to 2048×4096×4096 in every layout, each at every tile and 1
+// to 32 K slices (bf16, K = 4096, one slice: 256×256 tiles 76 µs for 16 of them, 114
+// for 256; 128×128 43, 75 for 512; 64×64 28, 114 for 2048; 16×128 22, 221 for 4096).
+// The choice is then within 5 % of the best of them, at most 11 % behind it.
+struct TileCost {
+  double alone, shared, fixed;
+  int resident;
 };
-constexpr StageCost kStage[2][kTiles] = {
-    {{0, 0}, {1.9, 1.75}, {0.75, 0.5}, {0.5, 0.3}},       // fp32
-    {{1.6, 1.6}, {0.62, 0.53}, {0.4, 0.25}, {0.4, 0.15}}  // bf16
+constexpr TileCost kCost[2][kTiles] = {
+    {{0, 0, 0, 1}, {2.05, 2.0, 6, 2}, {0.78, 0.6, 5, 3}, {0.49, 0.37, 5, 2}},          // fp32
+    {{1.62, 1.62, 8, 1}, {0.64, 0.55, 4.3, 2}, {0.375, 0.25, 4.2, 3}, {0.28, 0.235, 4.3, 2}}  // bf16
 };
 
-// Tile, K slices and copies by the time they should take: stages of the tiles that a
-// compute unit gets (256 of them), a K slice's partial sums through memory and the
-// launch that joins them, the copies of operands that 16-byte loads do not serve
-// and their launch; the register path takes those as they are, at twice the time of a
-// stage.
+// Tile, K slices and copies by the time they should take: the stages of the tiles that a
+// compute unit gets (256 of them) or the operands' way from memory, a K slice's partial
+// sums and the launch that joins them, the copies of operands that 16-byte
+// loads do not serve and their launch; the register path takes those as they are, at
+// 2.2 (bf16) and 1.2 times (fp32, bound by its MFMAs) the time of a stage.
 void choose(Product* p, bool may_split) {
   ProductArgs& a = p->a;
+  if ((p->rows = few_rows(*p)) > 0) {
+    a.half = a.N;
+    a.splits = 1;
+    a.tilesN = static_cast<int>((a.N + 63) / 64);
+    a.tilesM = static_cast<int>(a.groups > 0 ? a.M / p->rows + std::min<int64_t>(a.groups, a.M)
+                                             : (a.M + p->rows - 1) / p->rows);
+    return;
+  }
   const int64_t sz = size_of(p->dtype), bk = 128 / sz;
   const bool gated = a.e.epi == kEpiGated;
   const int64_t wide = gated ? 2 * a.N : a.N;
@@ -137,16 +169,18 @@ void choose(Product* p, bool may_split) {
     }
     const int64_t tiles = tm * tn * (a.along_k ? a.groups : 1);
     if (most * tn >= kMaxExtent) continue;
-    const StageCost& c = kStage[p->dtype == GT_BF16 ? 1 : 0][t];
+    const TileCost& c = kCost[p->dtype == GT_BF16 ? 1 : 0][t];
+    const double memory = static_cast<double>(a.M * a.K + std::min(bgroups, std::max<int64_t>(1, a.M)) * a.K * wide) * sz / 5.2e6;
     for (int reg = 0; reg < 2; ++reg) {
       if (reg ? (t < 2 || (sa.ok && sb.ok)) : !can_dma) continue;
-      const double copy = !reg && copies ? 5.0 + 2.0 * ((sa.ok ? 0 : sa.bytes) + (sb.ok ? 0 : sb.bytes)) / 4.5e6 : 0.0;
+      const double copy = !reg && copies ? 5.0 + 2.0 * ((sa.ok ? 0 : sa.bytes) + (sb.ok ? 0 : sb.bytes)) / 5.0e6 : 0.0;
       for (int64_t z = 1; z <= 64; z *= 2) {
         if (z > 1 && (!may_split || stages / z < 4)) break;
-        const double each = static_cast<double>((stages + z - 1) / z) * (reg ? 2.0 : 1.0);
-        const double queue = std::max(c.alone, c.shared * ((tiles * z + 255) / 256));
-        double cost = copy + each * queue + 4.0;
-        if (z > 1) cost += 4.0 + 2.0 * z * a.M * wide * 4 / 4.0e6;
+        const double each = static_cast<double>((stages + z - 1) / z) * (!reg ? 1.0 : p->dtype == GT_BF16 ? 2.2 : 1.2);
+        const int64_t queue = (tiles * z + 255) / 256;
+        double cost = copy + std::max(each * std::max(c.alone, c.shared * queue), memory) +
+                      c.fixed * ((queue + c.resident - 1) / c.resident);
+        if (z > 1) cost += 4.5 + 2.0 * z * a.M * wide * 4 / 6.0e6;
         if (best == 0.0 || cost < best) {
           best = cost;
           p->tile = t;
@@ -185,6 +219,10 @@ int run(const Product& p, void* ws, hipStream_t s) {
   ProductArgs a = p.a;
   if (a.M == 0) return GT_OK;
   if (a.splits < 1) return fail("layer product: too many tiles");
+  if (p.rows > 0) {
+    GT_TRY(launch_rows(p.dtype, p.rows, a, s), "layer product of a few rows");
+    return GT_OK;
+  }
   char* at = static_cast<char*>(ws);
   if (p.pad.n > 0) {
     PadJobs jobs = p.pad;
