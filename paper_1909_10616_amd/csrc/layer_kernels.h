@@ -54,12 +54,25 @@ hipError_t launch_act_grad(int dtype, const ActGradArgs& a, hipStream_t s);
 hipError_t launch_join(const float* part, int64_t rows, int64_t wide, const int32_t* offsets,
                        int groups, int64_t most, int bm, int per, float* out, hipStream_t s);
 
-// Rows of X and dY of the sorted entries: dst[p] = src[order[p] / k] for every
-// p below offsets[E] (either pair may be NULL).
-hipError_t launch_gather(int dtype, const void* a, int64_t lda, void* da, const void* b, int64_t ldb,
-                         void* db, int64_t ldd, int64_t cols, const int32_t* order,
-                         const int32_t* offsets, int E, int64_t entries, int k, int64_t T,
-                         hipStream_t s);
+// The sorted entries' rows of X and dY, in rows of whole 16-byte chunks, zero beyond D:
+// Xs[p] = X[order[p] / k] (X NULL: not wanted), dYs[p] likewise; and of each block of kSortRows
+// rows of a group and kSortCols columns
+//   sums[block row][D]: Σ w·dY over its rows (NULL: not wanted)
+//   dot[p][block column]: b2[e]·dY over its columns (b2 NULL: not wanted).
+constexpr int kSortRows = 64;
+constexpr int kSortCols = 512;
+struct SortArgs {
+  const void *X, *dY, *b2;
+  int64_t ldx, lddy;
+  void *Xs, *dYs;
+  int64_t ldd, D, T, entries;
+  int E, k;
+  const float* weights;
+  const int32_t *order, *offsets;
+  float *sums, *dot;
+  int64_t ldot;
+};
+hipError_t launch_sort(int dtype, const SortArgs& a, hipStream_t s);
 
 // out[t] = R[t] + Σ_s w[t][s]·O[place[t][s]] (w NULL: 1; R NULL: 0), s ascending.
 struct CombineArgs {
@@ -76,28 +89,10 @@ struct CombineArgs {
 };
 hipError_t launch_combine(int dtype, const CombineArgs& a, hipStream_t s);
 
-// part[chunk of kSumRows rows][D]: Σ w[order[p]]·rows[p] over the chunk's rows;
-// chunks counted per group.
-constexpr int kSumRows = 64;
-hipError_t launch_weighted_sums(int dtype, const void* rows, int64_t ld, int64_t D,
-                                const float* weights, const int32_t* order, int64_t entries,
-                                const int32_t* offsets, int E, float* part, hipStream_t s);
-
-// dweights[entry] = Σ of the ldot values at dot[place] (+ b2[e]·rows[place]), 0
-// for an entry without a place.
-struct WeightGradArgs {
-  int64_t entries, D;
-  int E;
-  const float* dot;
-  int64_t ldot;
-  const int32_t* place;
-  const int32_t* offsets;
-  const void* rows;   // dY of the sorted entries
-  int64_t ld;
-  const void* b2;     // or NULL
-  float* dweights;
-};
-hipError_t launch_weight_grad(int dtype, const WeightGradArgs& a, hipStream_t s);
+// dweights[entry] = Σ of the n values at dot[place], 0 for an entry without a place.
+hipError_t launch_weight_grad(const float* dot, int64_t ldot, int64_t n, const int32_t* place,
+                              const int32_t* offsets, int E, int64_t entries, float* dweights,
+                              hipStream_t s);
 
 // Routing (gt_route): launches and scratch.
 int64_t route_scratch(int64_t T, int E, int k, int groups);

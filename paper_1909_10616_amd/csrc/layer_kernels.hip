@@ -232,35 +232,90 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* part, int64_t r
   }
 }
 
-// ---- sorted copies of rows
+// ---- sorted copies of rows, and what else dY's rows give
 
-// One wavefront a row, a 16-byte chunk a lane (WIDE: of the source too).
+// 256 threads: a block of rows of one group, a 16-byte chunk of columns a lane, a wavefront
+// every fourth row, four of its rows at a time. Bound by memory. (WIDE: X and dY, and
+// b2, take 16-byte loads.)
 template <typename T, bool WIDE>
-__global__ __launch_bounds__(256) void gather_kernel(const T* a, int64_t lda, T* da, const T* b,
-                                                     int64_t ldb, T* db, int64_t ldd, int64_t cols,
-                                                     const int32_t* order, const int32_t* offsets,
-                                                     int E, int64_t entries, int k, int64_t tokens) {
-  constexpr int VEC = 16 / sizeof(T);
-  const int lane = threadIdx.x & 63;
-  const int64_t rows = clamp_offset(offsets[E], entries);
-  // (rows of ldd elements: zero beyond the columns)
-  const T* src = blockIdx.y == 0 ? a : b;
-  const int64_t lds = blockIdx.y == 0 ? lda : ldb;
-  T* dst = blockIdx.y == 0 ? da : db;
-  if (!src || !dst) return;
-  for (int64_t p = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); p < rows;
-       p += static_cast<int64_t>(gridDim.x) * 4) {
-    const int32_t entry = order[p];
-    const int64_t t = entry < 0 ? tokens : entry / k;
-    for (int64_t c = static_cast<int64_t>(lane) * VEC; c < ldd; c += 64 * VEC) {
-      u32x4 v{};
-      if (t < tokens) {
-        if constexpr (WIDE)
-          v = *reinterpret_cast<const u32x4*>(src + t * lds + c);
-        else
-          v = load_chunk<T, VEC>(src + t * lds + c, cols - c);
+__global__ __launch_bounds__(256) void sort_kernel(const SortArgs a) {
+  constexpr int VEC = 16 / sizeof(T), U = 4;
+  __shared__ float part[4][64 * VEC];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  ProductArgs g{};
+  g.offsets = a.offsets;
+  g.groups = a.E;
+  g.M = a.entries;
+  int64_t first;
+  const Span sp = group_of_tile<kSortRows>(g, static_cast<int>(blockIdx.x), &first);
+  if (sp.group < 0) return;
+  const int64_t end = first + kSortRows < sp.hi ? first + kSortRows : sp.hi;
+  const int64_t c0 = static_cast<int64_t>(blockIdx.y) * kSortCols;
+  const int64_t c1 = c0 + kSortCols < a.ldd ? c0 + kSortCols : a.ldd;
+  auto chunk = [&](const void* p, int64_t ld, int64_t row, int64_t c) __attribute__((always_inline)) {
+    const T* q = static_cast<const T*>(p) + row * ld + c;
+    if constexpr (WIDE) return *reinterpret_cast<const u32x4*>(q);
+    return load_chunk<T, VEC>(q, a.D - c);
+  };
+  for (int64_t cb = c0; cb < c1; cb += 64 * VEC) {   // (once in bf16, twice in fp32)
+    const int64_t c = cb + lane * VEC;
+    const bool in = c < c1;
+    float sum[VEC] = {}, b2[VEC] = {};
+    if (a.b2 && in) {
+      const u32x4 b = chunk(a.b2, a.D, sp.group, c);
+      T e[VEC];
+      __builtin_memcpy(e, &b, 16);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) b2[j] = to_float(e[j]);
+    }
+    for (int64_t p0 = first + wave; p0 < end; p0 += 4 * U) {
+      u32x4 x[U], y[U];
+      float w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t p = p0 + 4 * u;
+        x[u] = y[u] = u32x4{};
+        w[u] = 0.0f;
+        if (p >= end) continue;
+        const int entry = a.order[p];
+        const int64_t t = entry < 0 ? a.T : entry / a.k;
+        if (t >= a.T || !in) continue;
+        if (a.sums) w[u] = a.weights[entry];
+        y[u] = chunk(a.dY, a.lddy, t, c);
+        if (a.X) x[u] = chunk(a.X, a.ldx, t, c);
       }
-      *reinterpret_cast<u32x4*>(dst + p * ldd + c) = v;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t p = p0 + 4 * u;
+        if (p >= end) continue;
+        if (in) {
+          *reinterpret_cast<u32x4*>(static_cast<T*>(a.dYs) + p * a.ldd + c) = y[u];
+          if (a.X) *reinterpret_cast<u32x4*>(static_cast<T*>(a.Xs) + p * a.ldd + c) = x[u];
+        }
+        T e[VEC];
+        __builtin_memcpy(e, &y[u], 16);
+        float dot = 0.0f;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const float v = to_float(e[j]);
+          sum[j] = fmaf(w[u], v, sum[j]);
+          dot = fmaf(b2[j], v, dot);
+        }
+        if (a.b2) {
+#pragma unroll
+          for (int d = 1; d < 64; d <<= 1) dot += __shfl_xor(dot, d);
+          if (lane == 0) a.dot[p * a.ldot + cb / (64 * VEC)] = dot;
+        }
+      }
+    }
+    if (a.sums) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) part[wave][lane * VEC + j] = sum[j];
+      __syncthreads();
+      for (int i = threadIdx.x; i < 64 * VEC; i += 256)
+        if (cb + i < a.D && cb + i < c1)
+          a.sums[blockIdx.x * a.D + cb + i] = (part[0][i] + part[1][i]) + (part[2][i] + part[3][i]);
+      __syncthreads();
     }
   }
 }
@@ -323,63 +378,21 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
   }
 }
 
-// ---- weighted column sums of the experts' rows
-
-// 256 threads: 64 quads of columns, kSumRows rows, a quarter of them a thread.
-template <typename T>
-__global__ __launch_bounds__(256) void weighted_sums_kernel(const T* rows, int64_t ld, int64_t D,
-                                                            const float* weights,
-                                                            const int32_t* order, int64_t entries,
-                                                            const int32_t* offsets, ProductArgs a,
-                                                            float* part) {
-  __shared__ f32x4 sums[4][64];
-  int64_t first;
-  const Span sp = group_of_tile<kSumRows>(a, static_cast<int>(blockIdx.x), &first);
-  if (sp.group < 0) return;
-  const int q = threadIdx.x & 63, quarter = threadIdx.x >> 6;
-  const int64_t n = (static_cast<int64_t>(blockIdx.y) * 64 + q) * 4;
-  const int left = D - n < 4 ? static_cast<int>(D - n) : 4;
-  f32x4 s{};
-  if (left > 0)
-    for (int r = quarter; r < kSumRows; r += 4) {
-      const int64_t p = first + r;
-      if (p >= sp.hi) break;
-      const int64_t entry = order[p];
-      const float w = entry >= 0 && entry < entries ? weights[entry] : 0.0f;
-      const f32x4 v = load4(rows + p * ld + n, left, true);   // (our own rows: whole quads, aligned)
-      s += v * w;
-    }
-  sums[quarter][q] = s;
-  __syncthreads();
-  if (quarter != 0) return;
-  const f32x4 t = (sums[0][q] + sums[1][q]) + (sums[2][q] + sums[3][q]);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (i < left) part[blockIdx.x * D + n + i] = t[i];
-}
-
 // ---- the gradient of the routing weights
 
-// One wavefront an entry.
-template <typename T>
-__global__ __launch_bounds__(256) void weight_grad_kernel(const WeightGradArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (i >= a.entries) return;
-  const int64_t p = a.place[i];
+__global__ __launch_bounds__(256) void weight_grad_kernel(const float* dot, int64_t ldot, int64_t n,
+                                                          const int32_t* place,
+                                                          const int32_t* offsets, int E,
+                                                          int64_t entries, float* dweights) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= entries) return;
+  const int64_t p = place[i];
   float s = 0.0f;
-  if (p >= 0 && p < clamp_offset(a.offsets[a.E], a.entries)) {
-    for (int64_t j = lane; j < a.ldot; j += 64) s += a.dot[p * a.ldot + j];
-    if (a.b2) {
-      const int e = group_of_row(a.offsets, a.E, p);
-      const T* b = static_cast<const T*>(a.b2) + e * a.D;
-      const T* y = static_cast<const T*>(a.rows) + p * a.ld;
-      for (int64_t n = lane; n < a.D; n += 64) s = fmaf(to_float(b[n]), to_float(y[n]), s);
-    }
+  if (p >= 0 && p < clamp_offset(offsets[E], entries)) {
+#pragma unroll 4
+    for (int64_t j = 0; j < n; ++j) s += dot[p * ldot + j];
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d);
-  if (lane == 0) a.dweights[i] = s;
+  dweights[i] = s;
 }
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -435,31 +448,24 @@ hipError_t launch_join(const float* part, int64_t rows, int64_t wide, const int3
   return hipGetLastError();
 }
 
-hipError_t launch_gather(int dtype, const void* a, int64_t lda, void* da, const void* b, int64_t ldb,
-                         void* db, int64_t ldd, int64_t cols, const int32_t* order,
-                         const int32_t* offsets, int E, int64_t entries, int k, int64_t T,
-                         hipStream_t s) {
-  if (entries == 0) return hipSuccess;
+hipError_t launch_sort(int dtype, const SortArgs& a, hipStream_t s) {
+  if (a.entries == 0) return hipSuccess;
   const int64_t vec = dtype == GT_BF16 ? 8 : 4;
-  const bool wide = cols % vec == 0 && (!a || (lda % vec == 0 && aligned(a, 16))) &&
-                    (!b || (ldb % vec == 0 && aligned(b, 16))) && ldd % vec == 0;
-  const dim3 grid(blocks_for(entries, 4), 2);
-#define GT_GATHER(T_, V_)                                                                          \
-  gather_kernel<T_, V_><<<grid, 256, 0, s>>>(static_cast<const T_*>(a), lda, static_cast<T_*>(da), \
-                                             static_cast<const T_*>(b), ldb, static_cast<T_*>(db), \
-                                             ldd, cols, order, offsets, E, entries, k, T)
+  const bool wide = a.D % vec == 0 && (!a.X || (a.ldx % vec == 0 && aligned(a.X, 16))) &&
+                    a.lddy % vec == 0 && aligned(a.dY, 16) && (!a.b2 || aligned(a.b2, 16));
+  const dim3 grid(static_cast<unsigned>(a.entries / kSortRows + std::min<int64_t>(a.E, a.entries)),
+                  static_cast<unsigned>((a.ldd + kSortCols - 1) / kSortCols));
   if (dtype == GT_BF16) {
     if (wide)
-      GT_GATHER(uint16_t, true);
+      sort_kernel<uint16_t, true><<<grid, 256, 0, s>>>(a);
     else
-      GT_GATHER(uint16_t, false);
+      sort_kernel<uint16_t, false><<<grid, 256, 0, s>>>(a);
   } else {
     if (wide)
-      GT_GATHER(float, true);
+      sort_kernel<float, true><<<grid, 256, 0, s>>>(a);
     else
-      GT_GATHER(float, false);
+      sort_kernel<float, false><<<grid, 256, 0, s>>>(a);
   }
-#undef GT_GATHER
   return hipGetLastError();
 }
 
@@ -482,32 +488,12 @@ hipError_t launch_combine(int dtype, const CombineArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_weighted_sums(int dtype, const void* rows, int64_t ld, int64_t D,
-                                const float* weights, const int32_t* order, int64_t entries,
-                                const int32_t* offsets, int E, float* part, hipStream_t s) {
+hipError_t launch_weight_grad(const float* dot, int64_t ldot, int64_t n, const int32_t* place,
+                              const int32_t* offsets, int E, int64_t entries, float* dweights,
+                              hipStream_t s) {
   if (entries == 0) return hipSuccess;
-  ProductArgs a{};
-  a.offsets = offsets;
-  a.groups = E;
-  a.M = entries;
-  const dim3 grid(static_cast<unsigned>(entries / kSumRows + std::min<int64_t>(E, entries)),
-                  static_cast<unsigned>((D + 255) / 256));
-  if (dtype == GT_BF16)
-    weighted_sums_kernel<uint16_t><<<grid, 256, 0, s>>>(static_cast<const uint16_t*>(rows), ld, D,
-                                                        weights, order, entries, offsets, a, part);
-  else
-    weighted_sums_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float*>(rows), ld, D, weights,
-                                                     order, entries, offsets, a, part);
-  return hipGetLastError();
-}
-
-hipError_t launch_weight_grad(int dtype, const WeightGradArgs& a, hipStream_t s) {
-  if (a.entries == 0) return hipSuccess;
-  const dim3 grid(static_cast<unsigned>((a.entries + 3) / 4));
-  if (dtype == GT_BF16)
-    weight_grad_kernel<uint16_t><<<grid, 256, 0, s>>>(a);
-  else
-    weight_grad_kernel<float><<<grid, 256, 0, s>>>(a);
+  weight_grad_kernel<<<static_cast<unsigned>((entries + 255) / 256), 256, 0, s>>>(
+      dot, ldot, n, place, offsets, E, entries, dweights);
   return hipGetLastError();
 }
 

@@ -553,7 +553,7 @@ int experts_grad_checks(const gt_experts_grad_args* a, bool pointers) {
 }
 
 struct ExpertsGrad {
-  int64_t R, wide, ldd, ldp, ldh, ldo;
+  int64_t R, wide, ldd, ldp, ldh, ldo, ndot = 0, nb2 = 0;
   Product dh, dw2, dx, dw1;
   void *Xs = nullptr, *dYs = nullptr, *dP = nullptr, *Hw = nullptr, *rest = nullptr;
   float *dXs = nullptr, *dot = nullptr, *colsum = nullptr, *sums = nullptr;
@@ -614,7 +614,10 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     e.vec = width(q.H, {{q.P, q.ldp}, {g.dP, g.ldp}, {g.Hw, g.ldh}}, sz);
     choose(&g.dh, false);
     const TileShape& t = kTile[g.dh.tile];
-    e.ldot = static_cast<int64_t>(a.tilesN) * t.NWN;
+    // Σ dH·H of a row's tiles, then b2·dY of its columns' blocks
+    g.ndot = static_cast<int64_t>(a.tilesN) * t.NWN;
+    g.nb2 = q.b2 && q.dweights ? (g.ldd + 64 * vec - 1) / (64 * vec) : 0;
+    e.ldot = g.ndot + g.nb2;
     g.dot = e.dot = s.take<float>(g.R * e.ldot * 4);
     if (q.db1) g.colsum = e.colsum = s.take<float>(static_cast<int64_t>(a.tilesM) * t.NWM * g.wide * 4);
   }
@@ -663,7 +666,7 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
   }
   const int64_t rest = std::max({g.dh.scratch(), g.dw2.scratch(), g.dx.scratch(), g.dw1.scratch()});
   if (rest) g.rest = s.take(rest);
-  if (q.db2) g.sums = s.take<float>((g.R / kSumRows + std::min<int64_t>(q.E, g.R)) * q.D * 4);
+  if (q.db2) g.sums = s.take<float>((g.R / kSortRows + std::min<int64_t>(q.E, g.R)) * q.D * 4);
   g.bytes = s.used;
   return g;
 }
@@ -829,36 +832,39 @@ int gt_experts_backward(const gt_experts_grad_args* a, void* ws, int64_t ws_byte
   const hipStream_t s = static_cast<hipStream_t>(stream);
   ExpertsGrad g = experts_grad(*a, ws);
   GT_CHECK(scratch_ok(ws, ws_bytes, g.bytes));
-  GT_TRY(launch_gather(a->dtype, a->dW1 ? a->X : nullptr, a->ldx, g.Xs, a->dY, a->lddy, g.dYs, g.ldd,
-                       a->D, a->order, a->offsets, a->E, g.R, a->k, a->T, s),
-         "sorting the rows");
+  SortArgs q{};
+  q.X = a->dW1 ? a->X : nullptr;
+  q.dY = a->dY;
+  q.b2 = g.nb2 ? a->b2 : nullptr;
+  q.ldx = a->ldx;
+  q.lddy = a->lddy;
+  q.Xs = g.Xs;
+  q.dYs = g.dYs;
+  q.ldd = g.ldd;
+  q.D = a->D;
+  q.T = a->T;
+  q.entries = g.R;
+  q.E = a->E;
+  q.k = a->k;
+  q.weights = a->weights;
+  q.order = a->order;
+  q.offsets = a->offsets;
+  q.sums = g.sums;
+  q.dot = g.dot ? g.dot + g.ndot : nullptr;
+  q.ldot = g.ndot + g.nb2;
+  GT_TRY(launch_sort(a->dtype, q, s), "sorting the rows");
   if (g.dP) GT_CHECK(run(g.dh, g.rest, s));
   if (a->db1)
     GT_TRY(launch_join(g.colsum, 0, g.wide, a->offsets, a->E, g.R, kTile[g.dh.tile].BM,
                        kTile[g.dh.tile].NWM, a->db1, s),
            "gradient of b1");
-  if (a->db2) {
-    GT_TRY(launch_weighted_sums(a->dtype, g.dYs, g.ldd, a->D, a->weights, a->order, g.R, a->offsets,
-                                a->E, g.sums, s),
+  if (a->db2)
+    GT_TRY(launch_join(g.sums, 0, a->D, a->offsets, a->E, g.R, kSortRows, 1, a->db2, s),
            "gradient of b2");
-    GT_TRY(launch_join(g.sums, 0, a->D, a->offsets, a->E, g.R, kSumRows, 1, a->db2, s),
-           "gradient of b2");
-  }
-  if (a->dweights) {
-    WeightGradArgs w{};
-    w.entries = g.R;
-    w.D = a->D;
-    w.E = a->E;
-    w.dot = g.dot;
-    w.ldot = g.dh.a.e.ldot;
-    w.place = a->place;
-    w.offsets = a->offsets;
-    w.rows = g.dYs;
-    w.ld = g.ldd;
-    w.b2 = a->b2;
-    w.dweights = a->dweights;
-    GT_TRY(launch_weight_grad(a->dtype, w, s), "gradient of the weights");
-  }
+  if (a->dweights)
+    GT_TRY(launch_weight_grad(g.dot, g.ndot + g.nb2, g.ndot + g.nb2, a->place, a->offsets, a->E, g.R,
+                              a->dweights, s),
+           "gradient of the weights");
   if (a->dW2) GT_CHECK(run(g.dw2, g.rest, s));
   if (a->dX) {
     GT_CHECK(run(g.dx, g.rest, s));

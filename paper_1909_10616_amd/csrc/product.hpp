@@ -84,6 +84,21 @@ __device__ __forceinline__ int64_t offset_at(const ProductArgs& a, int g, int64_
   return v < 0 ? 0 : v > most ? most : v;
 }
 
+// Tile rows of BM rows of all groups.
+template <int BM>
+__device__ __forceinline__ int group_tiles(const ProductArgs& a) {
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+  for (int g = lane; g < a.groups; g += 64) {
+    const int lo = static_cast<int>(offset_at(a, g, a.M));
+    const int hi = static_cast<int>(offset_at(a, g + 1, a.M));
+    n += hi > lo ? (hi - lo + BM - 1) / BM : 0;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
+  return uni(n);
+}
+
 // The group whose tiles of BM rows hold tile row t, counted over all groups, and
 // *first, the first row of that tile. One wavefront-wide prefix sum per 64 groups.
 template <int BM>
@@ -513,15 +528,19 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   const int wm = wave % NWM, wn = wave / NWM;
   const int lI = lane % I, grp = lane / I;
 
-  // ---- which tile: XCD-contiguous runs, in groups of 4 tile rows
+  // ---- which tile: XCD-contiguous runs, in groups of 4 tile rows. With groups along m the
+  // launch has tiles for every way the rows may be spread; those past the last row's
+  // end here, and the others are dealt out to the XCDs without them.
   int tm, tn;
   {
-    const int nt = a.tilesM * a.tilesN;
-    int t = static_cast<int>(blockIdx.x);
+    int t = static_cast<int>(blockIdx.x), rows = a.tilesM;
+    if (a.groups > 0 && !a.along_k) rows = min(rows, group_tiles<BM>(a));
+    const int nt = rows * a.tilesN;
+    if (t >= nt) return;
     const int q = nt >> 3, r = nt & 7, x = t & 7;
     t = x * q + min(x, r) + (t >> 3);
     constexpr int ROWS = 4;
-    const int per = ROWS * a.tilesN, run = t / per, f = run * ROWS, gs = min(a.tilesM - f, ROWS);
+    const int per = ROWS * a.tilesN, run = t / per, f = run * ROWS, gs = min(rows - f, ROWS);
     const int in = t - run * per;
     tm = f + in % gs;
     tn = in / gs;

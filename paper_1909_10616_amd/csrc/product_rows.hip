@@ -20,17 +20,18 @@ namespace gt {
 namespace {
 
 constexpr int kRowWaves = 16;
+constexpr int kRowCols = 64;
 
-// AL: W's rows are 16-byte aligned and whole chunks: loads by descriptor, zero beyond a
-// wavefront's rows.
-template <int DT, int MR, bool G, bool AL>
+// AL: W's rows are 16-byte aligned and whole chunks: loads by descriptor, zero beyond W.
+template <int DT, int MR, bool G, bool AL, int CW>
 __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const ProductArgs a) {
   using T = typename Elem<DT>::T;
   constexpr int VEC = Elem<DT>::VEC;
-  constexpr int CL = 64 / VEC;          // lanes a row of 64 columns
+  constexpr int CL = CW / VEC;          // lanes a row of CW columns
   constexpr int KL = 64 / CL;           // rows of W a load
   constexpr int H = G ? 2 : 1;
-  constexpr int U = !AL ? 2 : G ? 4 : 8;   // loads of a half in flight, and as many being used
+  // loads of a half in flight, and as many being used
+  constexpr int U = !AL || H * MR == 8 ? 2 : G ? 4 : 8;
   extern __shared__ float lds[];        // X: [MR][K], then the wavefronts' sums
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
   int64_t m0 = static_cast<int64_t>(blockIdx.y) * MR, mend = a.M;
@@ -41,18 +42,17 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const ProductArgs 
     group = s.group;
     mend = s.hi;
   }
-  const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 64, n = n0 + lane % CL * VEC;
+  const int64_t n0 = static_cast<int64_t>(blockIdx.x) * CW, n = n0 + lane % CL * VEC;
   const int K = static_cast<int>(a.K);
   const T* W = static_cast<const T*>(a.B) + group * a.sB + n;
   const int valid = a.N - n >= VEC ? VEC : a.N > n ? static_cast<int>(a.N - n) : 0;
-  // a wavefront's rows of W: whole loads
-  const int each = (K + KL * kRowWaves - 1) / (KL * kRowWaves) * KL;
-  const int k0 = wave * each, k1 = min(K, k0 + each);
+  // the wavefronts take turns of U loads, so that the workgroup reads one run of rows
+  constexpr int STEP = U * KL * kRowWaves;
+  const int k0 = wave * U * KL;
 
   u32x4 w[H][U];
-  const T* first = static_cast<const T*>(a.B) + group * a.sB + n0 + static_cast<int64_t>(k0) * a.ldb;
-  const int64_t bytes =
-      k1 > k0 ? (static_cast<int64_t>(k1 - k0 - 1) * a.ldb + H * a.N - n0) * static_cast<int64_t>(sizeof(T)) : 0;
+  const T* first = static_cast<const T*>(a.B) + group * a.sB + n0;
+  const int64_t bytes = (static_cast<int64_t>(K - 1) * a.ldb + H * a.N - n0) * static_cast<int64_t>(sizeof(T));
   const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
       reinterpret_cast<void*>(uniform_ptr(first)), 0, uni(static_cast<int>(bytes < kReach ? bytes : kReach)), 0x00020000);
   const uint32_t ldb = static_cast<uint32_t>(a.ldb) * sizeof(T);
@@ -65,11 +65,11 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const ProductArgs 
         if constexpr (AL) {
           w[h][u] = __builtin_bit_cast(
               u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                         rsrc, lane0 + static_cast<uint32_t>(k - k0 + u * KL) * ldb +
+                         rsrc, lane0 + static_cast<uint32_t>(k + u * KL) * ldb +
                                    h * static_cast<uint32_t>(a.N) * sizeof(T), 0, 0));
         } else {
           const int row = k + u * KL + lane / CL;
-          w[h][u] = load_chunk<T, VEC>(W + static_cast<int64_t>(row) * a.ldb + h * a.N, row < k1 ? valid : 0);
+          w[h][u] = load_chunk<T, VEC>(W + static_cast<int64_t>(row) * a.ldb + h * a.N, row < K ? valid : 0);
         }
       }
     }
@@ -92,16 +92,16 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const ProductArgs 
   }
   __syncthreads();
   float acc[H][MR][VEC] = {};
-  for (int k = k0; k < k1; k += U * KL) {
+  for (int k = k0; k < K; k += STEP) {
     u32x4 v[H][U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int h = 0; h < H; ++h) v[h][u] = w[h][u];
-    if (k + U * KL < k1) load(k + U * KL);
+    if (k + STEP < K) load(k + STEP);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int row = min(k + u * KL + lane / CL, K - 1);   // (past the end: W is zero there)
+      const int row = min(k + u * KL + lane / CL, K - 1);   // (past the end: W is zero)
       float x[MR];
 #pragma unroll
       for (int m = 0; m < MR; ++m) x[m] = lds[m * K + row];
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const ProductArgs 
 #pragma unroll
         for (int d = CL; d < 64; d <<= 1) acc[h][m][c] += __shfl_xor(acc[h][m][c], d);
   __syncthreads();
-  // [wavefront][half][row][64]
+  // [wavefront][half][row][CW]
   if (lane < CL) {
 #pragma unroll
     for (int h = 0; h < H; ++h)
@@ -136,20 +136,21 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const ProductArgs 
       for (int m = 0; m < MR; ++m)
 #pragma unroll
         for (int c = 0; c < VEC; c += 4)
-          *reinterpret_cast<f32x4*>(lds + ((wave * H + h) * MR + m) * 64 + lane * VEC + c) =
+          *reinterpret_cast<f32x4*>(lds + ((wave * H + h) * MR + m) * CW + lane * VEC + c) =
               f32x4{acc[h][m][c], acc[h][m][c + 1], acc[h][m][c + 2], acc[h][m][c + 3]};
   }
   __syncthreads();
   const int i = threadIdx.x;
-  if (i >= MR * 16) return;
-  const int m = i / 16, q = i % 16;
+  constexpr int QN = CW / 4;
+  if (i >= MR * QN) return;
+  const int m = i / QN, q = i % QN;
   const int64_t row = m0 + m, col = n0 + q * 4;
   if (row >= mend || col >= written<T>(a.e, a.N)) return;
   f32x4 v{}, u{};
 #pragma unroll 4
   for (int s = 0; s < kRowWaves; ++s) {
-    v += *reinterpret_cast<const f32x4*>(lds + (s * H * MR + m) * 64 + q * 4);
-    if constexpr (G) u += *reinterpret_cast<const f32x4*>(lds + ((s * H + 1) * MR + m) * 64 + q * 4);
+    v += *reinterpret_cast<const f32x4*>(lds + (s * H * MR + m) * CW + q * 4);
+    if constexpr (G) u += *reinterpret_cast<const f32x4*>(lds + ((s * H + 1) * MR + m) * CW + q * 4);
   }
   const int left = a.N - col < 4 ? static_cast<int>(a.N - col) : 4;
   const f32x4 bv = bias_quad<T>(a.e, col, group, left);
@@ -162,13 +163,13 @@ template <int DT, int MR, bool G, bool AL>
 hipError_t rows_by(const ProductArgs& a, hipStream_t s) {
   const size_t lds = static_cast<size_t>(rows_lds(a.K, MR, G));
   if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(rows_kernel<DT, MR, G, AL>),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(rows_kernel<DT, MR, G, AL, kRowCols>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize,
                                              static_cast<int>(lds));
     if (e != hipSuccess) return e;
   }
   const dim3 grid(static_cast<unsigned>(a.tilesN), static_cast<unsigned>(a.tilesM));
-  rows_kernel<DT, MR, G, AL><<<grid, 64 * kRowWaves, lds, s>>>(a);
+  rows_kernel<DT, MR, G, AL, kRowCols><<<grid, 64 * kRowWaves, lds, s>>>(a);
   return hipGetLastError();
 }
 
@@ -178,7 +179,7 @@ hipError_t rows_of(const ProductArgs& a, hipStream_t s) {
   const bool g = a.e.epi == kEpiGated;
   const bool al = a.N % VEC == 0 && a.ldb % VEC == 0 && a.sB % VEC == 0 &&
                   reinterpret_cast<uintptr_t>(a.B) % 16 == 0 &&
-                  (a.K / kRowWaves + 64) * a.ldb * static_cast<int64_t>(sizeof(typename Elem<DT>::T)) < kReach;
+                  (a.K + 1024) * a.ldb * static_cast<int64_t>(sizeof(typename Elem<DT>::T)) < kReach;
   if (g) return al ? rows_by<DT, MR, true, true>(a, s) : rows_by<DT, MR, true, false>(a, s);
   return al ? rows_by<DT, MR, false, true>(a, s) : rows_by<DT, MR, false, false>(a, s);
 }
