@@ -85,6 +85,47 @@ __global__ __launch_bounds__(256) void reduce_kernel(const ProductArgs a) {
   }
 }
 
+// The join of the last tiles' slices: 256 threads a quad each of 4 rows of a tile.
+template <typename T>
+__global__ __launch_bounds__(256) void tail_kernel(const ProductArgs a) {
+  constexpr int BM = kTile[0].BM, BN = kTile[0].BN;
+  const bool gated = a.e.epi == kEpiGated;
+  GroupTiles<BM> tiles(a);
+  int rows = a.tilesM;
+  if (a.groups > 0) rows = min(rows, tiles.total());
+  const int nt = rows * a.tilesN;
+  constexpr int BK = kTile[0].KB / static_cast<int>(sizeof(T));
+  const Tail tail = tail_of(nt, static_cast<int>((a.K + BK - 1) / BK));
+  const int at = static_cast<int>(blockIdx.y);
+  if (tail.slices < 2 || at >= tail.left) return;
+  int tm, tn, group = 0;
+  tile_at(tail.full + at, nt, rows, a.tilesN, tm, tn);
+  int64_t m0 = static_cast<int64_t>(tm) * BM, mend = a.M;
+  if (a.groups > 0) {
+    const Span s = tiles.find(tm, &m0);
+    if (s.group < 0) return;
+    group = s.group;
+    mend = s.hi;
+  }
+  const int width = gated ? BN / 2 : BN, quads = width / 4;   // of outputs
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  const int r = i / quads, c = i % quads * 4;
+  const int64_t row = m0 + r, n = static_cast<int64_t>(tn) * width + c;
+  if (r >= BM || row >= mend || n >= written<T>(a.e, a.N)) return;
+  const float* p = a.tail + static_cast<int64_t>(at) * tail.slices * BM * BN + r * BN + c;
+  f32x4 v{}, u{};
+#pragma unroll 4
+  for (int z = 0; z < tail.slices; ++z) {
+    v += *reinterpret_cast<const f32x4*>(p + static_cast<int64_t>(z) * BM * BN);
+    if (gated) u += *reinterpret_cast<const f32x4*>(p + static_cast<int64_t>(z) * BM * BN + BN / 2);
+  }
+  const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
+  const f32x4 bv = bias_quad<T>(a.e, n, group, left);
+  const f32x4 bu = gated ? bias_quad<T>(a.e, n + a.N, group, left) : f32x4{};
+  linear_quad<T>(a.e, a.N, row, n, group, left, gated, v, u, bv, bu,
+                 residual_quad<T>(a.e, row, n, left));
+}
+
 // ---- the activation's gradient
 
 // 256 threads: 64 column quads (octets, WIDE), kActRows rows, four of them a thread: all its
@@ -247,7 +288,7 @@ __global__ __launch_bounds__(256) void sort_kernel(const SortArgs a) {
   g.groups = a.E;
   g.M = a.entries;
   int64_t first;
-  const Span sp = group_of_tile<kSortRows>(g, static_cast<int>(blockIdx.x), &first);
+  const Span sp = GroupTiles<kSortRows>(g).find(static_cast<int>(blockIdx.x), &first);
   if (sp.group < 0) return;
   const int64_t end = first + kSortRows < sp.hi ? first + kSortRows : sp.hi;
   const int64_t c0 = static_cast<int64_t>(blockIdx.y) * kSortCols;
@@ -419,6 +460,18 @@ hipError_t launch_reduce(int dtype, const ProductArgs& a, hipStream_t s) {
     reduce_kernel<uint16_t><<<grid, 256, 0, s>>>(a);
   else
     reduce_kernel<float><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_tail(int dtype, const ProductArgs& a, hipStream_t s) {
+  constexpr int BM = kTile[0].BM, BN = kTile[0].BN;
+  const int64_t tiles = static_cast<int64_t>(a.tilesM) * a.tilesN;
+  // (with two slices at least, half the units' number of tiles at most)
+  const dim3 grid(BM * BN / 4 / 256, static_cast<unsigned>(std::min<int64_t>(tiles, kUnits / 2)));
+  if (dtype == GT_BF16)
+    tail_kernel<uint16_t><<<grid, 256, 0, s>>>(a);
+  else
+    tail_kernel<float><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -61,6 +61,7 @@ struct Product {
   int rows = 0;           // > 0: the kernel for a few rows, so many a workgroup
   PadJobs pad{};          // operands copied to aligned rows first …
   int64_t pad_a = 0, pad_b = 0, part = 0;   // … and the bytes of that and of partial sums
+  bool tails = false;     // `part` is the last tiles'
 
   int64_t scratch() const { return up(pad_a, 256) + up(pad_b, 256) + up(part, 256); }
 };
@@ -150,6 +151,7 @@ void choose(Product* p, bool may_split) {
                            ax ? 64 : a.gather ? a.a_rows : 256, p->own_a, sz);
   const Stored sb = stored(a.B, a.ldb, a.sB, bgroups, bx ? a.K : a.N, bx ? wide : a.K,
                            bx && gated ? a.N : 0, bx ? 64 : 256, p->own_b, sz);
+  const bool may_tail = !a.along_k && a.e.epi != kEpiSlope;
   const bool copies = (!sa.ok && sa.bytes > 0) || (!sb.ok && sb.bytes > 0);
   const bool can_dma = (sa.ok || sa.bytes >= 0) && (sb.ok || sb.bytes >= 0);
   const int64_t stages = std::max<int64_t>(1, ((a.along_k ? a.K / std::max(1, a.groups) : a.K) + bk - 1) / bk);
@@ -181,10 +183,23 @@ void choose(Product* p, bool may_split) {
         double cost = copy + std::max(each * std::max(c.alone, c.shared * queue), memory) +
                       c.fixed * ((queue + c.resident - 1) / c.resident);
         if (z > 1) cost += 4.5 + 2.0 * z * a.M * wide * 4 / 6.0e6;
+        bool tails = false;
+        if (t == 0 && z == 1 && may_tail && tiles < kMaxExtent) {   // the last tiles in slices
+          const Tail tail = tail_of(static_cast<int>(tiles), static_cast<int>(stages));
+          const double cut = copy + c.shared * (stages * (tail.full / kUnits) +
+                                                (stages + tail.slices - 1) / tail.slices) +
+                             c.fixed * (tail.full / kUnits + 1) + 5.0 +
+                             2.0 * tail.left * tail.slices * s.BM * s.BN * 4 / 6.0e6;
+          if (tail.slices > 1 && cut < cost) {
+            tails = true;
+            cost = cut;
+          }
+        }
         if (best == 0.0 || cost < best) {
           best = cost;
           p->tile = t;
           p->reg = reg != 0;
+          p->tails = tails;
           a.splits = static_cast<int>(z);
           a.tilesM = static_cast<int>(most);
           a.tilesN = static_cast<int>(tn);
@@ -211,7 +226,9 @@ void choose(Product* p, bool may_split) {
   const TileShape& s = kTile[p->tile];
   const int64_t kb = (p->reg ? 128 : s.KB) / sz, all = (a.K + kb - 1) / kb;
   a.per_slice = static_cast<int>((all + a.splits - 1) / std::max(1, a.splits));
-  p->part = a.splits > 1 ? a.splits * a.M * a.e.ldpart * 4 : 0;
+  p->part = a.splits > 1 ? a.splits * a.M * a.e.ldpart * 4
+            : p->tails   ? static_cast<int64_t>(kUnits) * s.BM * s.BN * 4
+                         : 0;
 }
 
 // Launches a product; ws: its scratch() bytes.
@@ -242,7 +259,9 @@ int run(const Product& p, void* ws, hipStream_t s) {
     GT_TRY(launch_reduce(p.dtype, a, s), "joining the K slices");
     return GT_OK;
   }
+  if (p.tails) a.tail = reinterpret_cast<float*>(at);
   GT_TRY(launch_product(p.dtype, p.layout, p.tile, p.reg, a, s), "layer product");
+  if (p.tails) GT_TRY(launch_tail(p.dtype, a, s), "joining the last tiles");
   return GT_OK;
 }
 

@@ -84,53 +84,79 @@ __device__ __forceinline__ int64_t offset_at(const ProductArgs& a, int g, int64_
   return v < 0 ? 0 : v > most ? most : v;
 }
 
-// Tile rows of BM rows of all groups.
-template <int BM>
-__device__ __forceinline__ int group_tiles(const ProductArgs& a) {
+// The inclusive prefix sum over the wavefront (all lanes active): lane moves within rows of
+// 16, then the rows' totals.
+__device__ __forceinline__ int wave_prefix(int v) {
   const int lane = threadIdx.x & 63;
-  int n = 0;
-  for (int g = lane; g < a.groups; g += 64) {
-    const int lo = static_cast<int>(offset_at(a, g, a.M));
-    const int hi = static_cast<int>(offset_at(a, g + 1, a.M));
-    n += hi > lo ? (hi - lo + BM - 1) / BM : 0;
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
-  return uni(n);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);   // from 1, 2, 4, 8 lanes below
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  const int a = __builtin_amdgcn_readlane(v, 15), b = a + __builtin_amdgcn_readlane(v, 31),
+            c = b + __builtin_amdgcn_readlane(v, 47);
+  return v + (lane >= 48 ? c : lane >= 32 ? b : lane >= 16 ? a : 0);
 }
 
-// The group whose tiles of BM rows hold tile row t, counted over all groups, and
-// *first, the first row of that tile. One wavefront-wide prefix sum per 64 groups.
+// The groups' tiles of BM rows: up to 64 groups a lane each, loaded once; more, 64 at a time.
 template <int BM>
-__device__ __forceinline__ Span group_of_tile(const ProductArgs& a, int t, int64_t* first) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int g0 = 0; g0 < a.groups; g0 += 64) {
-    const int g = g0 + lane;
-    int lo = 0, hi = 0;
+struct GroupTiles {
+  const ProductArgs& a;
+  int lo, hi, mine, upto;   // of group g0 + lane: its rows, its tiles, the tiles up to its last
+  __device__ __forceinline__ explicit GroupTiles(const ProductArgs& args) : a(args) { load(0); }
+  __device__ __forceinline__ void load(int g0) {
+    const int g = g0 + (threadIdx.x & 63);
+    lo = hi = 0;
     if (g < a.groups) {
       lo = static_cast<int>(offset_at(a, g, a.M));
       hi = static_cast<int>(offset_at(a, g + 1, a.M));
     }
-    const int mine = hi > lo ? (hi - lo + BM - 1) / BM : 0;
-    int upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(upto, d);
-      if (lane >= d) upto += o;
-    }
-    const uint64_t past = __ballot(before + upto > t);
-    if (past != 0) {
-      const int at = __builtin_ctzll(past);
-      const int l = __shfl(lo, at), h = __shfl(hi, at);
-      const int tile = t - before - (__shfl(upto, at) - __shfl(mine, at));
-      *first = uni(l) + static_cast<int64_t>(uni(tile)) * BM;
-      return Span{uni(g0 + at), uni(l), uni(h)};
-    }
-    before += __shfl(upto, 63);
+    mine = hi > lo ? (hi - lo + BM - 1) / BM : 0;
+    upto = wave_prefix(mine);
   }
-  *first = 0;
-  return Span{-1, 0, 0};
+  // All groups' tiles.
+  __device__ __forceinline__ int total() {
+    int n = __builtin_amdgcn_readlane(upto, 63);
+    if (a.groups > 64) {
+      for (int g0 = 64; g0 < a.groups; g0 += 64) {
+        load(g0);
+        n += __builtin_amdgcn_readlane(upto, 63);
+      }
+      load(0);
+    }
+    return n;
+  }
+  // The group that holds tile t, counted over all groups, and the tile's first row.
+  __device__ __forceinline__ Span find(int t, int64_t* first) {
+    int before = 0;
+    for (int g0 = 0;;) {
+      const uint64_t past = __ballot(before + upto > t);
+      if (past != 0) {
+        const int at = __builtin_ctzll(past);
+        const int l = __builtin_amdgcn_readlane(lo, at), h = __builtin_amdgcn_readlane(hi, at);
+        const int tile = t - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at));
+        *first = l + static_cast<int64_t>(tile) * BM;
+        return Span{g0 + at, l, h};
+      }
+      before += __builtin_amdgcn_readlane(upto, 63);
+      g0 += 64;
+      if (g0 >= a.groups) break;
+      load(g0);
+    }
+    *first = 0;
+    return Span{-1, 0, 0};
+  }
+};
+
+// Tile t of `tiles` (rows × tilesN) → its row and column: every XCD gets a run of tiles, in
+// groups of 4 tile rows.
+__device__ __forceinline__ void tile_at(int t, int tiles, int rows, int tilesN, int& tm, int& tn) {
+  const int q = tiles >> 3, r = tiles & 7, x = t & 7;
+  t = x * q + min(x, r) + (t >> 3);
+  constexpr int ROWS = 4;
+  const int per = ROWS * tilesN, run = t / per, f = run * ROWS, gs = min(rows - f, ROWS);
+  const int in = t - run * per;
+  tm = f + in % gs;
+  tn = in / gs;
 }
 
 // XOR of the 16-byte chunk index of an XC row k in LDS. bf16: the transposing
@@ -339,6 +365,14 @@ struct EpiRows {
       if (p.row + h + r < p.row_end) *reinterpret_cast<f32x4*>(out + r * e.ldpart) = chunk(r, c);
   }
 
+  // The rows as they are into a tile of BN columns (out: its place of the first).
+  __device__ __forceinline__ void tail(float* out) const {
+    const int c = lane % CH, n = (c < CH / 2 ? 0 : BN / 2 - WN / 2) + c * 4;
+#pragma unroll 1
+    for (int r = lane / CH; r < RP; r += 64 / CH)
+      *reinterpret_cast<f32x4*>(out + r * BN + n) = chunk(r, c);
+  }
+
   // dH arrived: H = act(P) (times up), w the row's weight;
   // dP = w·dH·act'(P) (gated: ·up, and w·dH·act(gate) for up), Hw = w·H.
   // Every lane holds the weight of one row of 64; Q quads of columns a lane, U rows at a
@@ -532,35 +566,43 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   // launch has tiles for every way the rows may be spread; those past the last row's
   // end here, and the others are dealt out to the XCDs without them.
   int tm, tn;
-  {
-    int t = static_cast<int>(blockIdx.x), rows = a.tilesM;
-    if (a.groups > 0 && !a.along_k) rows = min(rows, group_tiles<BM>(a));
-    const int nt = rows * a.tilesN;
-    if (t >= nt) return;
-    const int q = nt >> 3, r = nt & 7, x = t & 7;
-    t = x * q + min(x, r) + (t >> 3);
-    constexpr int ROWS = 4;
-    const int per = ROWS * a.tilesN, run = t / per, f = run * ROWS, gs = min(rows - f, ROWS);
-    const int in = t - run * per;
-    tm = f + in % gs;
-    tn = in / gs;
-  }
-  const int z = static_cast<int>(blockIdx.y);
-  int64_t m0 = static_cast<int64_t>(tm) * BM, mend = a.M;
-  int64_t k0 = 0, kend = a.K;   // reduction range in stored coordinates
+  constexpr bool TAILS = BM == 256 && (EPI == kEpiPlain || EPI == kEpiLinear || EPI == kEpiGated);
+  int slice = 0, slices = 1, tail_at = -1;   // of the last tiles
+  int64_t m0, mend = a.M;
   int group = 0;
-  if (a.groups > 0) {
-    if (a.along_k) {
-      group = static_cast<int>(blockIdx.z);
-      k0 = uni64(offset_at(a, group, a.K));
-      kend = uni64(offset_at(a, group + 1, a.K));
-      if (kend < k0) kend = k0;
-    } else {
-      const Span s = group_of_tile<BM>(a, tm, &m0);
-      if (s.group < 0) return;
+  {
+    const bool grouped = a.groups > 0 && !a.along_k;
+    GroupTiles<BM> tiles(a);
+    int t = static_cast<int>(blockIdx.x), rows = a.tilesM;
+    if (grouped) rows = min(rows, tiles.total());
+    const int nt = rows * a.tilesN;
+    if (TAILS && a.tail) {
+      const Tail tail = tail_of(nt, static_cast<int>((a.K + BK - 1) / BK));
+      if (tail.slices > 1 && t >= tail.full) {
+        const int i = t - tail.full;
+        if (i >= tail.left * tail.slices) return;
+        slice = i / tail.left;
+        slices = tail.slices;
+        tail_at = (i % tail.left) * slices + slice;
+        t = tail.full + i % tail.left;
+      }
+    }
+    if (t >= nt) return;
+    tile_at(t, nt, rows, a.tilesN, tm, tn);
+    m0 = static_cast<int64_t>(tm) * BM;
+    if (grouped) {
+      const Span s = tiles.find(tm, &m0);
       group = s.group;
       mend = s.hi;
     }
+  }
+  const int z = static_cast<int>(blockIdx.y);
+  int64_t k0 = 0, kend = a.K;   // reduction range in stored coordinates
+  if (a.groups > 0 && a.along_k) {
+    group = static_cast<int>(blockIdx.z);
+    k0 = uni64(offset_at(a, group, a.K));
+    kend = uni64(offset_at(a, group + 1, a.K));
+    if (kend < k0) kend = k0;
   }
   // whether the tile's second half holds up values, B's columns N on
   const bool halves = EPI == kEpiGated || (EPI == kEpiPart && BX && !AX && a.e.gated != 0);
@@ -578,6 +620,12 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
     const int all = uni(static_cast<int>((kend - k0 + BK - 1) / BK));
     st0 = EPI == kEpiPart ? min(all, z * a.per_slice) : 0;
     st1 = EPI == kEpiPart ? min(all, st0 + a.per_slice) : all;
+    if constexpr (TAILS) {
+      if (slices > 1) {
+        st0 = all * slice / slices;
+        st1 = all * (slice + 1) / slices;
+      }
+    }
   }
   const int nst = st1 - st0;
   k0 += static_cast<int64_t>(st0) * BK;
@@ -921,7 +969,15 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    EpiRows<DT, EPI, WM, WN, XM, RP, BN>{a, place, h * RP, mine, lane}.run(sums);
+    const EpiRows<DT, EPI, WM, WN, XM, RP, BN> rows{a, place, h * RP, mine, lane};
+    if constexpr (TAILS) {
+      if (tail_at >= 0)
+        rows.tail(a.tail + static_cast<int64_t>(tail_at) * BM * BN + (wm * WM + h * RP) * BN + wn * HN);
+      else
+        rows.run(sums);
+    } else {
+      rows.run(sums);
+    }
     __builtin_amdgcn_wave_barrier();
   }
   if constexpr (EPI == kEpiSlope) {

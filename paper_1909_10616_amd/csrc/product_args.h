@@ -62,8 +62,31 @@ struct ProductArgs {
   int32_t per_slice;    // stages of a slice
   int64_t a_rows;       // rows A has (gather)
   int32_t tilesM, tilesN;
+  float* tail;          // sums of K slices of the last tiles, or null: see Tail
   Epilogue e;
 };
+
+// The tiles that are left when the compute units have had the same number of tiles of 0's
+// size each would keep a few of them busy for as long again. They are cut into K slices
+// instead, as many as the units take at once (at most kTailSlices, and no fewer than 4
+// stages each); their sums go to `tail`, [tile of the left][slice][BM][BN], and a
+// launch of its own joins them. The kernel finds out itself, since with groups
+// the host does not know the tiles.
+constexpr int kUnits = 256;
+constexpr int kTailSlices = 8;
+struct Tail {
+  int full, left, slices;   // whole tiles, tiles in slices, slices of each (1: whole too)
+};
+__host__ __device__ inline Tail tail_of(int tiles, int stages) {
+  Tail t{tiles / kUnits * kUnits, tiles % kUnits, 1};
+  if (t.left > 0) {
+    t.slices = kUnits / t.left;
+    if (t.slices > kTailSlices) t.slices = kTailSlices;
+    if (t.slices > stages / 4) t.slices = stages / 4;
+    if (t.slices < 1) t.slices = 1;
+  }
+  return t;
+}
 
 // How the operands lie: A and B along k or along their own index.
 enum Layout : int { kXW = 0, kPWt = 1, kXtP = 2 };  // KC·XC, KC·KC, XC·XC
@@ -87,6 +110,9 @@ constexpr TileShape kTile[kTiles] = {
 // along k or 1).
 hipError_t launch_product(int dtype, int layout, int tile, bool reg, const ProductArgs& a,
                           hipStream_t s);
+
+// Joins the K slices of the last tiles (a.tail) with the epilogue a.e.epi.
+hipError_t launch_tail(int dtype, const ProductArgs& a, hipStream_t s);
 
 // The product of a few rows (1, 2 or 4 a workgroup; of a group, with groups along m) with a
 // matrix, kXW with kEpiLinear or kEpiGated, in one launch: tilesN of 64 columns, tilesM of

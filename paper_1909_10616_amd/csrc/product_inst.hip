@@ -37,7 +37,8 @@ hipError_t go(const ProductArgs& a, hipStream_t s) {
   constexpr int KB = REG ? 128 : t.KB, NS = REG ? 2 : t.NS;
   constexpr auto* fn = product_kernel<LP_DT, t.I, LP_LAY == kXtP, LP_LAY != kPWt, t.BM, t.BN, t.NWM,
                                       t.NWN, KB, NS, REG, EPI>;
-  const dim3 grid(static_cast<unsigned>(a.tilesM) * static_cast<unsigned>(a.tilesN),
+  const dim3 grid(static_cast<unsigned>(a.tilesM) * static_cast<unsigned>(a.tilesN) +
+                      (a.tail ? kUnits : 0),
                   static_cast<unsigned>(a.splits),
                   a.along_k ? static_cast<unsigned>(a.groups) : 1u);
   static std::atomic<uint64_t> attr{0};

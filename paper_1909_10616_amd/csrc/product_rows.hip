@@ -37,7 +37,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const ProductArgs 
   int64_t m0 = static_cast<int64_t>(blockIdx.y) * MR, mend = a.M;
   int group = 0;
   if (a.groups > 0) {
-    const Span s = group_of_tile<MR>(a, static_cast<int>(blockIdx.y), &m0);
+    const Span s = GroupTiles<MR>(a).find(static_cast<int>(blockIdx.y), &m0);
     if (s.group < 0) return;
     group = s.group;
     mend = s.hi;
