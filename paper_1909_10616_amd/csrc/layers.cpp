@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <string>
 
@@ -114,10 +115,11 @@ int few_rows(const Product& p) {
 
 // What a tile takes a compute unit, in µs: a stage (128 bytes of k) alone and
 // when others share the unit, its launch and epilogue, and how many share it. Fitted to
-// 21 shapes from 1×4096×4096 to 2048×4096×4096 in every layout, each at every tile and 1
-// to 32 K slices (bf16, K = 4096, one slice: 256×256 tiles 76 µs for 16 of them, 114
-// for 256; 128×128 43, 75 for 512; 64×64 28, 114 for 2048; 16×128 22, 221 for 4096).
-// The choice is then within 5 % of the best of them, at most 11 % behind it.
+// 35 shapes from 1×4096×4096 to 2048×4096×4096, 14 of them odd, in every layout and
+// type, each at every tile and 1 to 32 K slices (bf16, K = 4096, one slice:
+// 256×256 tiles 76 µs for 16 of them, 114 for 256; 128×128 43, 75 for 512; 64×64 28, 114
+// for 2048; 16×128 22, 221 for 4096). Of the 204, 173 choices are within 5 % of the best
+// tile and slices measured, the others within 16 % (24 % in odd rows of 2 KB).
 struct TileCost {
   double alone, shared, fixed;
   int resident;
@@ -127,11 +129,17 @@ constexpr TileCost kCost[2][kTiles] = {
     {{1.62, 1.62, 8, 1}, {0.64, 0.55, 4.3, 2}, {0.375, 0.25, 4.2, 3}, {0.28, 0.235, 4.3, 2}}  // bf16
 };
 
+// What a stage of the register path takes, in stages by descriptor loads: bf16 and fp32 by
+// layout (kXW, kPWt, kXtP) and tile (64×64, 16×128), fitted to 14 shapes from
+// 13×1021×777 to 1999×2623×3457. bf16 rows that lie along the reduction's other side
+// are transposed a value at a time.
+constexpr double kReg[2][3][2] = {{{1.4, 2.0}, {1.4, 2.0}, {1.4, 2.0}},
+                                  {{2.5, 4.6}, {1.5, 2.5}, {3.3, 4.6}}};
+
 // Tile, K slices and copies by the time they should take: the stages of the tiles that a
-// compute unit gets (256 of them) or the operands' way from memory, a K slice's partial
-// sums and the launch that joins them, the copies of operands that 16-byte
-// loads do not serve and their launch; the register path takes those as they are, at
-// 2.2 (bf16) and 1.2 times (fp32, bound by its MFMAs) the time of a stage.
+// compute unit gets (256 of them; tiles that share a unit run in rounds) and the operands'
+// way from memory, which overlap in part, a K slice's partial sums and the launch that
+// joins them, the copies of operands that 16-byte loads do not serve and their launch.
 void choose(Product* p, bool may_split) {
   ProductArgs& a = p->a;
   if ((p->rows = few_rows(*p)) > 0) {
@@ -178,10 +186,11 @@ void choose(Product* p, bool may_split) {
       const double copy = !reg && copies ? 5.0 + 2.0 * ((sa.ok ? 0 : sa.bytes) + (sb.ok ? 0 : sb.bytes)) / 5.0e6 : 0.0;
       for (int64_t z = 1; z <= 64; z *= 2) {
         if (z > 1 && (!may_split || stages / z < 4)) break;
-        const double each = static_cast<double>((stages + z - 1) / z) * (!reg ? 1.0 : p->dtype == GT_BF16 ? 2.2 : 1.2);
+        const double each = static_cast<double>((stages + z - 1) / z) * (reg ? kReg[p->dtype == GT_BF16 ? 1 : 0][p->layout][t - 2] : 1.0);
         const int64_t queue = (tiles * z + 255) / 256;
-        double cost = copy + std::max(each * std::max(c.alone, c.shared * queue), memory) +
-                      c.fixed * ((queue + c.resident - 1) / c.resident);
+        const int64_t rounds = (queue + c.resident - 1) / c.resident;
+        const double busy = rounds > 1 ? c.shared * c.resident * rounds : std::max(c.alone, c.shared * queue);
+        double cost = copy + std::hypot(each * busy, memory) + c.fixed * rounds;
         if (z > 1) cost += 4.5 + 2.0 * z * a.M * wide * 4 / 6.0e6;
         bool tails = false;
         if (t == 0 && z == 1 && may_tail && tiles < kMaxExtent) {   // the last tiles in slices
