@@ -85,9 +85,12 @@ __global__ __launch_bounds__(256) void reduce_kernel(const ProductArgs a) {
   }
 }
 
-// The join of the last tiles' slices: 256 threads a quad each of 4 rows of a tile.
-template <typename T>
+// The join of the last tiles' slices (the 256×256 tile, bf16), 256 threads a quad each.
+// Bound by memory and its launch: 14 µs for 64 tiles of 4 slices, in place of a round
+// of tiles of which 64 units were busy (the down product of 16384 rows of
+// 4096 × 2048 in 8 groups: 214 → 159 + 14 µs).
 __global__ __launch_bounds__(256) void tail_kernel(const ProductArgs a) {
+  using T = uint16_t;
   constexpr int BM = kTile[0].BM, BN = kTile[0].BN;
   const bool gated = a.e.epi == kEpiGated;
   GroupTiles<BM> tiles(a);
@@ -463,15 +466,12 @@ hipError_t launch_reduce(int dtype, const ProductArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_tail(int dtype, const ProductArgs& a, hipStream_t s) {
+hipError_t launch_tail(const ProductArgs& a, hipStream_t s) {
   constexpr int BM = kTile[0].BM, BN = kTile[0].BN;
   const int64_t tiles = static_cast<int64_t>(a.tilesM) * a.tilesN;
   // (with two slices at least, half the units' number of tiles at most)
   const dim3 grid(BM * BN / 4 / 256, static_cast<unsigned>(std::min<int64_t>(tiles, kUnits / 2)));
-  if (dtype == GT_BF16)
-    tail_kernel<uint16_t><<<grid, 256, 0, s>>>(a);
-  else
-    tail_kernel<float><<<grid, 256, 0, s>>>(a);
+  tail_kernel<<<grid, 256, 0, s>>>(a);   // (tile 0 is bf16's)
   return hipGetLastError();
 }
 

@@ -122,13 +122,17 @@ struct oct {
   f32x4 a, b;
 };
 template <typename T>
-__device__ __forceinline__ oct load8(const T* p) {
+struct raw8 {   // as they lie in memory
+  u32x4 w[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ oct open8(const raw8<T>& r) {
   oct v;
   if constexpr (sizeof(T) == 4) {
-    v.a = *reinterpret_cast<const f32x4*>(p);
-    v.b = *reinterpret_cast<const f32x4*>(p + 4);
+    v.a = __builtin_bit_cast(f32x4, r.w[0]);
+    v.b = __builtin_bit_cast(f32x4, r.w[1]);
   } else {
-    const u32x4 u = *reinterpret_cast<const u32x4*>(p);
+    const u32x4 u = r.w[0];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       v.a[2 * i] = __builtin_bit_cast(float, u[i] << 16);
@@ -138,6 +142,10 @@ __device__ __forceinline__ oct load8(const T* p) {
     }
   }
   return v;
+}
+template <typename T>
+__device__ __forceinline__ oct load8(const T* p) {
+  return open8<T>(*reinterpret_cast<const raw8<T>*>(p));
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const oct& v) {

@@ -195,10 +195,10 @@ void choose(Product* p, bool may_split) {
         bool tails = false;
         if (t == 0 && z == 1 && may_tail && tiles < kMaxExtent) {   // the last tiles in slices
           const Tail tail = tail_of(static_cast<int>(tiles), static_cast<int>(stages));
-          const double cut = copy + c.shared * (stages * (tail.full / kUnits) +
-                                                (stages + tail.slices - 1) / tail.slices) +
-                             c.fixed * (tail.full / kUnits + 1) + 5.0 +
-                             2.0 * tail.left * tail.slices * s.BM * s.BN * 4 / 6.0e6;
+          const double cut = copy + std::hypot(c.shared * (stages * (tail.full / kUnits) +
+                                                           (stages + tail.slices - 1) / tail.slices), memory) +
+                             c.fixed * (tail.full / kUnits + 1) + 6.0 +
+                             2.0 * tail.left * tail.slices * s.BM * s.BN * 4 / 5.0e6;
           if (tail.slices > 1 && cut < cost) {
             tails = true;
             cost = cut;
@@ -270,7 +270,7 @@ int run(const Product& p, void* ws, hipStream_t s) {
   }
   if (p.tails) a.tail = reinterpret_cast<float*>(at);
   GT_TRY(launch_product(p.dtype, p.layout, p.tile, p.reg, a, s), "layer product");
-  if (p.tails) GT_TRY(launch_tail(p.dtype, a, s), "joining the last tiles");
+  if (p.tails) GT_TRY(launch_tail(a, s), "joining the last tiles");
   return GT_OK;
 }
 

@@ -373,96 +373,147 @@ struct EpiRows {
       *reinterpret_cast<f32x4*>(out + r * BN + n) = chunk(r, c);
   }
 
+  // The weight of one row of RP in each lane.
+  __device__ __forceinline__ float row_weight() const {
+    static_assert(RP <= 64, "a row's weight in each lane");
+    const Epilogue& e = a.e;
+    if (lane >= RP || p.row + h + lane >= p.row_end) return 0.0f;
+    const int64_t entry = e.order[p.row + h + lane];
+    return entry >= 0 && entry < e.entries ? e.weights[entry] : 0.0f;
+  }
+
   // dH arrived: H = act(P) (times up), w the row's weight;
-  // dP = w·dH·act'(P) (gated: ·up, and w·dH·act(gate) for up), Hw = w·H.
-  // Every lane holds the weight of one row of 64; Q quads of columns a lane, U rows at a
-  // time with their pre-activations loaded first.
-  template <bool WHOLE>
+  // dP = w·dH·act'(P) (gated: ·up, and w·dH·act(gate) for up), Hw = w·H. Octets of columns that
+  // all exist, the pre-activations of U rows loaded while the U rows before them are
+  // worked on.
+  template <int ACT>
+  __device__ __forceinline__ void slope_whole(EpiSums* sums) const {
+    const Epilogue& e = a.e;
+    constexpr int LR = CH / 2, STEP = 64 / LR, U = RP / STEP >= 2 ? 2 : 1;
+    const int c = lane % LR * 2, first = lane / LR;
+    const int64_t n = col(c), row0 = p.row + h + first;
+    const int64_t rows = p.row_end - row0;   // of this lane's first on
+    const T* P = static_cast<const T*>(e.P) + row0 * e.ldp + n;
+    T* out = static_cast<T*>(e.Y) + row0 * e.ldy + n;
+    T* hout = static_cast<T*>(e.Hw) + row0 * e.ldh + n;
+    float* dots = e.dot + row0 * e.ldot + p.pcol;
+    raw8<T> gate[U], up[U];
+    auto load = [&](int at) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int r = at + i * STEP;
+        gate[i] = raw8<T>{};
+        up[i] = raw8<T>{};
+        if (r < RP && r < rows) {
+          gate[i] = *reinterpret_cast<const raw8<T>*>(P + r * e.ldp);
+          if (e.gated) up[i] = *reinterpret_cast<const raw8<T>*>(P + r * e.ldp + a.N);
+        }
+      }
+    };
+    load(0);
+    const float mine_w = row_weight();
+#pragma unroll 1
+    for (int at = 0; at < RP; at += U * STEP) {
+      oct g[U], u[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        g[i] = open8<T>(gate[i]);
+        u[i] = e.gated ? open8<T>(up[i]) : oct{f32x4{1.0f, 1.0f, 1.0f, 1.0f}, f32x4{1.0f, 1.0f, 1.0f, 1.0f}};
+      }
+      load(at + U * STEP);
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int r = at + i * STEP;
+        const float w = __shfl(mine_w, first + r);
+        const bool live = r < rows;
+        float dot = 0.0f;
+        oct dg, du, hw;
+        auto quad = [&](const f32x4& v, const f32x4& gq, const f32x4& uq, f32x4& dgq, f32x4& duq,
+                        f32x4& hwq, EpiSums& sum) __attribute__((always_inline)) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float val, sl;
+            act_both(ACT, gq[j], &val, &sl);
+            const float wv = w * v[j], H = val * uq[j];
+            dot += live ? v[j] * H : 0.0f;
+            dgq[j] = live ? wv * uq[j] * sl : 0.0f;
+            duq[j] = live ? wv * val : 0.0f;
+            hwq[j] = w * H;
+          }
+          sum.g += dgq;
+          sum.u += duq;
+        };
+        quad(chunk(first + r, c), g[i].a, u[i].a, dg.a, du.a, hw.a, sums[0]);
+        quad(chunk(first + r, c + 1), g[i].b, u[i].b, dg.b, du.b, hw.b, sums[1]);
+        if (live) {
+          store8(out + r * e.ldy, dg);
+          if (e.gated) store8(out + r * e.ldy + a.N, du);
+          store8(hout + r * e.ldh, hw);
+        }
+#pragma unroll
+        for (int d = 1; d < LR; d <<= 1) dot += __shfl_xor(dot, d);
+        if (c == 0 && live) dots[r * e.ldot] = dot;
+      }
+    }
+  }
+
+  // The same a quad a lane, every column checked; U rows at a time with their
+  // pre-activations loaded first.
   __device__ __forceinline__ void slope(EpiSums* sums) const {
     const Epilogue& e = a.e;
-    constexpr int Q = WHOLE ? 2 : 1, LR = CH / Q, STEP = 64 / LR;
-    constexpr int U = RP / STEP >= 2 ? 2 : 1;
-    static_assert(RP <= 64, "a row's weight in each lane");
-    const int c = lane % LR * Q;
+    constexpr int LR = CH, STEP = 64 / LR, U = RP / STEP >= 2 ? 2 : 1;
+    const int c = lane % LR;
     const int64_t n = col(c);
     const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
     const bool vec = e.vec != 0;
-    float mine_w = 0.0f;
-    if (lane < RP && p.row + h + lane < p.row_end) {
-      const int64_t entry = e.order[p.row + h + lane];
-      if (entry >= 0 && entry < e.entries) mine_w = e.weights[entry];
-    }
+    const float mine_w = row_weight();
 #pragma unroll 1
     for (int r0 = lane / LR; r0 < RP; r0 += U * STEP) {
-      f32x4 gate[U][Q], up[U][Q];
+      f32x4 gate[U], up[U];
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int64_t row = p.row + h + r0 + i * STEP;
         const T* pp = static_cast<const T*>(e.P) + row * e.ldp + n;
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-          gate[i][q] = f32x4{};
-          up[i][q] = f32x4{1.0f, 1.0f, 1.0f, 1.0f};
-        }
-        if (row >= p.row_end || (!WHOLE && left <= 0)) continue;
-        if constexpr (WHOLE) {
-          const oct g = load8(pp);
-          gate[i][0] = g.a;
-          gate[i][Q - 1] = g.b;
-          if (e.gated) {
-            const oct u = load8(pp + a.N);
-            up[i][0] = u.a;
-            up[i][Q - 1] = u.b;
-          }
-        } else {
-          gate[i][0] = load4(pp, left, vec);
-          if (e.gated) up[i][0] = load4(pp + a.N, left, vec);
-        }
+        gate[i] = f32x4{};
+        up[i] = f32x4{1.0f, 1.0f, 1.0f, 1.0f};
+        if (row >= p.row_end || left <= 0) continue;
+        gate[i] = load4(pp, left, vec);
+        if (e.gated) up[i] = load4(pp + a.N, left, vec);
       }
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int r = r0 + i * STEP;
         const int64_t row = p.row + h + r;
         const float w = __shfl(mine_w, r);
-        const bool live = row < p.row_end && (WHOLE || left > 0);
+        const bool live = row < p.row_end && left > 0;
         float dot = 0.0f;
-        f32x4 dg[Q], du[Q], hw[Q];
+        f32x4 dg, du, hw;
+        const f32x4 v = chunk(r, c);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-          const f32x4 v = chunk(r, c + q);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float val, sl;
-            act_both(e.act, gate[i][q][j], &val, &sl);
-            const float wv = w * v[j], H = val * up[i][q][j];
-            const bool in = live && (WHOLE || j < left);
-            dot += in ? v[j] * H : 0.0f;
-            dg[q][j] = in ? wv * up[i][q][j] * sl : 0.0f;
-            du[q][j] = in ? wv * val : 0.0f;
-            hw[q][j] = in ? w * H : 0.0f;
-          }
-          sums[q].g += dg[q];
-          sums[q].u += du[q];
+        for (int j = 0; j < 4; ++j) {
+          float val, sl;
+          act_both(e.act, gate[i][j], &val, &sl);
+          const float wv = w * v[j], H = val * up[i][j];
+          const bool in = live && j < left;
+          dot += in ? v[j] * H : 0.0f;
+          dg[j] = in ? wv * up[i][j] * sl : 0.0f;
+          du[j] = in ? wv * val : 0.0f;
+          hw[j] = in ? w * H : 0.0f;
         }
-        if (live || (row < p.row_end && n < written<T>(e, a.N))) {
+        sums[0].g += dg;
+        sums[0].u += du;
+        if (row < p.row_end && n < written<T>(e, a.N)) {
           T* out = static_cast<T*>(e.Y) + row * e.ldy + n;
-          T* hout = static_cast<T*>(e.Hw) + row * e.ldh + n;
-          if constexpr (WHOLE) {
-            store8(out, oct{dg[0], dg[Q - 1]});
-            if (e.gated) store8(out + a.N, oct{du[0], du[Q - 1]});
-            store8(hout, oct{hw[0], hw[Q - 1]});
-          } else {
-            // (rows padded with zeros: dP's end with the up half when gated)
-            store4(out, dg[0], e.gated ? left : e.zero_pad ? 4 : left, vec);
-            if (e.gated) {
-              store4(out + a.N, du[0], left, vec);
-              constexpr int64_t VEC = 16 / sizeof(T);
-              const int64_t pad = (2 * a.N + VEC - 1) / VEC * VEC - 2 * a.N;
-              if (e.zero_pad && left > 0 && n + left == a.N)
-                for (int64_t z = 0; z < pad; ++z) (out + a.N)[left + z] = T(0);
-            }
-            store4(hout, hw[0], left, vec);
+          // (rows padded with zeros: dP's end with the up half when gated)
+          store4(out, dg, e.gated ? left : e.zero_pad ? 4 : left, vec);
+          if (e.gated) {
+            store4(out + a.N, du, left, vec);
+            constexpr int64_t VEC = 16 / sizeof(T);
+            const int64_t pad = (2 * a.N + VEC - 1) / VEC * VEC - 2 * a.N;
+            if (e.zero_pad && left > 0 && n + left == a.N)
+              for (int64_t z = 0; z < pad; ++z) (out + a.N)[left + z] = T(0);
           }
+          store4(static_cast<T*>(e.Hw) + row * e.ldh + n, hw, left, vec);
         }
 #pragma unroll
         for (int d = 1; d < LR; d <<= 1) dot += __shfl_xor(dot, d);
@@ -476,10 +527,16 @@ struct EpiRows {
     if constexpr (EPI == kEpiPart) {
       part();
     } else if constexpr (EPI == kEpiSlope) {
-      if (whole_slope(a, p))
-        slope<true>(sums);
+      if (!whole_slope(a, p))
+        slope(sums);
+      else if (e.act == GT_ACT_SILU)
+        slope_whole<GT_ACT_SILU>(sums);
+      else if (e.act == GT_ACT_GELU)
+        slope_whole<GT_ACT_GELU>(sums);
+      else if (e.act == GT_ACT_RELU)
+        slope_whole<GT_ACT_RELU>(sums);
       else
-        slope<false>(sums);
+        slope_whole<GT_ACT_NONE>(sums);
     } else {
       const bool all = e.vec == 2 && p.row + WM <= p.row_end &&
                        p.col + (G ? WN / 2 : BN / 2 + WN / 2) <= a.N;

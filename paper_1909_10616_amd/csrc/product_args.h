@@ -112,7 +112,7 @@ hipError_t launch_product(int dtype, int layout, int tile, bool reg, const Produ
                           hipStream_t s);
 
 // Joins the K slices of the last tiles (a.tail) with the epilogue a.e.epi.
-hipError_t launch_tail(int dtype, const ProductArgs& a, hipStream_t s);
+hipError_t launch_tail(const ProductArgs& a, hipStream_t s);
 
 // The product of a few rows (1, 2 or 4 a workgroup; of a group, with groups along m) with a
 // matrix, kXW with kEpiLinear or kEpiGated, in one launch: tilesN of 64 columns, tilesM of
