@@ -39,7 +39,7 @@ def untouched(buf, rows, cols):
 @pytest.mark.parametrize("gated", [False, True])
 def test_linear(L, gated, odd):
     """bias, residual and pre-activations; products below 2^24 and P below 2^8 in bf16."""
-    M, N, K = (4350, 2160 + odd, 1032) if gated else (4250, 4344 + odd, 1032)
+    M, N, K = (4340, 2048 - odd, 1032) if gated else (4340, 4096 - odd, 1032)
     print(f"linear {M} {N} {K} gated {gated}", flush=True)
     gen = torch.Generator().manual_seed(M + odd)
     wide = 2 * N if gated else N
@@ -58,9 +58,9 @@ def test_linear(L, gated, odd):
     untouched(pbuf, M, wide)
 
 
-@pytest.mark.parametrize("K", [4352, 4349])
+@pytest.mark.parametrize("K", [4096, 4091])
 def test_linear_backward(L, K):
-    M, N = 4250, 1040
+    M, N = 4340, 1040
     print(f"linear_backward {M} {N} {K}", flush=True)
     gen = torch.Generator().manual_seed(K)
     dY, W, X = ints(gen, M, N, most=1), ints(gen, K, N, most=1), ints(gen, M, K, most=1)
@@ -71,11 +71,11 @@ def test_linear_backward(L, K):
     untouched(buf, M, K)
 
 
-@pytest.mark.parametrize("D", [4808, 4809])
-def test_experts(L, D):
+@pytest.mark.parametrize("T,k,D,H", [(1700, 2, 4600, 1032), (4000, 1, 4096, 2056), (4000, 1, 4091, 2056)])
+def test_experts(L, T, k, D, H):
     """One-hot tokens, weights of one half and small whole matrices; an expert without rows and
     tokens without experts."""
-    T, E, k, H = 1700, 5, 2, 1032
+    E = 5
     print(f"experts {T} {E} {k} {D} {H}", flush=True)
     gen = torch.Generator().manual_seed(D)
     x = torch.randn(T, E, generator=gen)
