@@ -9,8 +9,9 @@
  *     is asynchronous on `stream` (hipStream_t, NULL = default), keeps nothing
  *     afterwards, and may be captured into a graph.
  *   - Scratch memory is the caller's too: gt_*_workspace gives the bytes a call
- *     with these arguments needs (0: none); `ws` must be 256-byte aligned, and
- *     may be reused by the next call on the same stream. GT_ESMALL if ws_bytes
+ *     with these arguments needs (0: none; the alignment of the pointers counts,
+ *     as does which of the optional ones are null); `ws` must be 256-byte aligned,
+ *     and may be reused by the next call on the same stream. GT_ESMALL if ws_bytes
  *     is less. Its contents need no preparation.
  *   - Matrices are row-major with a leading dimension (`ld*`, elements between
  *     rows, at least the row's length); any extents, alignment and leading
@@ -21,9 +22,10 @@
  *     the same bits. Values are rounded once, where they are stored; the
  *     intermediates stored in the operands' type (dP of the gradients, an expert
  *     layer's activations) are named below.
- *   - GT_EINVAL: a null pointer where one is needed, an unknown enum, a
- *     negative or too large extent, a leading dimension below its row. Nothing
- *     is launched then.
+ *   - GT_EINVAL: a null pointer where one is needed, a pointer not aligned to
+ *     its elements, an unknown enum, a negative extent or one of 2^31 or more, a
+ *     leading dimension below its row, an array of more than 2^45 elements.
+ *     Nothing is launched then.
  */
 #ifndef GEMMTUNE_LAYERS_H
 #define GEMMTUNE_LAYERS_H

@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <exception>
 #include <string>
 
 #include "gemmtune_layers.h"
@@ -16,6 +17,7 @@ namespace gt {
 namespace {
 
 constexpr int64_t kMaxExtent = int64_t{1} << 31;
+constexpr int64_t kMaxElements = int64_t{1} << 45;   // of one array: no size below leaves 64 bits
 
 int fail(const std::string& what) {
   set_error(what);
@@ -38,9 +40,9 @@ bool aligned(const void* p, int64_t n) { return reinterpret_cast<uintptr_t>(p) %
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 // An array inside the caller's scratch, 256-byte aligned.
 struct Scratch {
-  char* base;
+  uintptr_t base;   // (0 in a query)
   int64_t used = 0;
-  explicit Scratch(void* p) : base(static_cast<char*>(p)) {}
+  explicit Scratch(void* p) : base(reinterpret_cast<uintptr_t>(p)) {}
   template <typename T = void>
   T* take(int64_t bytes) {
     const int64_t at = used;
@@ -290,10 +292,18 @@ int extent(int64_t v, int64_t least, const char* name) {
   if (v < least || v >= kMaxExtent) return fail(std::string(name) + " out of range");
   return GT_OK;
 }
-int row(const void* p, int64_t ld, int64_t cols, const char* name) {
-  if (p && ld < cols) return fail(std::string("leading dimension of ") + name + " below its row");
-  if (p && ld >= kMaxExtent) return fail(std::string("leading dimension of ") + name + " too large");
+// A matrix that is there, or has to be (needed): rows of cols, ld apart, of sz-byte elements.
+int matrix(const void* p, bool needed, int64_t ld, int64_t rows, int64_t cols, int64_t sz,
+           const char* name) {
+  if (!p && !needed) return GT_OK;
+  if (ld < cols) return fail(std::string("leading dimension of ") + name + " below its row");
+  if (ld >= kMaxExtent || rows > kMaxElements / ld)
+    return fail(std::string(name) + " is too large");
+  if (!aligned(p, sz)) return fail(std::string(name) + " is not aligned to its elements");
   return GT_OK;
+}
+int vector(const void* p, int64_t sz, const char* name) {
+  return aligned(p, sz) ? GT_OK : fail(std::string(name) + " is not aligned to its elements");
 }
 int scratch_ok(const void* ws, int64_t have, int64_t need) {
   if (need == 0) return GT_OK;
@@ -324,11 +334,13 @@ int linear_checks(const gt_linear_args* a, bool pointers) {
   if (pointers && a->M > 0 && (!a->X || !a->W || !a->Y)) return fail("gt_linear: null X, W or Y");
   if (a->out_dtype != a->dtype && a->R == a->Y && a->R)
     return fail("gt_linear: R may be Y only in the same type");
-  GT_CHECK(row(a->X, a->ldx, a->K, "X"));
-  GT_CHECK(row(a->W, a->ldw, wide, "W"));
-  GT_CHECK(row(a->R, a->ldr, a->N, "R"));
-  GT_CHECK(row(a->Y, a->ldy, a->N, "Y"));
-  return row(a->P, a->ldp, wide, "P");
+  const int64_t sz = size_of(a->dtype);
+  GT_CHECK(matrix(a->X, true, a->ldx, a->M, a->K, sz, "X"));
+  GT_CHECK(matrix(a->W, true, a->ldw, a->K, wide, sz, "W"));
+  GT_CHECK(vector(a->bias, sz, "bias"));
+  GT_CHECK(matrix(a->R, false, a->ldr, a->M, a->N, sz, "R"));
+  GT_CHECK(matrix(a->Y, true, a->ldy, a->M, a->N, size_of(a->out_dtype), "Y"));
+  return matrix(a->P, false, a->ldp, a->M, wide, sz, "P");
 }
 
 Product linear_product(const gt_linear_args& q) {
@@ -378,12 +390,15 @@ int linear_grad_checks(const gt_linear_grad_args* a, bool pointers) {
     if ((a->dX && !a->W) || (a->dW && !a->X))
       return fail("gt_linear_backward: dX needs W, dW needs X");
   }
-  GT_CHECK(row(a->dY, a->lddy, a->N, "dY"));
-  GT_CHECK(row(a->X, a->ldx, a->K, "X"));
-  GT_CHECK(row(a->W, a->ldw, wide, "W"));
-  GT_CHECK(row(a->act != GT_ACT_NONE ? a->P : nullptr, a->ldp, wide, "P"));
-  GT_CHECK(row(a->dX, a->lddx, a->K, "dX"));
-  return row(a->dW, a->lddw, wide, "dW");
+  const int64_t sz = size_of(a->dtype);
+  const bool act = a->act != GT_ACT_NONE;
+  GT_CHECK(matrix(a->dY, true, a->lddy, a->M, a->N, sz, "dY"));
+  GT_CHECK(matrix(a->X, a->dW, a->ldx, a->M, a->K, sz, "X"));
+  GT_CHECK(matrix(a->W, a->dX, a->ldw, a->K, wide, sz, "W"));
+  GT_CHECK(matrix(act ? a->P : nullptr, act, a->ldp, a->M, wide, sz, "P"));
+  GT_CHECK(matrix(a->dX, false, a->lddx, a->M, a->K, sz, "dX"));
+  GT_CHECK(matrix(a->dW, false, a->lddw, a->K, wide, size_of(a->dw_dtype), "dW"));
+  return vector(a->db, 4, "db");
 }
 
 struct LinearGrad {
@@ -458,11 +473,28 @@ LinearGrad linear_grad(const gt_linear_grad_args& q, void* ws) {
 int experts_checks(int64_t T, int64_t D, int64_t H, int E, int k, int dtype, int act) {
   GT_CHECK(extent(T, 0, "T"));
   GT_CHECK(extent(D, 1, "D"));
-  GT_CHECK(extent(act & GT_ACT_GATED ? 2 * H : H, 1, "H"));
+  GT_CHECK(extent(H, 1, "H"));
+  if (act & GT_ACT_GATED) GT_CHECK(extent(2 * H, 1, "2H"));
   if (E < 1 || E > 1024 || k < 1 || k > 64) return fail("experts: E is 1 … 1024, k 1 … 64");
   if (T * k >= kMaxExtent) return fail("experts: T·k out of range");
   if (!dtype_ok(dtype) || !act_ok(act)) return fail("experts: unknown dtype or activation");
+  if (T * k > kMaxElements / std::max(D, 2 * H) || D > kMaxElements / (2 * H) / E)
+    return fail("experts: the rows or the matrices are too large");
   return GT_OK;
+}
+// The experts' matrices (sw apart) and the lists.
+int stack(const void* p, bool needed, int64_t ld, int64_t sw, int64_t rows, int64_t cols, int E,
+          int64_t sz, const char* name) {
+  if (!p && !needed) return GT_OK;
+  GT_CHECK(matrix(p, true, ld, rows, cols, sz, name));
+  if (sw < 0) return fail(std::string("negative stride between the experts of ") + name);
+  return sw > kMaxElements / E ? fail(std::string(name) + " is too large") : GT_OK;
+}
+int lists(const float* weights, const int32_t* offsets, const int32_t* order, const int32_t* place) {
+  GT_CHECK(vector(weights, 4, "weights"));
+  GT_CHECK(vector(offsets, 4, "offsets"));
+  GT_CHECK(vector(order, 4, "order"));
+  return vector(place, 4, "place");
 }
 
 int experts_args_checks(const gt_experts_args* a, bool pointers) {
@@ -472,13 +504,16 @@ int experts_args_checks(const gt_experts_args* a, bool pointers) {
   if (pointers && a->T > 0 &&
       (!a->X || !a->W1 || !a->W2 || !a->Y || !a->weights || !a->offsets || !a->order || !a->place))
     return fail("gt_experts: null X, W1, W2, Y or list");
-  GT_CHECK(row(a->X, a->ldx, a->D, "X"));
-  GT_CHECK(row(a->W1, a->ldw1, wide, "W1"));
-  GT_CHECK(row(a->W2, a->ldw2, a->D, "W2"));
-  GT_CHECK(row(a->R, a->ldr, a->D, "R"));
-  GT_CHECK(row(a->Y, a->ldy, a->D, "Y"));
-  if (a->sw1 < 0 || a->sw2 < 0) return fail("gt_experts: negative stride between experts");
-  return row(a->P, a->ldp, wide, "P");
+  const int64_t sz = size_of(a->dtype);
+  GT_CHECK(matrix(a->X, true, a->ldx, a->T, a->D, sz, "X"));
+  GT_CHECK(stack(a->W1, true, a->ldw1, a->sw1, a->D, wide, a->E, sz, "W1"));
+  GT_CHECK(stack(a->W2, true, a->ldw2, a->sw2, a->H, a->D, a->E, sz, "W2"));
+  GT_CHECK(vector(a->b1, sz, "b1"));
+  GT_CHECK(vector(a->b2, sz, "b2"));
+  GT_CHECK(matrix(a->R, false, a->ldr, a->T, a->D, sz, "R"));
+  GT_CHECK(matrix(a->Y, true, a->ldy, a->T, a->D, sz, "Y"));
+  GT_CHECK(matrix(a->P, false, a->ldp, a->T * a->k, wide, sz, "P"));
+  return lists(a->weights, a->offsets, a->order, a->place);
 }
 
 struct Experts {
@@ -571,13 +606,20 @@ int experts_grad_checks(const gt_experts_grad_args* a, bool pointers) {
       return fail("gt_experts_backward: dX needs W1, dW1 needs X");
   }
   if (pointers && a->T == 0 && !a->offsets) return fail("gt_experts_backward: null offsets");
-  GT_CHECK(row(a->dY, a->lddy, a->D, "dY"));
-  GT_CHECK(row(a->X, a->ldx, a->D, "X"));
-  GT_CHECK(row(a->W1, a->ldw1, wide, "W1"));
-  GT_CHECK(row(a->W2, a->ldw2, a->D, "W2"));
-  GT_CHECK(row(a->P, a->ldp, wide, "P"));
-  if (a->sw1 < 0 || a->sw2 < 0) return fail("gt_experts_backward: negative stride between experts");
-  return row(a->dX, a->lddx, a->D, "dX");
+  const int64_t sz = size_of(a->dtype);
+  GT_CHECK(matrix(a->dY, true, a->lddy, a->T, a->D, sz, "dY"));
+  GT_CHECK(matrix(a->X, a->dW1, a->ldx, a->T, a->D, sz, "X"));
+  GT_CHECK(stack(a->W1, a->dX, a->ldw1, a->sw1, a->D, wide, a->E, sz, "W1"));
+  GT_CHECK(stack(a->W2, true, a->ldw2, a->sw2, a->H, a->D, a->E, sz, "W2"));
+  GT_CHECK(vector(a->b2, sz, "b2"));
+  GT_CHECK(matrix(a->P, true, a->ldp, a->T * a->k, wide, sz, "P"));
+  GT_CHECK(matrix(a->dX, false, a->lddx, a->T, a->D, sz, "dX"));
+  GT_CHECK(vector(a->dW1, sz, "dW1"));
+  GT_CHECK(vector(a->dW2, sz, "dW2"));
+  GT_CHECK(vector(a->db1, 4, "db1"));
+  GT_CHECK(vector(a->db2, 4, "db2"));
+  GT_CHECK(vector(a->dweights, 4, "dweights"));
+  return lists(a->weights, a->offsets, a->order, a->place);
 }
 
 struct ExpertsGrad {
@@ -717,32 +759,32 @@ hipError_t launch_product(int dtype, int layout, int tile, bool reg, const Produ
 
 }  // namespace gt
 
+namespace {
+
 using namespace gt;
 
-extern "C" {
-
-int gt_linear_workspace(const gt_linear_args* a, int64_t* bytes) {
+int linear_workspace_impl(const gt_linear_args* a, int64_t* bytes) {
   if (!bytes) return fail("gt_linear_workspace: null argument");
   GT_CHECK(linear_checks(a, false));
   *bytes = linear_product(*a).scratch();
   return GT_OK;
 }
 
-int gt_linear(const gt_linear_args* a, void* ws, int64_t ws_bytes, void* stream) {
+int linear_impl(const gt_linear_args* a, void* ws, int64_t ws_bytes, void* stream) {
   GT_CHECK(linear_checks(a, true));
   Product p = linear_product(*a);
   GT_CHECK(scratch_ok(ws, ws_bytes, p.scratch()));
   return run(p, ws, static_cast<hipStream_t>(stream));
 }
 
-int gt_linear_backward_workspace(const gt_linear_grad_args* a, int64_t* bytes) {
+int linear_backward_workspace_impl(const gt_linear_grad_args* a, int64_t* bytes) {
   if (!bytes) return fail("gt_linear_backward_workspace: null argument");
   GT_CHECK(linear_grad_checks(a, false));
   *bytes = linear_grad(*a, nullptr).bytes;
   return GT_OK;
 }
 
-int gt_linear_backward(const gt_linear_grad_args* a, void* ws, int64_t ws_bytes, void* stream) {
+int linear_backward_impl(const gt_linear_grad_args* a, void* ws, int64_t ws_bytes, void* stream) {
   GT_CHECK(linear_grad_checks(a, true));
   const hipStream_t s = static_cast<hipStream_t>(stream);
   LinearGrad g = linear_grad(*a, ws);
@@ -772,15 +814,7 @@ int gt_linear_backward(const gt_linear_grad_args* a, void* ws, int64_t ws_bytes,
   return GT_OK;
 }
 
-int gt_route_workspace(const gt_route_args* a, int64_t* bytes) {
-  if (!a || !bytes) return fail("gt_route_workspace: null argument");
-  if (a->T < 0 || a->T >= kMaxExtent || a->E < 1 || a->E > 1024 || a->k < 1 || a->k > 64)
-    return fail("gt_route: T, E or k out of range");
-  *bytes = route_scratch(a->T, a->E, a->k, a->groups);
-  return GT_OK;
-}
-
-int gt_route(const gt_route_args* a, void* ws, int64_t ws_bytes, void* stream) {
+int route_checks(const gt_route_args* a, bool pointers) {
   if (!a) return fail("gt_route: null arguments");
   GT_CHECK(extent(a->T, 0, "T"));
   if (a->E < 1 || a->E > 1024 || a->groups < 1 || a->E % a->groups != 0 || a->keep < 1 ||
@@ -791,16 +825,30 @@ int gt_route(const gt_route_args* a, void* ws, int64_t ws_bytes, void* stream) {
   if (a->T * a->k >= kMaxExtent) return fail("gt_route: T·k out of range");
   if (!dtype_ok(a->dtype) || (a->score != GT_SCORE_SOFTMAX && a->score != GT_SCORE_SIGMOID))
     return fail("gt_route: unknown dtype or score");
-  if (!a->offsets ||
-      (a->T > 0 && (!a->logits || !a->weights || !a->experts || !a->order || !a->place)))
+  if (pointers && (!a->offsets || (a->T > 0 && (!a->logits || !a->weights || !a->experts ||
+                                                !a->order || !a->place))))
     return fail("gt_route: null logits or output");
-  GT_CHECK(row(a->logits, a->ldl, a->E, "the logits"));
+  GT_CHECK(matrix(a->logits, true, a->ldl, a->T, a->E, size_of(a->dtype), "the logits"));
+  GT_CHECK(vector(a->bias, 4, "bias"));
+  GT_CHECK(vector(a->experts, 4, "experts"));
+  return lists(a->weights, a->offsets, a->order, a->place);
+}
+
+int route_workspace_impl(const gt_route_args* a, int64_t* bytes) {
+  if (!bytes) return fail("gt_route_workspace: null argument");
+  GT_CHECK(route_checks(a, false));
+  *bytes = route_scratch(a->T, a->E, a->k, a->groups);
+  return GT_OK;
+}
+
+int route_impl(const gt_route_args* a, void* ws, int64_t ws_bytes, void* stream) {
+  GT_CHECK(route_checks(a, true));
   GT_CHECK(scratch_ok(ws, ws_bytes, route_scratch(a->T, a->E, a->k, a->groups)));
   GT_TRY(launch_route(*a, ws, static_cast<hipStream_t>(stream)), "routing");
   return GT_OK;
 }
 
-int gt_route_backward(const gt_route_grad_args* a, void* stream) {
+int route_backward_impl(const gt_route_grad_args* a, void* stream) {
   if (!a) return fail("gt_route_backward: null arguments");
   GT_CHECK(extent(a->T, 0, "T"));
   if (a->E < 1 || a->E > 1024 || a->k < 1 || a->k > 64 || a->k > a->E)
@@ -809,20 +857,23 @@ int gt_route_backward(const gt_route_grad_args* a, void* stream) {
     return fail("gt_route_backward: unknown dtype or score");
   if (a->T > 0 && (!a->logits || !a->experts || !a->dweights || !a->dlogits))
     return fail("gt_route_backward: null argument");
-  GT_CHECK(row(a->logits, a->ldl, a->E, "the logits"));
-  GT_CHECK(row(a->dlogits, a->lddl, a->E, "dlogits"));
+  const int64_t sz = size_of(a->dtype);
+  GT_CHECK(matrix(a->logits, true, a->ldl, a->T, a->E, sz, "the logits"));
+  GT_CHECK(matrix(a->dlogits, true, a->lddl, a->T, a->E, sz, "dlogits"));
+  GT_CHECK(vector(a->experts, 4, "experts"));
+  GT_CHECK(vector(a->dweights, 4, "dweights"));
   GT_TRY(launch_route_grad(*a, static_cast<hipStream_t>(stream)), "gradient of the routing");
   return GT_OK;
 }
 
-int gt_experts_workspace(const gt_experts_args* a, int64_t* bytes) {
+int experts_workspace_impl(const gt_experts_args* a, int64_t* bytes) {
   if (!bytes) return fail("gt_experts_workspace: null argument");
   GT_CHECK(experts_args_checks(a, false));
   *bytes = experts(*a, nullptr).bytes;
   return GT_OK;
 }
 
-int gt_experts(const gt_experts_args* a, void* ws, int64_t ws_bytes, void* stream) {
+int experts_impl(const gt_experts_args* a, void* ws, int64_t ws_bytes, void* stream) {
   GT_CHECK(experts_args_checks(a, true));
   if (a->T == 0) return GT_OK;
   const hipStream_t s = static_cast<hipStream_t>(stream);
@@ -848,14 +899,14 @@ int gt_experts(const gt_experts_args* a, void* ws, int64_t ws_bytes, void* strea
   return GT_OK;
 }
 
-int gt_experts_backward_workspace(const gt_experts_grad_args* a, int64_t* bytes) {
+int experts_backward_workspace_impl(const gt_experts_grad_args* a, int64_t* bytes) {
   if (!bytes) return fail("gt_experts_backward_workspace: null argument");
   GT_CHECK(experts_grad_checks(a, false));
   *bytes = experts_grad(*a, nullptr).bytes;
   return GT_OK;
 }
 
-int gt_experts_backward(const gt_experts_grad_args* a, void* ws, int64_t ws_bytes, void* stream) {
+int experts_backward_impl(const gt_experts_grad_args* a, void* ws, int64_t ws_bytes, void* stream) {
   GT_CHECK(experts_grad_checks(a, true));
   const hipStream_t s = static_cast<hipStream_t>(stream);
   ExpertsGrad g = experts_grad(*a, ws);
@@ -911,6 +962,54 @@ int gt_experts_backward(const gt_experts_grad_args* a, void* ws, int64_t ws_byte
   }
   if (a->dW1) GT_CHECK(run(g.dw1, g.rest, s));
   return GT_OK;
+}
+
+// Messages allocate host memory: no C++ exception crosses the C ABI.
+template <class F>
+int guarded(F f) {
+  try {
+    return f();
+  } catch (const std::exception&) {
+    return GT_EINVAL;
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int gt_linear_workspace(const gt_linear_args* a, int64_t* bytes) {
+  return guarded([&] { return linear_workspace_impl(a, bytes); });
+}
+int gt_linear(const gt_linear_args* a, void* ws, int64_t ws_bytes, void* stream) {
+  return guarded([&] { return linear_impl(a, ws, ws_bytes, stream); });
+}
+int gt_linear_backward_workspace(const gt_linear_grad_args* a, int64_t* bytes) {
+  return guarded([&] { return linear_backward_workspace_impl(a, bytes); });
+}
+int gt_linear_backward(const gt_linear_grad_args* a, void* ws, int64_t ws_bytes, void* stream) {
+  return guarded([&] { return linear_backward_impl(a, ws, ws_bytes, stream); });
+}
+int gt_route_workspace(const gt_route_args* a, int64_t* bytes) {
+  return guarded([&] { return route_workspace_impl(a, bytes); });
+}
+int gt_route(const gt_route_args* a, void* ws, int64_t ws_bytes, void* stream) {
+  return guarded([&] { return route_impl(a, ws, ws_bytes, stream); });
+}
+int gt_route_backward(const gt_route_grad_args* a, void* stream) {
+  return guarded([&] { return route_backward_impl(a, stream); });
+}
+int gt_experts_workspace(const gt_experts_args* a, int64_t* bytes) {
+  return guarded([&] { return experts_workspace_impl(a, bytes); });
+}
+int gt_experts(const gt_experts_args* a, void* ws, int64_t ws_bytes, void* stream) {
+  return guarded([&] { return experts_impl(a, ws, ws_bytes, stream); });
+}
+int gt_experts_backward_workspace(const gt_experts_grad_args* a, int64_t* bytes) {
+  return guarded([&] { return experts_backward_workspace_impl(a, bytes); });
+}
+int gt_experts_backward(const gt_experts_grad_args* a, void* ws, int64_t ws_bytes, void* stream) {
+  return guarded([&] { return experts_backward_impl(a, ws, ws_bytes, stream); });
 }
 
 }  // extern "C"

@@ -1,6 +1,6 @@
 #!/bin/bash
 # Host-side memory and undefined-behaviour check, CPU only: rebuilds the host
-# units of libgemmtune.so (space, search, runtime, lookup) with AddressSanitizer
+# units of libgemmtune.so (space, search, runtime, lookup, layers) with AddressSanitizer
 # and UBSan on the host pass only, links them with the kernel objects of the
 # last build, builds the oracle with the same sanitizers (clang, one runtime),
 # and runs the CPU test suite against both with the runtime preloaded.
@@ -15,13 +15,14 @@ CXXF="-O1 -g -std=c++17 -fPIC --offload-arch=gfx950 -Xclang -target-feature -Xcl
 SAN="-Xarch_host -fsanitize=address -Xarch_host -fsanitize=undefined -Xarch_host -fno-omit-frame-pointer
      -Xarch_host -fno-sanitize-recover=undefined"
 ls "$R"/_build/gemm_*_c*.o > /dev/null   # kernel objects of a normal build
-for u in space search runtime gemm_lookup; do
+for u in space search runtime gemm_lookup layers; do
   $H $CXXF $SAN -x hip -c "$R/paper_1909_10616_amd/csrc/$u.cpp" -o "$O/$u.o" &
 done
 wait
 $H --offload-arch=gfx950 -shared -fPIC -Xarch_host -fsanitize=address -Xarch_host -fsanitize=undefined \
    -shared-libsan "$O"/space.o "$O"/search.o "$O"/runtime.o "$O"/gemm_lookup.o \
-   "$R"/_build/aux_kernels.o "$R"/_build/noalloc.o "$R"/_build/gemm_*_c*.o -o "$O/libgemmtune.so"
+   "$O"/layers.o "$R"/_build/aux_kernels.o "$R"/_build/noalloc.o "$R"/_build/gemm_*_c*.o \
+   "$R"/_build/layer_kernels.o "$R"/_build/route.o "$R"/_build/product_*.o -o "$O/libgemmtune.so"
 /opt/rocm/llvm/bin/clang -O1 -g -std=c11 -fPIC -shared -fsanitize=address,undefined \
    -fno-sanitize-recover=undefined -fno-omit-frame-pointer -shared-libsan \
    "$R/oracle/oracle.c" -o "$O/liboracle.so" -lpthread -lm
