@@ -42,7 +42,8 @@ def _units():
     # layer operators: the host side, the memory-bound kernels, and the products
     # by operand type and layout
     units += [("layers", "layers.cpp", []), ("layer_kernels", "layer_kernels.hip", []),
-              ("route", "route.hip", []), ("product_rows", "product_rows.hip", [])]
+              ("route", "route.hip", []), ("product_rows", "product_rows.hip", []),
+              ("product_slim", "product_slim.hip", [])]
     units += [(f"product_{dn}_{lay}", "product_inst.hip", [f"-DLP_DT={dt}", f"-DLP_LAY={lay}"])
               for dt, dn in ((0, "f32"), (1, "bf16")) for lay in (0, 1, 2)]
     for dt, dn in ((0, "f32"), (1, "bf16")):

@@ -115,6 +115,36 @@ int few_rows(const Product& p) {
   return a.M / rows + a.groups < 65536 ? rows : 0;
 }
 
+// The kernel of 16 rows a workgroup: its tile rows at most.
+constexpr int kSlimRows = 16;
+int64_t slim_rows(const ProductArgs& a) {
+  return a.groups > 0 ? a.M / kSlimRows + std::min<int64_t>(a.groups, a.M)
+                      : (a.M + kSlimRows - 1) / kSlimRows;
+}
+// And its time in µs in z K slices (0: it does not serve): the steps of a wavefront for every
+// workgroup that a compute unit gets, or W once for every tile row, at 10 TB/s while
+// the last cache holds it. Fitted to 60 shapes from 1×7×3 to 512×4096×4096, plain and gated,
+// with 1 to 16 slices; it is chosen up to 64 rows or so, or more of small matrices
+// (13×1021×777 in fp32: 9.6 µs, the best tile with its join 14.2; 64×1024×1024 in bf16 6.4
+// and 8.5; 256×1024×1024 6.9 and 8.9; but 64×11008×4096 59 and 25).
+double slim_cost(const Product& p, int64_t z) {
+  const ProductArgs& a = p.a;
+  const int64_t rows = slim_rows(a), cols = (a.N + 63) / 64;
+  if (a.M < 1 || rows >= 65536 || rows * cols >= kMaxExtent) return 0.0;
+  const bool bf16 = p.dtype == GT_BF16, gated = a.e.epi == kEpiGated;
+  const int64_t step = bf16 ? 32 : 16, steps = (a.K + step - 1) / step, waves = slim_waves(gated);
+  if (z > 1 && steps < 16 * z) return 0.0;
+  const double each = static_cast<double>(((steps + z - 1) / z + waves - 1) / waves);
+  const double queue = static_cast<double>((rows * cols * z + 255) / 256);
+  // [type][gated][aligned]
+  constexpr double kStep[2][2][2] = {{{1.8, 1.7}, {2.3, 1.65}}, {{3.0, 1.45}, {3.5, 1.25}}};
+  const double per = kStep[bf16][gated][slim_aligned(p.dtype, a)];
+  const double matrix = static_cast<double>(a.K) * a.N * (gated ? 2 : 1) * size_of(p.dtype);
+  const double memory = std::max(rows * matrix / (matrix <= 64e6 ? 10e6 : 6e6), matrix / 5.2e6);
+  return 4.2 + std::hypot(each * per * queue, memory) +
+         (z > 1 ? 4.5 + 2.0 * z * a.M * a.N * (gated ? 2 : 1) * 4 / 6.0e6 : 0.0);
+}
+
 // What a tile takes a compute unit, in µs: a stage (128 bytes of k) alone and
 // when others share the unit, its launch and epilogue, and how many share it. Fitted to
 // 35 shapes from 1×4096×4096 to 2048×4096×4096, 14 of them odd, in every layout and
@@ -218,7 +248,26 @@ void choose(Product* p, bool may_split) {
       }
     }
   }
+  if (p->layout == kXW) {
+    for (int64_t z = 1; z <= 16; z *= 2) {
+      if (z > 1 && !may_split) break;
+      const double cost = slim_cost(*p, z);
+      if (cost > 0.0 && cost < best) {
+        best = cost;
+        p->rows = kSlimRows;
+        a.splits = static_cast<int>(z);
+      }
+    }
+  }
   a.half = a.N;
+  a.e.ldpart = up(a.N, 4) * (gated ? 2 : 1);
+  p->part = a.splits > 1 ? a.splits * a.M * a.e.ldpart * 4 : 0;
+  if (p->rows > 0) {
+    p->reg = p->tails = false;
+    a.tilesN = static_cast<int>((a.N + 63) / 64);
+    a.tilesM = static_cast<int>(slim_rows(a));
+    return;
+  }
   if (!p->reg) {
     if (!sa.ok) {
       p->pad.job[p->pad.n++] = sa.job;
@@ -233,13 +282,15 @@ void choose(Product* p, bool may_split) {
       if (sb.job.half) a.half = sb.job.half;
     }
   }
-  a.e.ldpart = up(a.N, 4) * (gated ? 2 : 1);
   const TileShape& s = kTile[p->tile];
   const int64_t kb = (p->reg ? 128 : s.KB) / sz, all = (a.K + kb - 1) / kb;
   a.per_slice = static_cast<int>((all + a.splits - 1) / std::max(1, a.splits));
-  p->part = a.splits > 1 ? a.splits * a.M * a.e.ldpart * 4
-            : p->tails   ? static_cast<int64_t>(kUnits) * s.BM * s.BN * 4
-                         : 0;
+  if (p->tails) p->part = static_cast<int64_t>(kUnits) * s.BM * s.BN * 4;
+}
+
+hipError_t launch(const Product& p, const ProductArgs& a, hipStream_t s) {
+  return p.rows == kSlimRows ? launch_slim(p.dtype, a, s)
+                             : launch_product(p.dtype, p.layout, p.tile, p.reg, a, s);
 }
 
 // Launches a product; ws: its scratch() bytes.
@@ -247,7 +298,7 @@ int run(const Product& p, void* ws, hipStream_t s) {
   ProductArgs a = p.a;
   if (a.M == 0) return GT_OK;
   if (a.splits < 1) return fail("layer product: too many tiles");
-  if (p.rows > 0) {
+  if (p.rows > 0 && p.rows < kSlimRows) {
     GT_TRY(launch_rows(p.dtype, p.rows, a, s), "layer product of a few rows");
     return GT_OK;
   }
@@ -265,13 +316,13 @@ int run(const Product& p, void* ws, hipStream_t s) {
     a.e.part = reinterpret_cast<float*>(at);
     const int epi = a.e.epi;
     a.e.epi = kEpiPart;
-    GT_TRY(launch_product(p.dtype, p.layout, p.tile, p.reg, a, s), "layer product");
+    GT_TRY(launch(p, a, s), "layer product");
     a.e.epi = epi;
     GT_TRY(launch_reduce(p.dtype, a, s), "joining the K slices");
     return GT_OK;
   }
   if (p.tails) a.tail = reinterpret_cast<float*>(at);
-  GT_TRY(launch_product(p.dtype, p.layout, p.tile, p.reg, a, s), "layer product");
+  GT_TRY(launch(p, a, s), "layer product");
   if (p.tails) GT_TRY(launch_tail(a, s), "joining the last tiles");
   return GT_OK;
 }

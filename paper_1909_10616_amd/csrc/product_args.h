@@ -119,5 +119,8 @@ hipError_t launch_tail(const ProductArgs& a, hipStream_t s);
 // `rows` rows. The LDS it takes holds the rows.
 int64_t rows_lds(int64_t K, int rows, bool gated);
 hipError_t launch_rows(int dtype, int rows, const ProductArgs& a, hipStream_t s);
+constexpr int slim_waves(bool gated) { return gated ? 8 : 16; }   // (as registers allow)
+bool slim_aligned(int dtype, const ProductArgs& a);
+hipError_t launch_slim(int dtype, const ProductArgs& a, hipStream_t s);
 
 }  // namespace gt
