@@ -44,7 +44,7 @@ struct ActGradArgs {
   void* dP;
   int64_t lddp;
   float* part;
-  int vec;
+  bool wide;   // whole octets of columns
   int pad;   // columns of dP beyond its last that are written as zero
 };
 hipError_t launch_act_grad(int dtype, const ActGradArgs& a, hipStream_t s);
@@ -77,7 +77,8 @@ hipError_t launch_sort(int dtype, const SortArgs& a, hipStream_t s);
 // out[t] = R[t] + Σ_s w[t][s]·O[place[t][s]] (w NULL: 1; R NULL: 0), s ascending.
 struct CombineArgs {
   int64_t T, D, entries;
-  int k, vec;
+  int k;
+  bool wide;   // whole octets of columns
   const float* O;
   int64_t ldo;
   const float* weights;

@@ -142,7 +142,6 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const ActGradArgs a) {
   const int64_t r0 = static_cast<int64_t>(blockIdx.x) * kActRows + part;
   const int64_t left64 = a.N - n;
   const int left = left64 < 4 ? static_cast<int>(left64) : 4;
-  const bool vec = a.vec != 0;
   f32x4 dy[U][Q], gate[U][Q], up[U][Q];
 #pragma unroll
   for (int i = 0; i < U; ++i) {
@@ -167,10 +166,10 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const ActGradArgs a) {
         }
       }
     } else {
-      dy[i][0] = load4(d, left, vec);
+      dy[i][0] = load4(d, left);
       if (a.P) {
-        gate[i][0] = load4(p, left, vec);
-        if (a.gated) up[i][0] = load4(p + a.N, left, vec);
+        gate[i][0] = load4(p, left);
+        if (a.gated) up[i][0] = load4(p + a.N, left);
       }
     }
   }
@@ -202,8 +201,8 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const ActGradArgs a) {
         store8(out, oct{g[0], g[1]});
         if (a.gated) store8(out + a.N, oct{u[0], u[1]});
       } else {
-        store4(out, g[0], left, vec);
-        if (a.gated) store4(out + a.N, u[0], left, vec);
+        store4(out, g[0], left);
+        if (a.gated) store4(out + a.N, u[0], left);
         if (n + left == a.N)
           for (int z = 0; z < a.pad; ++z) out[(a.gated ? a.N : 0) + left + z] = T(0);
       }
@@ -371,7 +370,6 @@ template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
   constexpr int Q = WIDE ? 2 : 1;
   const uint32_t per = static_cast<uint32_t>((a.D + 4 * Q - 1) / (4 * Q));
-  const bool vec = a.vec != 0;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < a.T * per;
        i += static_cast<int64_t>(gridDim.x) * 256) {
     const int64_t t = i / per, n = (i - t * per) * 4 * Q;
@@ -384,7 +382,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
         r[0] = o.a;
         r[1] = o.b;
       } else {
-        r[0] = load4(p, left, vec);
+        r[0] = load4(p, left);
       }
     }
     for (int s0 = 0; s0 < a.k; s0 += 4) {
@@ -418,7 +416,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
     if constexpr (WIDE)
       store8(out, oct{v[0], v[1]});
     else
-      store4(out, v[0], left, vec);
+      store4(out, v[0], left);
   }
 }
 
@@ -477,16 +475,16 @@ hipError_t launch_tail(const ProductArgs& a, hipStream_t s) {
 
 hipError_t launch_act_grad(int dtype, const ActGradArgs& a, hipStream_t s) {
   if (a.M == 0) return hipSuccess;
-  const int cols = a.vec == 2 ? 512 : 256;
+  const int cols = a.wide ? 512 : 256;
   const dim3 grid(static_cast<unsigned>((a.M + kActRows - 1) / kActRows),
                   static_cast<unsigned>((a.N + cols - 1) / cols));
   if (dtype == GT_BF16) {
-    if (a.vec == 2)
+    if (a.wide)
       act_grad_kernel<uint16_t, true><<<grid, 256, 0, s>>>(a);
     else
       act_grad_kernel<uint16_t, false><<<grid, 256, 0, s>>>(a);
   } else {
-    if (a.vec == 2)
+    if (a.wide)
       act_grad_kernel<float, true><<<grid, 256, 0, s>>>(a);
     else
       act_grad_kernel<float, false><<<grid, 256, 0, s>>>(a);
@@ -523,17 +521,17 @@ hipError_t launch_sort(int dtype, const SortArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_combine(int dtype, const CombineArgs& a, hipStream_t s) {
-  const int cols = a.vec == 2 ? 8 : 4;
+  const int cols = a.wide ? 8 : 4;
   const int64_t n = a.T * ((a.D + cols - 1) / cols);
   if (n == 0) return hipSuccess;
   const dim3 grid(blocks_for(n, 256));
   if (dtype == GT_BF16) {
-    if (a.vec == 2)
+    if (a.wide)
       combine_kernel<uint16_t, true><<<grid, 256, 0, s>>>(a);
     else
       combine_kernel<uint16_t, false><<<grid, 256, 0, s>>>(a);
   } else {
-    if (a.vec == 2)
+    if (a.wide)
       combine_kernel<float, true><<<grid, 256, 0, s>>>(a);
     else
       combine_kernel<float, false><<<grid, 256, 0, s>>>(a);

@@ -80,15 +80,17 @@ __device__ __forceinline__ T from_float(float v) {
     return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
 }
 
-// Up to 4 values from p on, the first n of them (all at once if vec); zero beyond.
+// Up to 4 values from p on, the first n of them; zero beyond. Four are one access, at any
+// alignment (which the memory system splits where it must).
 template <typename T>
-__device__ __forceinline__ f32x4 load4(const T* p, int n, bool vec) {
+__device__ __forceinline__ f32x4 load4(const T* p, int n) {
   f32x4 v{};
-  if (vec && n >= 4) {
+  if (n >= 4) {
     if constexpr (sizeof(T) == 4) {
-      v = *reinterpret_cast<const f32x4*>(p);
+      __builtin_memcpy(&v, p, 16);
     } else {
-      const uint2 u = *reinterpret_cast<const uint2*>(p);
+      uint2 u;
+      __builtin_memcpy(&u, p, 8);
       v[0] = __builtin_bit_cast(float, u.x << 16);
       v[1] = __builtin_bit_cast(float, u.x & 0xffff0000u);
       v[2] = __builtin_bit_cast(float, u.y << 16);
@@ -96,28 +98,29 @@ __device__ __forceinline__ f32x4 load4(const T* p, int n, bool vec) {
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 3; ++i)
       if (i < n) v[i] = to_float(p[i]);
   }
   return v;
 }
 
 template <typename T>
-__device__ __forceinline__ void store4(T* p, f32x4 v, int n, bool vec) {
-  if (vec && n >= 4) {
-    if constexpr (sizeof(T) == 4)
-      *reinterpret_cast<f32x4*>(p) = v;
-    else
-      *reinterpret_cast<uint2*>(p) =
-          __builtin_bit_cast(uint2, __builtin_convertvector(v, bf16x4));
+__device__ __forceinline__ void store4(T* p, f32x4 v, int n) {
+  if (n >= 4) {
+    if constexpr (sizeof(T) == 4) {
+      __builtin_memcpy(p, &v, 16);
+    } else {
+      const uint2 u = __builtin_bit_cast(uint2, __builtin_convertvector(v, bf16x4));
+      __builtin_memcpy(p, &u, 8);
+    }
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 3; ++i)
       if (i < n) p[i] = from_float<T>(v[i]);
   }
 }
 
-// 8 values at a 16-byte aligned p.
+// 8 values, at any alignment.
 struct oct {
   f32x4 a, b;
 };
@@ -145,17 +148,20 @@ __device__ __forceinline__ oct open8(const raw8<T>& r) {
 }
 template <typename T>
 __device__ __forceinline__ oct load8(const T* p) {
-  return open8<T>(*reinterpret_cast<const raw8<T>*>(p));
+  raw8<T> r;
+  __builtin_memcpy(&r, p, sizeof(r));
+  return open8<T>(r);
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const oct& v) {
   if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<f32x4*>(p) = v.a;
-    *reinterpret_cast<f32x4*>(p + 4) = v.b;
+    __builtin_memcpy(p, &v.a, 16);
+    __builtin_memcpy(p + 4, &v.b, 16);
   } else {
     const uint2 x = __builtin_bit_cast(uint2, __builtin_convertvector(v.a, bf16x4));
     const uint2 y = __builtin_bit_cast(uint2, __builtin_convertvector(v.b, bf16x4));
-    *reinterpret_cast<u32x4*>(p) = u32x4{x.x, x.y, y.x, y.y};
+    const u32x4 w{x.x, x.y, y.x, y.y};
+    __builtin_memcpy(p, &w, 16);
   }
 }
 template <int ACT>

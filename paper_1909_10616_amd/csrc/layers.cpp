@@ -327,18 +327,6 @@ int run(const Product& p, void* ws, hipStream_t s) {
   return GT_OK;
 }
 
-// Rows of n elements of sz bytes (pointer and leading dimension; null: none): 2
-// if all take accesses of 8 elements, 1 of 4, 0 of one.
-int width(int64_t n, std::initializer_list<std::pair<const void*, int64_t>> rows, int64_t sz) {
-  for (int w = 2; w >= 1; --w) {
-    const int64_t e = 4 * w, bytes = std::min<int64_t>(16, e * sz);
-    bool ok = n % e == 0;
-    for (const auto& r : rows) ok = ok && (!r.first || (aligned(r.first, bytes) && r.second % e == 0));
-    if (ok) return w;
-  }
-  return 0;
-}
-
 int extent(int64_t v, int64_t least, const char* name) {
   if (v < least || v >= kMaxExtent) return fail(std::string(name) + " out of range");
   return GT_OK;
@@ -418,8 +406,6 @@ Product linear_product(const gt_linear_args& q) {
   e.bias = q.bias;
   e.R = q.R;
   e.ldr = q.ldr;
-  e.vec = std::min(width(q.N, {{q.P, q.ldp}, {q.bias, 0}, {q.R, q.ldr}}, size_of(q.dtype)),
-                   width(q.N, {{q.Y, q.ldy}}, size_of(q.out_dtype)));
   choose(&p, true);
   return p;
 }
@@ -462,12 +448,11 @@ struct LinearGrad {
   int64_t bytes = 0;
 };
 
-void output(Epilogue* e, void* y, int64_t ldy, bool f32, int64_t n, int64_t sz) {
+void output(Epilogue* e, void* y, int64_t ldy, bool f32) {
   e->epi = kEpiPlain;
   e->Y = y;
   e->ldy = ldy;
   e->out_f32 = f32 ? 1 : 0;
-  e->vec = width(n, {{y, ldy}}, f32 ? 4 : sz);
 }
 
 LinearGrad linear_grad(const gt_linear_grad_args& q, void* ws) {
@@ -493,7 +478,7 @@ LinearGrad linear_grad(const gt_linear_grad_args& q, void* ws) {
     a.M = q.M;
     a.N = q.K;
     a.K = g.wide;
-    output(&a.e, q.dX, q.lddx, q.dtype == GT_F32, q.K, sz);
+    output(&a.e, q.dX, q.lddx, q.dtype == GT_F32);
     g.dx.own_a = g.own_dP;
     choose(&g.dx, true);
     rest = std::max(rest, g.dx.scratch());
@@ -509,7 +494,7 @@ LinearGrad linear_grad(const gt_linear_grad_args& q, void* ws) {
     a.M = q.K;
     a.N = g.wide;
     a.K = q.M;
-    output(&a.e, q.dW, q.lddw, q.dw_dtype == GT_F32, g.wide, sz);
+    output(&a.e, q.dW, q.lddw, q.dw_dtype == GT_F32);
     g.dw.own_b = g.own_dP;
     choose(&g.dw, true);
     rest = std::max(rest, g.dw.scratch());
@@ -611,7 +596,6 @@ Experts experts(const gt_experts_args& q, void* ws) {
     e.ldp = q.ldp;
     e.bias = q.b1;
     e.sbias = wide;
-    e.vec = width(q.H, {{q.P, q.ldp}, {q.b1, 0}, {x.H, ldh}}, sz);
     e.zero_pad = 1;
     choose(&x.up, true);
   }
@@ -636,7 +620,6 @@ Experts experts(const gt_experts_args& q, void* ws) {
     e.ldy = x.ldo;
     e.bias = q.b2;
     e.sbias = q.D;
-    e.vec = std::min(width(q.D, {{q.b2, 0}}, sz), width(q.D, {{x.O, x.ldo}}, 4));
     x.down.own_a = true;
     choose(&x.down, true);
   }
@@ -732,7 +715,6 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     e.wide = g.wide;
     e.zero_pad = 1;
     g.dh.own_a = true;
-    e.vec = width(q.H, {{q.P, q.ldp}, {g.dP, g.ldp}, {g.Hw, g.ldh}}, sz);
     choose(&g.dh, false);
     const TileShape& t = kTile[g.dh.tile];
     // Σ dH·H of a row's tiles, then b2·dY of its columns' blocks
@@ -751,7 +733,7 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     a.M = q.H;
     a.N = q.D;
     a.K = g.R;
-    output(&a.e, q.dW2, q.D, q.dtype == GT_F32, q.D, sz);
+    output(&a.e, q.dW2, q.D, q.dtype == GT_F32);
     a.e.sY = q.H * q.D;
     g.dw2.own_a = g.dw2.own_b = true;
     choose(&g.dw2, false);
@@ -767,7 +749,7 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     a.N = q.D;
     a.K = g.wide;
     g.dXs = s.take<float>(g.R * g.ldo * 4);
-    output(&a.e, g.dXs, g.ldo, true, q.D, sz);
+    output(&a.e, g.dXs, g.ldo, true);
     g.dx.own_a = true;
     choose(&g.dx, false);
   }
@@ -780,7 +762,7 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     a.M = q.D;
     a.N = g.wide;
     a.K = g.R;
-    output(&a.e, q.dW1, g.wide, q.dtype == GT_F32, g.wide, sz);
+    output(&a.e, q.dW1, g.wide, q.dtype == GT_F32);
     a.e.sY = q.D * g.wide;
     g.dw1.own_a = g.dw1.own_b = true;
     choose(&g.dw1, false);
@@ -854,7 +836,7 @@ int linear_backward_impl(const gt_linear_grad_args* a, void* ws, int64_t ws_byte
     q.lddp = g.lddp;
     q.part = g.sums;
     q.pad = static_cast<int>(g.lddp - g.wide);
-    q.vec = width(a->N, {{a->dY, a->lddy}, {q.P, a->ldp}, {g.dP, g.lddp}}, size_of(a->dtype));
+    q.wide = a->N % 8 == 0;
     GT_TRY(launch_act_grad(a->dtype, q, s), "gradient of the activation");
     if (a->db)
       GT_TRY(launch_join(g.sums, (a->M + kActRows - 1) / kActRows, g.wide, nullptr, 1, 0, 1, 1, a->db, s),
@@ -945,7 +927,7 @@ int experts_impl(const gt_experts_args* a, void* ws, int64_t ws_bytes, void* str
   c.ldr = a->ldr;
   c.out = a->Y;
   c.ldout = a->ldy;
-  c.vec = width(a->D, {{a->R, a->ldr}, {a->Y, a->ldy}}, size_of(a->dtype));
+  c.wide = a->D % 8 == 0;
   GT_TRY(launch_combine(a->dtype, c, s), "summing the experts' outputs");
   return GT_OK;
 }
@@ -1008,7 +990,7 @@ int experts_backward_impl(const gt_experts_grad_args* a, void* ws, int64_t ws_by
     c.place = a->place;
     c.out = a->dX;
     c.ldout = a->lddx;
-    c.vec = width(a->D, {{a->dX, a->lddx}}, size_of(a->dtype));
+    c.wide = a->D % 8 == 0;
     GT_TRY(launch_combine(a->dtype, c, s), "summing the experts' gradients");
   }
   if (a->dW1) GT_CHECK(run(g.dw1, g.rest, s));

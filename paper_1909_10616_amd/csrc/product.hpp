@@ -178,13 +178,12 @@ template <typename T>
 __device__ __forceinline__ void linear_quad(const Epilogue& e, int64_t N, int64_t row, int64_t n,
                                             int group, int left, bool gated, f32x4 v, f32x4 u,
                                             f32x4 bv, f32x4 bu, f32x4 r) {
-  const bool vec = e.vec != 0;
   v += bv;
   u += bu;
   if (e.P) {
     T* p = static_cast<T*>(e.P) + row * e.ldp + n;
-    store4(p, v, left, vec);
-    if (gated) store4(p + N, u, left, vec);
+    store4(p, v, left);
+    if (gated) store4(p + N, u, left);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = act_value(e.act, v[i]);
@@ -195,9 +194,9 @@ __device__ __forceinline__ void linear_quad(const Epilogue& e, int64_t N, int64_
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = i < left ? v[i] : 0.0f;
   if (e.out_f32)
-    store4(static_cast<float*>(e.Y) + at, v, pad ? 4 : left, vec || pad);
+    store4(static_cast<float*>(e.Y) + at, v, pad ? 4 : left);
   else
-    store4(static_cast<T*>(e.Y) + at, v, pad ? 4 : left, vec || pad);
+    store4(static_cast<T*>(e.Y) + at, v, pad ? 4 : left);
 }
 // Columns that an epilogue writes: N, or up to the next 16 bytes.
 template <typename T>
@@ -207,12 +206,11 @@ __device__ __forceinline__ int64_t written(const Epilogue& e, int64_t N) {
 }
 template <typename T>
 __device__ __forceinline__ f32x4 bias_quad(const Epilogue& e, int64_t n, int group, int left) {
-  return e.bias ? load4(static_cast<const T*>(e.bias) + group * e.sbias + n, left, e.vec != 0)
-                : f32x4{};
+  return e.bias ? load4(static_cast<const T*>(e.bias) + group * e.sbias + n, left) : f32x4{};
 }
 template <typename T>
 __device__ __forceinline__ f32x4 residual_quad(const Epilogue& e, int64_t row, int64_t n, int left) {
-  return e.R ? load4(static_cast<const T*>(e.R) + row * e.ldr + n, left, e.vec != 0) : f32x4{};
+  return e.R ? load4(static_cast<const T*>(e.R) + row * e.ldr + n, left) : f32x4{};
 }
 
 // Where a wavefront's tile lies.
@@ -249,10 +247,10 @@ struct EpiRows {
 
   // Whether the slope epilogue takes octets: columns that all exist.
   __device__ static __forceinline__ bool whole_slope(const ProductArgs& a, const EpiPlace& p) {
-    return a.e.vec == 2 && p.col + BN / 2 + WN / 2 <= a.N;
+    return p.col + BN / 2 + WN / 2 <= a.N;
   }
 
-  // A whole tile of aligned rows of whole octets: 16-byte accesses, nothing checked.
+  // A whole tile: 16-byte accesses, at any alignment, nothing checked.
   // The residuals of U rows are loaded before the first of them is stored (an output may
   // be the residual itself) and while the U rows before them are worked on.
   template <int ACT>
@@ -405,8 +403,8 @@ struct EpiRows {
         gate[i] = raw8<T>{};
         up[i] = raw8<T>{};
         if (r < RP && r < rows) {
-          gate[i] = *reinterpret_cast<const raw8<T>*>(P + r * e.ldp);
-          if (e.gated) up[i] = *reinterpret_cast<const raw8<T>*>(P + r * e.ldp + a.N);
+          __builtin_memcpy(&gate[i], P + r * e.ldp, sizeof(gate[i]));
+          if (e.gated) __builtin_memcpy(&up[i], P + r * e.ldp + a.N, sizeof(up[i]));
         }
       }
     };
@@ -465,7 +463,6 @@ struct EpiRows {
     const int c = lane % LR;
     const int64_t n = col(c);
     const int left = a.N - n < 4 ? static_cast<int>(a.N - n) : 4;
-    const bool vec = e.vec != 0;
     const float mine_w = row_weight();
 #pragma unroll 1
     for (int r0 = lane / LR; r0 < RP; r0 += U * STEP) {
@@ -477,8 +474,8 @@ struct EpiRows {
         gate[i] = f32x4{};
         up[i] = f32x4{1.0f, 1.0f, 1.0f, 1.0f};
         if (row >= p.row_end || left <= 0) continue;
-        gate[i] = load4(pp, left, vec);
-        if (e.gated) up[i] = load4(pp + a.N, left, vec);
+        gate[i] = load4(pp, left);
+        if (e.gated) up[i] = load4(pp + a.N, left);
       }
 #pragma unroll
       for (int i = 0; i < U; ++i) {
@@ -505,15 +502,15 @@ struct EpiRows {
         if (row < p.row_end && n < written<T>(e, a.N)) {
           T* out = static_cast<T*>(e.Y) + row * e.ldy + n;
           // (rows padded with zeros: dP's end with the up half when gated)
-          store4(out, dg, e.gated ? left : e.zero_pad ? 4 : left, vec);
+          store4(out, dg, e.gated ? left : e.zero_pad ? 4 : left);
           if (e.gated) {
-            store4(out + a.N, du, left, vec);
+            store4(out + a.N, du, left);
             constexpr int64_t VEC = 16 / sizeof(T);
             const int64_t pad = (2 * a.N + VEC - 1) / VEC * VEC - 2 * a.N;
             if (e.zero_pad && left > 0 && n + left == a.N)
               for (int64_t z = 0; z < pad; ++z) (out + a.N)[left + z] = T(0);
           }
-          store4(static_cast<T*>(e.Hw) + row * e.ldh + n, hw, left, vec);
+          store4(static_cast<T*>(e.Hw) + row * e.ldh + n, hw, left);
         }
 #pragma unroll
         for (int d = 1; d < LR; d <<= 1) dot += __shfl_xor(dot, d);
@@ -538,7 +535,7 @@ struct EpiRows {
       else
         slope_whole<GT_ACT_NONE>(sums);
     } else {
-      const bool all = e.vec == 2 && p.row + WM <= p.row_end &&
+      const bool all = p.row + WM <= p.row_end &&
                        p.col + (G ? WN / 2 : BN / 2 + WN / 2) <= a.N;
       if (!all)
         edge();

@@ -21,8 +21,6 @@ struct Epilogue {
   int32_t act;       // gt_act
   int32_t gated;     // columns n and N + n are a gate and its up value
   int32_t out_f32;   // Y in fp32, else in the operands' type
-  int32_t vec;       // every row and pointer takes accesses of: 1: 4 elements, 2: 8 (16 bytes
-                     // at least), 0: one
   int32_t zero_pad;  // columns of Y from N to the next 16 bytes are written as zero
   void* Y;           // [rows][ldy]; group g at Y + g·sY (groups along k)
   int64_t ldy, sY;
