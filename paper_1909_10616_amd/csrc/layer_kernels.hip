@@ -278,11 +278,12 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* part, int64_t r
 // ---- sorted copies of rows, and what else dY's rows give
 
 // 256 threads: a block of rows of one group, a 16-byte chunk of columns a lane, a wavefront
-// every fourth row, four of its rows at a time. Bound by memory. (WIDE: X and dY, and
+// every fourth row, eight of its rows at a time. Bound by memory. (WIDE: X and dY, and
 // b2, take 16-byte loads.)
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void sort_kernel(const SortArgs a) {
-  constexpr int VEC = 16 / sizeof(T), U = 4;
+  constexpr int VEC = 16 / sizeof(T), U = 8;
+  static_assert(kSortRows % (4 * U) == 0 && kSortRows <= 256);
   __shared__ float part[4][64 * VEC];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   ProductArgs g{};
@@ -295,6 +296,16 @@ __global__ __launch_bounds__(256) void sort_kernel(const SortArgs a) {
   const int64_t end = first + kSortRows < sp.hi ? first + kSortRows : sp.hi;
   const int64_t c0 = static_cast<int64_t>(blockIdx.y) * kSortCols;
   const int64_t c1 = c0 + kSortCols < a.ldd ? c0 + kSortCols : a.ldd;
+  // row 4·i of the wavefront's in lane i: its token (T: none) and its weight
+  int token = static_cast<int>(a.T);
+  float weight = 0.0f;
+  if (lane < kSortRows / 4 && first + wave + 4 * lane < end) {
+    const int entry = a.order[first + wave + 4 * lane];
+    if (entry >= 0 && entry / a.k < a.T) {
+      token = entry / a.k;
+      if (a.sums) weight = a.weights[entry];
+    }
+  }
   auto chunk = [&](const void* p, int64_t ld, int64_t row, int64_t c) __attribute__((always_inline)) {
     const T* q = static_cast<const T*>(p) + row * ld + c;
     if constexpr (WIDE) return *reinterpret_cast<const u32x4*>(q);
@@ -311,19 +322,16 @@ __global__ __launch_bounds__(256) void sort_kernel(const SortArgs a) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) b2[j] = to_float(e[j]);
     }
-    for (int64_t p0 = first + wave; p0 < end; p0 += 4 * U) {
+    int i0 = 0;
+    for (int64_t p0 = first + wave; p0 < end; p0 += 4 * U, i0 += U) {
       u32x4 x[U], y[U];
       float w[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int64_t p = p0 + 4 * u;
         x[u] = y[u] = u32x4{};
-        w[u] = 0.0f;
-        if (p >= end) continue;
-        const int entry = a.order[p];
-        const int64_t t = entry < 0 ? a.T : entry / a.k;
+        const int64_t t = __builtin_amdgcn_readlane(token, i0 + u);
+        w[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), i0 + u));
         if (t >= a.T || !in) continue;
-        if (a.sums) w[u] = a.weights[entry];
         y[u] = chunk(a.dY, a.lddy, t, c);
         if (a.X) x[u] = chunk(a.X, a.ldx, t, c);
       }
