@@ -1,21 +1,24 @@
 // Routing of tokens to experts: scores, choice, the lists of the experts' rows,
 // and the gradient of the weights.
 //
-// One wavefront a token. Lane l holds the logits of experts l, l + 64, …; the
-// choice is k times the largest key over the wavefront (lane moves within rows of 16,
-// then four scalars), whose lowest index the lanes' votes give, register by
-// register. The lists are a counting sort over at most kMaxBlocks blocks of tokens:
-// the block that routes its tokens counts them per expert; then each block sums
-// what the blocks before it counted and ranks its entries, 64 at a time, by the
-// votes on their experts' bits, so that an expert's entries keep their order.
-// Two launches; one for a few tokens.
+// A token's lanes hold its logits; the choice is k times the largest key over them (lane
+// moves within rows of 16), and of equals the lowest index. Up to 256 experts, 16
+// slots and groups of whole lanes: a row of 16 lanes a token, four tokens a wavefront,
+// neighbouring experts in a lane; otherwise, and for a few tokens, a wavefront a
+// token, experts l, l + 64, … in lane l. The lists are a counting sort over at most
+// kMaxBlocks blocks of tokens: the block that routes its tokens counts them per expert;
+// then each block sums what the blocks before it counted and ranks its entries, 64 at a
+// time, by the votes on their experts' bits, so that an expert's entries keep their
+// order. Two launches; one for a few tokens.
 //
-// Bound by the latency of the choice's chain of maxima: 16384 tokens, 8 of 256 experts
-// in 8 groups, with their lists.
+// Bound by the instructions of the choice: 16384 tokens, 8 of 256 experts in 8 groups, in
+// bf16: 15 µs (27 with a wavefront a token), the lists 10 (each block reads all
+// blocks' counts), the gradient 9 (11).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cstdint>
+#include <utility>
 
 #include "layer_kernels.h"
 #include "layer_math.hpp"
@@ -85,6 +88,37 @@ __device__ __forceinline__ float wave_sum(float v) {
   return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
 
+// The same over the 16 lanes of a row.
+__device__ __forceinline__ int32_t row_max(int32_t v) {
+  v = max(v, moved<0xb1>(v));
+  v = max(v, moved<0x4e>(v));
+  v = max(v, moved<0x141>(v));
+  return max(v, moved<0x140>(v));
+}
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, moved<0xb1>(v));
+  v = fmaxf(v, moved<0x4e>(v));
+  v = fmaxf(v, moved<0x141>(v));
+  return fmaxf(v, moved<0x140>(v));
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v += moved<0xb1>(v);
+  v += moved<0x4e>(v);
+  v += moved<0x141>(v);
+  return v + moved<0x140>(v);
+}
+// A token's lanes: a wavefront's, or a row's.
+template <bool ROW, typename V>
+__device__ __forceinline__ V token_max(V v) {
+  if constexpr (ROW) return row_max(v);
+  else return wave_max(v);
+}
+template <bool ROW>
+__device__ __forceinline__ float token_sum(float v) {
+  if constexpr (ROW) return row_sum(v);
+  else return wave_sum(v);
+}
+
 // exp(x − m) where m is the largest of the values: 1 for the largest, +inf included.
 __device__ __forceinline__ float exp_below(float x, float m) { return x == m ? 1.0f : expf(x - m); }
 
@@ -102,8 +136,8 @@ struct Shares {
   float score;   // sigmoid: the score
   float top, total;  // softmax: the largest logit, Σ exp(logit − top) over all
 };
-// all(f): f over this lane's logits of the row.
-template <int EPL>
+// x: this lane's logits of the row.
+template <bool ROW, int EPL>
 __device__ __forceinline__ Shares shares_of(int score, int renormalise, const float (&x)[EPL],
                                             float chosen, bool live) {
   Shares r{0.0f, 0.0f, 0.0f, 1.0f};
@@ -112,28 +146,28 @@ __device__ __forceinline__ Shares shares_of(int score, int renormalise, const fl
     r.score = 1.0f / (1.0f + expf(-chosen));
     r.part = live ? r.score : 0.0f;
     if (renormalise) {
-      const float top = wave_max(live ? chosen : ninf);
+      const float top = token_max<ROW>(live ? chosen : ninf);
       const float e = live ? sigmoid_ratio(chosen, top) : 0.0f;
-      const float total = wave_sum(e);
+      const float total = token_sum<ROW>(e);
       r.part = live ? e / total : 0.0f;
     }
     return r;
   }
   if (renormalise) {     // the softmax over the chosen alone
-    const float top = wave_max(live ? chosen : ninf);
+    const float top = token_max<ROW>(live ? chosen : ninf);
     const float e = live ? exp_below(chosen, top) : 0.0f;
-    const float total = wave_sum(e);
+    const float total = token_sum<ROW>(e);
     r.part = live ? e / total : 0.0f;
     return r;
   }
   float top = ninf;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) top = fmaxf(top, x[i]);
-  r.top = wave_max(top);
+  r.top = token_max<ROW>(top);
   float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) sum += x[i] > ninf ? exp_below(x[i], r.top) : 0.0f;
-  r.total = wave_sum(sum);
+  r.total = token_sum<ROW>(sum);
   r.part = live ? exp_below(chosen, r.top) / r.total : 0.0f;
   return r;
 }
@@ -284,7 +318,7 @@ __device__ __forceinline__ int route_row(const gt_route_args& a, const Runs<EPL>
       }
     }
   }
-  const Shares sh = shares_of<EPL>(a.score, a.renormalise, x, chosen, mine >= 0);
+  const Shares sh = shares_of<false, EPL>(a.score, a.renormalise, x, chosen, mine >= 0);
   if (lane < k) {
     a.experts[t * k + lane] = mine;
     a.weights[t * k + lane] = a.scale * sh.part;
@@ -323,6 +357,116 @@ __global__ __launch_bounds__(64 * kWaves) void route_kernel(const RouteArgs r) {
                      [&](int64_t, int e) {
                        if (e >= 0) atomicAdd(&hist[e], 1);   // whole numbers: any order gives the same
                      });
+  __syncthreads();
+  for (int e = threadIdx.x; e < E; e += 64 * kWaves)
+    r.counts[static_cast<int64_t>(blockIdx.x) * E + e] = hist[e];
+}
+
+// KPL values from p, the first n of them; `none` beyond.
+template <typename T, int KPL>
+__device__ __forceinline__ void load_run(const T* p, int n, float none, float (&v)[KPL]) {
+  T e[KPL];
+  if (n >= KPL) {
+    __builtin_memcpy(e, p, sizeof(e));   // at any alignment
+  } else {
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) e[i] = i < n ? p[i] : T(0);
+  }
+#pragma unroll
+  for (int i = 0; i < KPL; ++i) v[i] = i < n ? to_float(e[i]) : none;
+}
+
+template <typename F, int... I>
+__device__ __forceinline__ void for_each(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
+// Four tokens a wavefront, a row of 16 lanes each, KPL neighbouring experts a lane: the
+// instructions of a maximum, a vote or an exponential serve four tokens, for those
+// of looking through a lane's KPL keys. Serves up to 256 experts and 16 slots, groups of
+// whole lanes (a power of two).
+template <typename T, int KPL>
+__global__ __launch_bounds__(64 * kWaves) void route_quad_kernel(const RouteArgs r) {
+  __shared__ int hist[16 * KPL];
+  const gt_route_args& a = r.a;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15;
+  const int E = a.E, k = a.k, e0 = l * KPL;
+  for (int e = threadIdx.x; e < E; e += 64 * kWaves) hist[e] = 0;
+  float bias[KPL];
+  load_run<float, KPL>(a.bias + e0, a.bias ? E - e0 : 0, 0.0f, bias);
+  const int parts = a.groups > 1 ? E / a.groups / KPL : 1;   // lanes of a group
+  __syncthreads();
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * r.tokens;
+  const int64_t t1 = t0 + r.tokens < a.T ? t0 + r.tokens : a.T;
+  for (int64_t tw = t0 + wave * 4; tw < t1; tw += kWaves * 4) {
+    const int64_t t = tw + (lane >> 4);
+    const bool there = t < t1;
+    const T* row = static_cast<const T*>(a.logits) + (there ? t : tw) * a.ldl;
+    float x[KPL];
+    int32_t key[KPL];
+    load_run<T, KPL>(row + e0, E - e0, -__builtin_inff(), x);
+#pragma unroll
+    for (int i = 0; i < KPL; ++i)   // (a NaN is never chosen and has no share)
+      if (x[i] != x[i]) x[i] = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) {
+      const float v = x[i] + bias[i];
+      key[i] = v == v ? ordered(v) : kNone;
+    }
+    if (a.groups > 1) {
+      Best best{kNone, kNone};
+#pragma unroll
+      for (int i = 0; i < KPL; ++i) best.add(key[i]);
+      if (parts > 1) best.add(moved<0xb1>(best.a), moved<0xb1>(best.b));
+      if (parts > 2) best.add(moved<0x4e>(best.a), moved<0x4e>(best.b));
+      if (parts > 4) best.add(moved<0x141>(best.a), moved<0x141>(best.b));
+      const float s = unordered(best.a) + unordered(best.b);   // (NaN: +inf and −inf in one run)
+      const int32_t own = e0 < E && s == s ? ordered(s) : kNone;
+      int better = 0;   // lanes of better groups
+      const int mine = l / parts * parts;
+      auto against = [&](auto o) __attribute__((always_inline)) {
+        constexpr int O = decltype(o)::value;
+        if (O < E / KPL) {
+          const int32_t v = moved<0x150 + O>(own);   // lane O's of each row
+          better += v > own || (v == own && O < mine) ? 1 : 0;
+        }
+      };
+      for_each(against, std::make_integer_sequence<int, 16>{});
+      if (better >= a.keep * parts) {
+#pragma unroll
+        for (int i = 0; i < KPL; ++i) key[i] = kNone;
+      }
+    }
+    int slot = -1;
+    for (int s = 0; s < k; ++s) {
+      int32_t mine = key[0];
+#pragma unroll
+      for (int i = 1; i < KPL; ++i) mine = max(mine, key[i]);
+      const int32_t m = row_max(mine);
+      if (__ballot(m != kNone) == 0) break;
+      // the lowest lane that has it takes its lowest expert
+      const uint32_t have = static_cast<uint32_t>(__ballot(mine == m) >> (lane & 48)) & 0xffff;
+      bool open = m != kNone && l == __builtin_ctz(have);
+      int e = -1;
+#pragma unroll
+      for (int i = 0; i < KPL; ++i) {
+        const bool hit = open && key[i] == m;
+        e = hit ? e0 + i : e;
+        key[i] = hit ? kNone : key[i];
+        open = open && !hit;
+      }
+      e = row_max(e);
+      if (l == s) slot = e;
+    }
+    const bool live = slot >= 0 && there;
+    const float chosen = live ? to_float(row[slot]) : 0.0f;
+    const Shares sh = shares_of<true, KPL>(a.score, a.renormalise, x, chosen, live);
+    if (l < k && there) {
+      a.experts[t * k + l] = slot;
+      a.weights[t * k + l] = a.scale * sh.part;
+      if (live) atomicAdd(&hist[slot], 1);   // whole numbers: any order gives the same
+    }
+  }
   __syncthreads();
   for (int e = threadIdx.x; e < E; e += 64 * kWaves)
     r.counts[static_cast<int64_t>(blockIdx.x) * E + e] = hist[e];
@@ -463,7 +607,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const gt_route_grad_arg
   const bool live = e >= 0 && e < E;
   const float chosen = live ? to_float(static_cast<const T*>(a.logits)[t * a.ldl + e]) : 0.0f;
   const float g = live ? a.scale * a.dweights[t * k + lane] : 0.0f;
-  const Shares sh = shares_of<EPL>(a.score, a.renormalise, x, chosen, live);
+  const Shares sh = shares_of<false, EPL>(a.score, a.renormalise, x, chosen, live);
   // mean = Σ of the chosen's share·gradient
   const float mean = wave_sum(live ? sh.part * g : 0.0f);
   float d;
@@ -489,6 +633,57 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const gt_route_grad_arg
   }
 }
 
+// The same with a row of 16 lanes a token and KPL neighbouring experts a lane; the logits
+// are read where all of them count, in the softmax over all experts.
+template <typename T, int KPL>
+__global__ __launch_bounds__(256) void route_grad_quad_kernel(const gt_route_grad_args a) {
+  __shared__ float rows[16][16 * KPL];
+  const int lane = threadIdx.x & 63, l = lane & 15, e0 = l * KPL;
+  const int64_t tw = static_cast<int64_t>(blockIdx.x) * 16 + (threadIdx.x >> 6) * 4;
+  if (tw >= a.T) return;
+  const bool there = tw + (lane >> 4) < a.T;
+  const int64_t t = there ? tw + (lane >> 4) : tw;
+  const int E = a.E, k = a.k;
+  float* row = rows[threadIdx.x >> 4];
+  const T* logits = static_cast<const T*>(a.logits) + t * a.ldl;
+  const int e = l < k ? a.experts[t * k + l] : -1;
+  const bool live = e >= 0 && e < E;
+  const float chosen = live ? to_float(logits[e]) : 0.0f;
+  const float g = live ? a.scale * a.dweights[t * k + l] : 0.0f;
+  const bool all = a.score == GT_SCORE_SOFTMAX && !a.renormalise;
+  float x[KPL];
+#pragma unroll
+  for (int i = 0; i < KPL; ++i) x[i] = -__builtin_inff();
+  if (all) {
+    load_run<T, KPL>(logits + e0, E - e0, -__builtin_inff(), x);
+#pragma unroll
+    for (int i = 0; i < KPL; ++i)
+      if (x[i] != x[i]) x[i] = -__builtin_inff();
+  }
+  const Shares sh = shares_of<true, KPL>(a.score, a.renormalise, x, chosen, live);
+  const float mean = row_sum(live ? sh.part * g : 0.0f);
+  float d = sh.part * (a.renormalise ? g - mean : g);
+  if (a.score == GT_SCORE_SIGMOID) d *= 1.0f - sh.score;
+#pragma unroll
+  for (int i = 0; i < KPL; ++i)
+    row[e0 + i] = all && x[i] > -__builtin_inff() ? -mean * exp_below(x[i], sh.top) / sh.total : 0.0f;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (live) row[e] += d;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (!there) return;
+  T out[KPL];
+#pragma unroll
+  for (int i = 0; i < KPL; ++i) out[i] = from_float<T>(row[e0 + i]);
+  T* to = static_cast<T*>(a.dlogits) + t * a.lddl + e0;
+  if (e0 + KPL <= E) {
+    __builtin_memcpy(to, out, sizeof(out));   // at any alignment
+  } else {
+#pragma unroll
+    for (int i = 0; i < KPL; ++i)
+      if (e0 + i < E) to[i] = out[i];
+  }
+}
+
 // Tokens of a block: whole rounds of its wavefronts, at most kMaxBlocks blocks.
 int32_t block_tokens(int64_t T) {
   const int64_t each = (T + kMaxBlocks - 1) / kMaxBlocks;
@@ -501,6 +696,16 @@ bool few(int64_t T, int E, int k, int groups) {
   return T == 0 || (T <= 64 && T * k <= kEntries && group_floats(E, groups) * kWaves * 4 <= 48 * 1024);
 }
 
+// Experts a lane where a row of 16 lanes a token serves, 0 where it does not.
+int quad_experts(int E, int k) { return E > 256 || k > 16 ? 0 : E <= 64 ? 4 : E <= 128 ? 8 : 16; }
+int quad_experts(const gt_route_args& a) {
+  const int kpl = quad_experts(a.E, a.k);
+  if (kpl == 0) return 0;
+  const int size = a.E / a.groups, parts = size / kpl;
+  const bool lanes = size % kpl == 0 && (parts & (parts - 1)) == 0 && parts <= 8;
+  return a.groups == 1 || lanes ? kpl : 0;
+}
+
 template <typename T, int EPL>
 hipError_t route_by(const gt_route_args& a, void* ws, hipStream_t s) {
   RouteArgs r{a, static_cast<int32_t*>(ws), 0, 0};
@@ -509,24 +714,43 @@ hipError_t route_by(const gt_route_args& a, void* ws, hipStream_t s) {
     route_few_kernel<T, EPL><<<1, 64 * kWaves, lds, s>>>(r);
     return hipGetLastError();
   }
-  if (lds > 48 * 1024) {   // E + groups beyond 640: a launch may use more than its default LDS
-    const hipError_t e =
-        hipFuncSetAttribute(reinterpret_cast<const void*>(route_kernel<T, EPL>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
-    if (e != hipSuccess) return e;
-  }
   r.tokens = block_tokens(a.T);
   r.blocks = static_cast<int32_t>((a.T + r.tokens - 1) / r.tokens);
-  route_kernel<T, EPL><<<static_cast<unsigned>(r.blocks), 64 * kWaves, lds, s>>>(r);
+  const dim3 grid(static_cast<unsigned>(r.blocks)), block(64 * kWaves);
+  const int quad = quad_experts(a);
+  if (quad == 4) {
+    route_quad_kernel<T, 4><<<grid, block, 0, s>>>(r);
+  } else if (quad == 8) {
+    route_quad_kernel<T, 8><<<grid, block, 0, s>>>(r);
+  } else if (quad == 16) {
+    route_quad_kernel<T, 16><<<grid, block, 0, s>>>(r);
+  } else {
+    if (lds > 48 * 1024) {   // E + groups beyond 640: a launch may use more than its default LDS
+      const hipError_t e =
+          hipFuncSetAttribute(reinterpret_cast<const void*>(route_kernel<T, EPL>),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+      if (e != hipSuccess) return e;
+    }
+    route_kernel<T, EPL><<<grid, block, lds, s>>>(r);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  place_kernel<<<static_cast<unsigned>(r.blocks), kEntries, 0, s>>>(r);
+  place_kernel<<<grid, kEntries, 0, s>>>(r);
   return hipGetLastError();
 }
 
 template <typename T, int EPL>
 hipError_t grad_by(const gt_route_grad_args& a, hipStream_t s) {
-  route_grad_kernel<T, EPL>
+  const dim3 grid(static_cast<unsigned>((a.T + 15) / 16));
+  const int quad = quad_experts(a.E, a.k);
+  if (quad == 4)
+    route_grad_quad_kernel<T, 4><<<grid, 256, 0, s>>>(a);
+  else if (quad == 8)
+    route_grad_quad_kernel<T, 8><<<grid, 256, 0, s>>>(a);
+  else if (quad == 16)
+    route_grad_quad_kernel<T, 16><<<grid, 256, 0, s>>>(a);
+  else
+    route_grad_kernel<T, EPL>
       <<<static_cast<unsigned>((a.T + 3) / 4), 256, 4 * a.E * sizeof(float), s>>>(a);
   return hipGetLastError();
 }
