@@ -97,6 +97,11 @@ Stored stored(const void* ptr, int64_t ld, int64_t sgroup, int64_t groups, int64
   return s;
 }
 
+// The part of the groups that get no row, were the rows spread evenly.
+double no_row(const ProductArgs& a) {
+  return std::pow(1.0 - 1.0 / a.groups, static_cast<double>(a.M));
+}
+
 // Rows a workgroup of the kernel for a few rows takes, 0 where it does not serve: up to 4
 // rows, or up to 4 a group on average (the groups that get a row, were the rows
 // spread evenly), that fit its LDS.
@@ -106,13 +111,39 @@ int few_rows(const Product& p) {
   double each = static_cast<double>(a.M);
   if (a.groups > 0) {
     if (a.M > 4 * a.groups) return 0;
-    double none = 1.0;   // that a group gets no row
-    for (int64_t i = 0; i < a.M; ++i) none *= 1.0 - 1.0 / a.groups;
-    each = a.M / (a.groups * (1.0 - none));
+    each = a.M / (a.groups * (1.0 - no_row(a)));
   }
   const int rows = each <= 1.3 ? 1 : each <= 2.3 ? 2 : each <= 4.0 ? 4 : 0;
   if (rows == 0 || rows_lds(a.K, rows, p.a.e.epi == kEpiGated) > 128 * 1024) return 0;
   return a.M / rows + a.groups < 65536 ? rows : 0;
+}
+
+// K slices of that kernel. A workgroup, one a compute unit, draws its columns of W from
+// memory at 24 GB/s (30 gated, 35 in fp32, where a row gives two lines of memory) after
+// 3 µs, the whole chip at 5.2 TB/s, so W comes sooner if more of them share it, for the
+// launch that joins their sums and its host time: taken where a sixth is to be won
+// (bf16, W past the caches: 1×4096×4096 by 64 workgroups 22.4 µs, 256 in 4 slices
+// 15.5; 1×4096×11008 51.7 and 25.3; 1×11008×4096, 172 workgroups, 23.5 and in 2 slices 29.3).
+int rows_slices(const Product& p) {
+  const ProductArgs& a = p.a;
+  const bool gated = a.e.epi == kEpiGated;
+  const double each = static_cast<double>(a.K) * (gated ? 128 : 64) * size_of(p.dtype);
+  const double rows = a.groups > 0 ? std::min<double>(a.groups * (1.0 - no_row(a)), a.M)
+                                   : static_cast<double>((a.M + p.rows - 1) / p.rows);
+  const double shares = rows * a.tilesN, rate = p.dtype != GT_BF16 ? 35e3 : gated ? 30e3 : 24e3;
+  int best = 1;
+  double least = 0.0, alone = 0.0;
+  for (int z : {1, 2, 3, 4, 6, 8, 16}) {
+    const double rounds = std::ceil(shares * z / 256.0);
+    const double t = 3.0 * rounds + (z > 1 ? 4.5 : 0.0) +
+                     std::hypot(rounds * each / z / rate, shares * each / 5.2e6);
+    if (z == 1) alone = t;
+    if (z == 1 || (t < least && t < alone * 5 / 6)) {
+      best = z;
+      least = t;
+    }
+  }
+  return best;
 }
 
 // The kernel of 16 rows a workgroup: its tile rows at most.
@@ -174,12 +205,14 @@ constexpr double kReg[2][3][2] = {{{1.4, 2.0}, {1.4, 2.0}, {1.4, 2.0}},
 // joins them, the copies of operands that 16-byte loads do not serve and their launch.
 void choose(Product* p, bool may_split) {
   ProductArgs& a = p->a;
+  a.half = a.N;
+  a.e.ldpart = up(a.N, 4) * (a.e.epi == kEpiGated ? 2 : 1);
   if ((p->rows = few_rows(*p)) > 0) {
-    a.half = a.N;
-    a.splits = 1;
     a.tilesN = static_cast<int>((a.N + 63) / 64);
     a.tilesM = static_cast<int>(a.groups > 0 ? a.M / p->rows + std::min<int64_t>(a.groups, a.M)
                                              : (a.M + p->rows - 1) / p->rows);
+    a.splits = may_split ? rows_slices(*p) : 1;
+    p->part = a.splits > 1 ? a.splits * a.M * a.e.ldpart * 4 : 0;
     return;
   }
   const int64_t sz = size_of(p->dtype), bk = 128 / sz;
@@ -259,8 +292,6 @@ void choose(Product* p, bool may_split) {
       }
     }
   }
-  a.half = a.N;
-  a.e.ldpart = up(a.N, 4) * (gated ? 2 : 1);
   p->part = a.splits > 1 ? a.splits * a.M * a.e.ldpart * 4 : 0;
   if (p->rows > 0) {
     p->reg = p->tails = false;
@@ -290,6 +321,7 @@ void choose(Product* p, bool may_split) {
 
 hipError_t launch(const Product& p, const ProductArgs& a, hipStream_t s) {
   return p.rows == kSlimRows ? launch_slim(p.dtype, a, s)
+         : p.rows > 0        ? launch_rows(p.dtype, p.rows, a, s)
                              : launch_product(p.dtype, p.layout, p.tile, p.reg, a, s);
 }
 
@@ -298,10 +330,6 @@ int run(const Product& p, void* ws, hipStream_t s) {
   ProductArgs a = p.a;
   if (a.M == 0) return GT_OK;
   if (a.splits < 1) return fail("layer product: too many tiles");
-  if (p.rows > 0 && p.rows < kSlimRows) {
-    GT_TRY(launch_rows(p.dtype, p.rows, a, s), "layer product of a few rows");
-    return GT_OK;
-  }
   char* at = static_cast<char*>(ws);
   if (p.pad.n > 0) {
     PadJobs jobs = p.pad;

@@ -28,7 +28,8 @@ def test_route(L, case, dtype, kind):  # noqa: F811
 
 @pytest.mark.parametrize("pad", [0, 8, 5])
 @pytest.mark.parametrize("shape", [(5, 1, 1), (7, 65, 33), (16, 64, 16), (17, 100, 300), (40, 33, 1000),
-                                   (64, 200, 77), (6, 12, 2100), (31, 129, 512)], ids=str)
+                                   (64, 200, 77), (6, 12, 2100), (31, 129, 512), (1, 200, 4100), (3, 70, 5000), (2, 129, 3001),
+                                   (4, 64, 2056)], ids=str)
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=IDS.get)
 def test_linear(L, dtype, shape, pad):  # noqa: F811
     base.test_linear(L, dtype, shape, pad)
@@ -42,7 +43,7 @@ def test_linear_whole_numbers(L, case):  # noqa: F811
 
 @pytest.mark.parametrize("holes", [False, True])
 @pytest.mark.parametrize("pad", [0, 3])
-@pytest.mark.parametrize("case", [(48, 6, 2, 72, 40), (100, 8, 1, 130, 66), (37, 3, 2, 33, 129)], ids=str)
+@pytest.mark.parametrize("case", [(48, 6, 2, 72, 40), (100, 8, 1, 130, 66), (37, 3, 2, 33, 129), (2, 3, 2, 4100, 40), (1, 4, 2, 520, 2056)], ids=str)
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=IDS.get)
 def test_experts_and_their_gradients(L, dtype, case, pad, holes):  # noqa: F811
     base.test_experts_and_their_gradients(L, dtype, case, pad, holes)
