@@ -85,19 +85,20 @@ __global__ __launch_bounds__(256) void reduce_kernel(const ProductArgs a) {
   }
 }
 
-// The join of the last tiles' slices (the 256×256 tile, bf16), 256 threads a quad each.
-// Bound by memory and its launch: 14 µs for 64 tiles of 4 slices, in place of a round
-// of tiles of which 64 units were busy (the down product of 16384 rows of
-// 4096 × 2048 in 8 groups: 214 → 159 + 14 µs).
+// The join of the last tiles' slices, 256 threads a quad each. Bound by memory and its
+// launch: 14 µs for 64 tiles of 256×256 in 4 slices, in place of a round of tiles of which
+// 64 units were busy (the down product of 8192 rows of 4096 × 2048 in 8 groups:
+// 214 → 159 + 14 µs); 80 of 336 tiles of 128×128 in 3 slices 7 (1999×2623×3457 in bf16:
+// 71 → 57 + 7; 472×9008×1024 in fp32, 28 of 284: 130 → 88 in all).
+template <typename T, int TILE>
 __global__ __launch_bounds__(256) void tail_kernel(const ProductArgs a) {
-  using T = uint16_t;
-  constexpr int BM = kTile[0].BM, BN = kTile[0].BN;
+  constexpr int BM = kTile[TILE].BM, BN = kTile[TILE].BN;
   const bool gated = a.e.epi == kEpiGated;
   GroupTiles<BM> tiles(a);
   int rows = a.tilesM;
   if (a.groups > 0) rows = min(rows, tiles.total());
   const int nt = rows * a.tilesN;
-  constexpr int BK = kTile[0].KB / static_cast<int>(sizeof(T));
+  constexpr int BK = kTile[TILE].KB / static_cast<int>(sizeof(T));
   const Tail tail = tail_of(nt, static_cast<int>((a.K + BK - 1) / BK));
   const int at = static_cast<int>(blockIdx.y);
   if (tail.slices < 2 || at >= tail.left) return;
@@ -472,13 +473,20 @@ hipError_t launch_reduce(int dtype, const ProductArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_tail(const ProductArgs& a, hipStream_t s) {
-  constexpr int BM = kTile[0].BM, BN = kTile[0].BN;
+namespace {
+template <typename T, int TILE>
+hipError_t tail_by(const ProductArgs& a, hipStream_t s) {
   const int64_t tiles = static_cast<int64_t>(a.tilesM) * a.tilesN;
   // (with two slices at least, half the units' number of tiles at most)
-  const dim3 grid(BM * BN / 4 / 256, static_cast<unsigned>(std::min<int64_t>(tiles, kUnits / 2)));
-  tail_kernel<<<grid, 256, 0, s>>>(a);   // (tile 0 is bf16's)
+  const dim3 grid(kTile[TILE].BM * kTile[TILE].BN / 4 / 256,
+                  static_cast<unsigned>(std::min<int64_t>(tiles, kUnits / 2)));
+  tail_kernel<T, TILE><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
+}
+}  // namespace
+hipError_t launch_tail(int dtype, int tile, const ProductArgs& a, hipStream_t s) {
+  if (dtype != GT_BF16) return tail_by<float, 1>(a, s);   // (tile 0 is bf16's)
+  return tile == 0 ? tail_by<uint16_t, 0>(a, s) : tail_by<uint16_t, 1>(a, s);
 }
 
 hipError_t launch_act_grad(int dtype, const ActGradArgs& a, hipStream_t s) {

@@ -258,11 +258,16 @@ void choose(Product* p, bool may_split) {
         double cost = copy + std::hypot(each * busy, memory) + c.fixed * rounds;
         if (z > 1) cost += 4.5 + 2.0 * z * a.M * wide * 4 / 6.0e6;
         bool tails = false;
-        if (t == 0 && z == 1 && may_tail && tiles < kMaxExtent) {   // the last tiles in slices
+        // the last tiles in slices (with groups, whose tiles are a guess, of the largest only)
+        if ((t == 0 || (t == 1 && a.groups == 0)) && z == 1 && may_tail && tiles < kMaxExtent) {
           const Tail tail = tail_of(static_cast<int>(tiles), static_cast<int>(stages));
-          const double cut = copy + std::hypot(c.shared * (stages * (tail.full / kUnits) +
-                                                           (stages + tail.slices - 1) / tail.slices), memory) +
-                             c.fixed * (tail.full / kUnits + 1) + 6.0 +
+          const int64_t q = tail.full / kUnits, slice = (stages + tail.slices - 1) / tail.slices;
+          // (where two share a unit, one tile or a slice may be left alone)
+          const double work = c.resident == 1 ? c.shared * (stages * q + slice)
+                              : q % 2 == 1    ? c.shared * (stages * (q - 1) + 2 * slice) +
+                                                 c.alone * (stages - slice)
+                                              : c.shared * stages * q + c.alone * slice;
+          const double cut = copy + std::hypot(work, memory) + c.fixed * ((q + c.resident) / c.resident) + 6.0 +
                              2.0 * tail.left * tail.slices * s.BM * s.BN * 4 / 5.0e6;
           if (tail.slices > 1 && cut < cost) {
             tails = true;
@@ -351,7 +356,7 @@ int run(const Product& p, void* ws, hipStream_t s) {
   }
   if (p.tails) a.tail = reinterpret_cast<float*>(at);
   GT_TRY(launch(p, a, s), "layer product");
-  if (p.tails) GT_TRY(launch_tail(a, s), "joining the last tiles");
+  if (p.tails) GT_TRY(launch_tail(p.dtype, p.tile, a, s), "joining the last tiles");
   return GT_OK;
 }
 

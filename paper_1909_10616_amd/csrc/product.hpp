@@ -580,7 +580,12 @@ __device__ __forceinline__ void epilogue_sums(const ProductArgs& a, const EpiPla
 
 // ---- the kernel ------------------------------------------------------------
 
-// Measured (bf16, one MI355X): see the instances' list in product_inst.hip.
+// Bound by the matrix pipes and the clock they leave where the tiles fill the chip (bf16,
+// 256×256: 4096×4096×4096 116 µs, 1,180 TFLOP/s, either gradient; 4096×11008×4096
+// with bias, GELU and kept pre-activations 335), by the operands' way into LDS in smaller
+// tiles, and by the launch, its first loads and its epilogue (5 to 8 µs) where K is short.
+// 8 wavefronts of 128×64 in the large tile took 135 → 115 µs against 4 of 128×128, whose
+// 256 accumulators left the other registers no room.
 template <int DT, int I, bool AX, bool BX, int BM, int BN, int NWM, int NWN, int KB, int NS, bool REG, int EPI>
 __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductArgs a) {
   using T = typename Elem<DT>::T;
@@ -620,7 +625,7 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   // launch has tiles for every way the rows may be spread; those past the last row's
   // end here, and the others are dealt out to the XCDs without them.
   int tm, tn;
-  constexpr bool TAILS = BM == 256 && (EPI == kEpiPlain || EPI == kEpiLinear || EPI == kEpiGated);
+  constexpr bool TAILS = BM >= 128 && !REG && (EPI == kEpiPlain || EPI == kEpiLinear || EPI == kEpiGated);
   int slice = 0, slices = 1, tail_at = -1;   // of the last tiles
   int64_t m0, mend = a.M;
   int group = 0;

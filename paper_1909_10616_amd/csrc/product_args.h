@@ -64,8 +64,7 @@ struct ProductArgs {
   Epilogue e;
 };
 
-// The tiles that are left when the compute units have had the same number of tiles of 0's
-// size each would keep a few of them busy for as long again. They are cut into K slices
+// The large tiles that are left when the compute units have had the same number each would keep a few of them busy for as long again. They are cut into K slices
 // instead, as many as the units take at once (at most kTailSlices, and no fewer than 4
 // stages each); their sums go to `tail`, [tile of the left][slice][BM][BN], and a
 // launch of its own joins them. The kernel finds out itself, since with groups
@@ -110,7 +109,7 @@ hipError_t launch_product(int dtype, int layout, int tile, bool reg, const Produ
                           hipStream_t s);
 
 // Joins the K slices of the last tiles (a.tail) with the epilogue a.e.epi.
-hipError_t launch_tail(const ProductArgs& a, hipStream_t s);
+hipError_t launch_tail(int dtype, int tile, const ProductArgs& a, hipStream_t s);
 
 // The product of a few rows (1, 2 or 4 a workgroup; of a group, with groups along m) with a
 // matrix, kXW with kEpiLinear or kEpiGated, in one launch: tilesN of 64 columns, tilesM of

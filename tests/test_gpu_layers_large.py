@@ -58,6 +58,26 @@ def test_linear(L, gated, odd):
     untouched(pbuf, M, wide)
 
 
+@pytest.mark.parametrize("dtype,M,N,K,gated", [(F32, 1100, 1104, 2056, False), (F32, 1100, 1099, 2060, False),
+                                               (F32, 1100, 560, 2056, True), (F32, 1100, 555, 2056, True),
+                                               (F32, 2304, 2304, 520, False), (BF16, 1999, 2624, 3464, False),
+                                               (BF16, 1999, 2621, 3464, False)])
+def test_linear_smaller_tiles(L, dtype, M, N, K, gated):
+    print(f"linear {dtype} {M} {N} {K} gated {gated}", flush=True)
+    gen = torch.Generator().manual_seed(N)
+    wide = 2 * N if gated else N
+    X, W, R = (ints(gen, *shape, most=1).to(dtype) for shape in ((M, K), (K, wide), (M, N)))
+    ybuf, Y = framed(F32, M, N, N + 3)
+    pbuf, P = framed(F32 if dtype == F32 else BF16, M, wide, wide + 5)
+    L.gt_linear(X, W, residual=R, act="relu", gated=gated, Y=Y, P=P)
+    p = X.float() @ W.float()
+    assert float(p.abs().max()) <= 256
+    assert torch.equal(Y, (p[:, :N].relu() * p[:, N:] if gated else p.relu()) + R.float())
+    assert torch.equal(P.float(), p)
+    untouched(ybuf, M, N)
+    untouched(pbuf, M, wide)
+
+
 @pytest.mark.parametrize("K", [4096, 4091])
 def test_linear_backward(L, K):
     M, N = 4340, 1040
