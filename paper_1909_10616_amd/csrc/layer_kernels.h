@@ -23,7 +23,7 @@ struct PadJob {
   int64_t ld, sgroup;     // of src
   int64_t ldd, half;      // of dst, groups one after the other
 };
-constexpr int kPadJobs = 3;
+constexpr int kPadJobs = 4;   // of two products
 struct PadJobs {
   PadJob job[kPadJobs];
   int n;

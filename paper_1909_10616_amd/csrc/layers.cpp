@@ -66,7 +66,8 @@ struct Product {
   int64_t pad_a = 0, pad_b = 0, part = 0;   // … and the bytes of that and of partial sums
   bool tails = false;     // `part` is the last tiles'
 
-  int64_t scratch() const { return up(pad_a, 256) + up(pad_b, 256) + up(part, 256); }
+  int64_t pads() const { return up(pad_a, 256) + up(pad_b, 256); }
+  int64_t scratch() const { return pads() + up(part, 256); }
 };
 
 // One operand as it is stored: whether 16-byte loads serve it (aligned rows of whole
@@ -305,12 +306,12 @@ void choose(Product* p, bool may_split) {
     return;
   }
   if (!p->reg) {
-    if (!sa.ok) {
+    if (!sa.ok && sa.bytes > 0) {
       p->pad.job[p->pad.n++] = sa.job;
       p->pad_a = sa.bytes;
       a.lda = sa.job.ldd;
     }
-    if (!sb.ok) {
+    if (!sb.ok && sb.bytes > 0) {
       p->pad.job[p->pad.n++] = sb.job;
       p->pad_b = sb.bytes;
       a.ldb = sb.job.ldd;
@@ -330,20 +331,31 @@ hipError_t launch(const Product& p, const ProductArgs& a, hipStream_t s) {
                              : launch_product(p.dtype, p.layout, p.tile, p.reg, a, s);
 }
 
+// A product's copies to aligned rows into its pads() bytes at `at`: their jobs, and the
+// operands that they become.
+void place_pads(const Product& p, char* at, ProductArgs* a, PadJobs* jobs) {
+  int n = 0;
+  auto place = [&](int64_t bytes) {
+    PadJob& j = jobs->job[jobs->n++] = p.pad.job[n++];
+    j.dst = at;
+    at += up(bytes, 256);
+    return j.dst;
+  };
+  if (p.pad_a) a->A = place(p.pad_a);
+  if (p.pad_b) a->B = place(p.pad_b);
+}
+
 // Launches a product; ws: its scratch() bytes.
 int run(const Product& p, void* ws, hipStream_t s) {
   ProductArgs a = p.a;
   if (a.M == 0) return GT_OK;
   if (a.splits < 1) return fail("layer product: too many tiles");
   char* at = static_cast<char*>(ws);
-  if (p.pad.n > 0) {
-    PadJobs jobs = p.pad;
-    int n = 0;
-    if (p.pad_a) a.A = jobs.job[n++].dst = at;
-    at += up(p.pad_a, 256);
-    if (p.pad_b) a.B = jobs.job[n++].dst = at;
-    at += up(p.pad_b, 256);
+  if (p.pads() > 0) {
+    PadJobs jobs{};
+    place_pads(p, at, &a, &jobs);
     GT_TRY(launch_pad(p.dtype, jobs, s), "copy to aligned rows");
+    at += p.pads();
   }
   if (a.splits > 1) {
     a.e.part = reinterpret_cast<float*>(at);
@@ -476,7 +488,8 @@ struct LinearGrad {
   int64_t lddp = 0, wide = 0;
   Product dx, dw;
   // scratch
-  void *dP = nullptr, *rest = nullptr;   // rest: the products' own, one after the other
+  void *dP = nullptr, *rest = nullptr;   // rest: the products' partial sums, one after the other
+  char* pads = nullptr;                  // both products' copies to aligned rows
   float* sums = nullptr;
   int64_t bytes = 0;
 };
@@ -514,7 +527,7 @@ LinearGrad linear_grad(const gt_linear_grad_args& q, void* ws) {
     output(&a.e, q.dX, q.lddx, q.dtype == GT_F32);
     g.dx.own_a = g.own_dP;
     choose(&g.dx, true);
-    rest = std::max(rest, g.dx.scratch());
+    rest = std::max(rest, g.dx.part);
   }
   if (q.dW) {   // Xᵀ · dP
     g.dw.dtype = q.dtype;
@@ -530,8 +543,9 @@ LinearGrad linear_grad(const gt_linear_grad_args& q, void* ws) {
     output(&a.e, q.dW, q.lddw, q.dw_dtype == GT_F32);
     g.dw.own_b = g.own_dP;
     choose(&g.dw, true);
-    rest = std::max(rest, g.dw.scratch());
+    rest = std::max(rest, g.dw.part);
   }
+  if (g.dx.pads() + g.dw.pads() > 0) g.pads = s.take<char>(g.dx.pads() + g.dw.pads());
   if (rest) g.rest = s.take(rest);
   g.bytes = s.used;
   return g;
@@ -874,6 +888,13 @@ int linear_backward_impl(const gt_linear_grad_args* a, void* ws, int64_t ws_byte
     if (a->db)
       GT_TRY(launch_join(g.sums, (a->M + kActRows - 1) / kActRows, g.wide, nullptr, 1, 0, 1, 1, a->db, s),
              "gradient of the bias");
+  }
+  if (g.pads) {
+    PadJobs jobs{};
+    place_pads(g.dx, g.pads, &g.dx.a, &jobs);
+    place_pads(g.dw, g.pads + g.dx.pads(), &g.dw.a, &jobs);
+    g.dx.pad_a = g.dx.pad_b = g.dw.pad_a = g.dw.pad_b = 0;
+    GT_TRY(launch_pad(a->dtype, jobs, s), "copies to aligned rows");
   }
   if (a->dX) GT_CHECK(run(g.dx, g.rest, s));
   if (a->dW) GT_CHECK(run(g.dw, g.rest, s));
