@@ -87,6 +87,7 @@ class ExpertGrads(typing.NamedTuple):
 
 
 _lib = None
+_calls = {}   # entry point → its function and its scratch query
 
 
 def lib():
@@ -103,6 +104,7 @@ def lib():
             f.argtypes = [ctypes.POINTER(args), _P, _i64, _P]
             w = getattr(L, name + "_workspace")
             w.argtypes, w.restype = [ctypes.POINTER(args), ctypes.POINTER(_i64)], ctypes.c_int
+            _calls[name] = f, w
         _lib = L
     return _lib
 
@@ -123,25 +125,27 @@ def _type(t, name):
 
 
 def _tensor(t, name, like, shape, dtype=None):
-    """A tensor of this shape, type (like's unless given) and device whose rows are
+    """A tensor of this shape, type (like's unless given) and like's device whose rows are
     contiguous; its pointer and row stride."""
     if t.dtype is not (dtype or like.dtype):
         raise ValueError(f"{name} must be {dtype or like.dtype}")
-    if t.device != like.device or not t.is_cuda:
+    if t.device != like.device:
         raise ValueError(f"{name} must be a GPU tensor on {like.device}")
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    have = t.shape
+    if have != shape:
+        raise ValueError(f"{name} has shape {tuple(have)}, not {tuple(shape)}")
     st = t.stride()
     n = len(st)
-    if n == 0 or (t.shape[-1] != 1 and st[-1] != 1):
+    if n == 0 or (st[-1] != 1 and have[-1] != 1):
         raise ValueError(f"the rows of {name} must be contiguous")
+    cols = have[-1]
     if n == 1:
-        return t.data_ptr(), t.shape[0]
+        return t.data_ptr(), cols
     ld = st[-2]
-    if t.shape[-2] == 1 or t.shape[-1] == 0:
-        ld = max(ld, t.shape[-1])
-    if ld < t.shape[-1]:
-        raise ValueError(f"the rows of {name} must not overlap")
+    if ld < cols or cols == 0:
+        if have[-2] != 1 and cols != 0:
+            raise ValueError(f"the rows of {name} must not overlap")
+        ld = max(ld, cols)
     return t.data_ptr(), ld
 
 
@@ -170,22 +174,25 @@ def _call(name, a, like, workspace, stream):
     """Runs an entry point on like's device, with scratch of its own unless given."""
     import torch
     L = lib()
-    need = _i64()
     ref = ctypes.byref(a)
     with torch.cuda.device(like.device) if like.device.index != torch._C._cuda_getDevice() \
             else _NOTHING:
         if name in NO_SCRATCH:
             _check(getattr(L, name)(ref, _stream(stream)), name)
             return
-        _check(getattr(L, name + "_workspace")(ref, ctypes.byref(need)), name)
+        run, query = _calls[name]
+        need = _i64()
+        _check(query(ref, ctypes.byref(need)), name)
         n = need.value
-        if n and workspace is None:
+        if n == 0:
+            _check(run(ref, None, 0, _stream(stream)), name)
+            return
+        if workspace is None:
             workspace = _empty((n,), torch.uint8, like.device, stream)
-        elif n and (workspace.device != like.device or not workspace.is_contiguous()):
+        elif workspace.device != like.device or not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous, on the operands' device")
-        _check(getattr(L, name)(ref, workspace.data_ptr() if n else None,
-                                workspace.numel() * workspace.element_size() if n else 0,
-                                _stream(stream)), name)
+        _check(run(ref, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                   _stream(stream)), name)
 
 
 class _Nothing:
@@ -307,8 +314,8 @@ def gt_route(logits, k, bias=None, score="softmax", groups=1, keep=1, renormalis
     n = T * k
     dev = logits.device
     weights = _empty((T, k), torch.float32, dev, stream)
-    experts, place = _empty((2, T, k), torch.int32, dev, stream).unbind(0)
-    order, offsets = _empty((n,), torch.int32, dev, stream), _empty((E + 1,), torch.int32, dev, stream)
+    experts, place, order, offsets = _empty((3 * n + E + 1,), torch.int32, dev, stream).split((n, n, n, E + 1))
+    experts, place = experts.view(T, k), place.view(T, k)
     _call("gt_route", gt_route_args(T, E, k, groups, keep, dt, SCORES[score], int(bool(renormalise)),
                                     scale, x, ldl, b, weights.data_ptr(), experts.data_ptr(),
                                     offsets.data_ptr(), order.data_ptr(), place.data_ptr()),
