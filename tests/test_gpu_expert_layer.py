@@ -40,7 +40,8 @@ def test_gradients_are_autograds(X):
         a = torch.nn.functional.silu(p[:, :H]) * p[:, H:]
         h = h + share[:, s:s + 1] * ((a.unsqueeze(1) @ w["W2"][e]).squeeze(1) + w["b2"][e])
     want = h @ w["head"] + w["bias"]
-    assert float((Y.cpu().double() - want).abs().max()) <= 1e-5 * float(want.abs().max())
+    exact = want.detach()
+    assert float((Y.cpu().double() - exact).abs().max()) <= 1e-5 * float(exact.abs().max())
     (want * dY.cpu().double()).sum().backward()
     for n, t in w.items():
         g = got[n].cpu().double()
