@@ -182,15 +182,15 @@ double slim_cost(const Product& p, int64_t z) {
 // 48 shapes from 1×4096×4096 to 2048×4096×4096, 14 of them odd, in every layout and
 // type, each at every tile and 1 to 32 K slices (bf16, K = 4096, one slice:
 // 256×256 tiles 76 µs for 16 of them, 114 for 256; 128×128 43, 75 for 512; 64×64 28, 114
-// for 2048; 16×128 22, 221 for 4096). Of 376 choices 310 are within 5 % of the best form
-// measured, 345 within 10 %; the furthest are few rows whose K slices would save 3 to 5 µs
+// for 2048; 16×128 22, 221 for 4096). Of 376 choices five in six are within 5 % of the best form
+// measured, nine in ten within 10 %; the furthest are few rows whose K slices would save 3 to 5 µs
 // in a graph and cost as much of host time in a second launch without one.
 struct TileCost {
   double alone, shared, fixed;
   int resident;
 };
 constexpr TileCost kCost[2][kTiles] = {
-    {{0, 0, 0, 1}, {2.05, 2.0, 6, 2}, {0.78, 0.6, 5, 3}, {0.49, 0.41, 5, 2}},          // fp32
+    {{0, 0, 0, 1}, {2.05, 2.0, 6, 2}, {0.71, 0.59, 5, 3}, {0.49, 0.41, 5, 2}},         // fp32
     {{1.62, 1.62, 8, 1}, {0.64, 0.55, 4.3, 2}, {0.375, 0.25, 4.2, 3}, {0.28, 0.235, 4.3, 2}}  // bf16
 };
 
@@ -764,7 +764,7 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     e.zero_pad = 1;
     g.dh.own_a = true;
     choose(&g.dh, false);
-    const TileShape& t = kTile[g.dh.tile];
+    const TileShape t = tile_shape(q.dtype, g.dh.tile);
     // Σ dH·H of a row's tiles, then b2·dY of its columns' blocks
     g.ndot = static_cast<int64_t>(a.tilesN) * t.NWN;
     g.nb2 = q.b2 && q.dweights ? (g.ldd + 64 * vec - 1) / (64 * vec) : 0;
@@ -1023,7 +1023,7 @@ int experts_backward_impl(const gt_experts_grad_args* a, void* ws, int64_t ws_by
   if (g.dP) GT_CHECK(run(g.dh, g.rest, s));
   if (a->db1)
     GT_TRY(launch_join(g.colsum, 0, g.wide, a->offsets, a->E, g.R, kTile[g.dh.tile].BM,
-                       kTile[g.dh.tile].NWM, a->db1, s),
+                       tile_shape(a->dtype, g.dh.tile).NWM, a->db1, s),
            "gradient of b1");
   if (a->db2)
     GT_TRY(launch_join(g.sums, 0, a->D, a->offsets, a->E, g.R, kSortRows, 1, a->db2, s),

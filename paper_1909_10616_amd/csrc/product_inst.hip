@@ -33,7 +33,7 @@ hipError_t launch_with_lds(F fn, std::atomic<uint64_t>& attr, const ProductArgs&
 
 template <int TILE, bool REG, int EPI>
 hipError_t go(const ProductArgs& a, hipStream_t s) {
-  constexpr TileShape t = kTile[TILE];
+  constexpr TileShape t = tile_shape(LP_DT, TILE);
   constexpr int KB = REG ? 128 : t.KB, NS = REG ? 2 : t.NS;
   constexpr auto* fn = product_kernel<LP_DT, t.I, LP_LAY == kXtP, LP_LAY != kPWt, t.BM, t.BN, t.NWM,
                                       t.NWN, KB, NS, REG, EPI>;
