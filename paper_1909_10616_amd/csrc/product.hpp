@@ -383,7 +383,8 @@ struct EpiRows {
   // dH arrived: H = act(P) (times up), w the row's weight;
   // dP = w·dH·act'(P) (gated: ·up, and w·dH·act(gate) for up), Hw = w·H. Octets of columns that
   // all exist, the pre-activations of U rows loaded while the U rows before them are
-  // worked on.
+  // worked on. (16384 rows of 1024 × 1024, gated, bf16: 104 µs; 114 with U = 1, 141 with 4,
+  // which leaves one wavefront a SIMD, 122 with the rows' loads not ahead.)
   template <int ACT>
   __device__ __forceinline__ void slope_whole(EpiSums* sums) const {
     const Epilogue& e = a.e;
