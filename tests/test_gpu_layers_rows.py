@@ -47,3 +47,9 @@ def test_linear_whole_numbers(L, case):  # noqa: F811
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=IDS.get)
 def test_experts_and_their_gradients(L, dtype, case, pad, holes):  # noqa: F811
     base.test_experts_and_their_gradients(L, dtype, case, pad, holes)
+
+
+@pytest.mark.parametrize("case", [(40, 200, 3, 64, 48), (120, 300, 4, 72, 40), (300, 130, 3, 40, 24)], ids=str)
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=IDS.get)
+def test_many_experts(L, dtype, case):  # noqa: F811
+    base.test_experts_and_their_gradients(L, dtype, case, 3, True)
