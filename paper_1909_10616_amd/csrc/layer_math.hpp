@@ -188,4 +188,17 @@ __device__ __forceinline__ u32x4 load_chunk(const T* p, int64_t n) {
   return v;
 }
 
+// The inclusive prefix sum over the wavefront (all lanes active): lane moves within rows of
+// 16, then the rows' totals.
+__device__ __forceinline__ int wave_prefix(int v) {
+  const int lane = threadIdx.x & 63;
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);   // from 1, 2, 4, 8 lanes below
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  const int a = __builtin_amdgcn_readlane(v, 15), b = a + __builtin_amdgcn_readlane(v, 31),
+            c = b + __builtin_amdgcn_readlane(v, 47);
+  return v + (lane >= 48 ? c : lane >= 32 ? b : lane >= 16 ? a : 0);
+}
+
 }  // namespace gt

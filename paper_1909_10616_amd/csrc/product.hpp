@@ -84,19 +84,6 @@ __device__ __forceinline__ int64_t offset_at(const ProductArgs& a, int g, int64_
   return v < 0 ? 0 : v > most ? most : v;
 }
 
-// The inclusive prefix sum over the wavefront (all lanes active): lane moves within rows of
-// 16, then the rows' totals.
-__device__ __forceinline__ int wave_prefix(int v) {
-  const int lane = threadIdx.x & 63;
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);   // from 1, 2, 4, 8 lanes below
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
-  const int a = __builtin_amdgcn_readlane(v, 15), b = a + __builtin_amdgcn_readlane(v, 31),
-            c = b + __builtin_amdgcn_readlane(v, 47);
-  return v + (lane >= 48 ? c : lane >= 32 ? b : lane >= 16 ? a : 0);
-}
-
 // The groups' tiles of BM rows: up to 64 groups a lane each, loaded once; more, 64 at a time.
 template <int BM>
 struct GroupTiles {

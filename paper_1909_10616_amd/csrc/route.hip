@@ -12,7 +12,7 @@
 // order. Two launches; one for a few tokens.
 //
 // Bound by the instructions of the choice: 16384 tokens, 8 of 256 experts in 8 groups, in
-// bf16: 15 µs (27 with a wavefront a token), the lists 10 (each block reads all
+// bf16: 15 µs (27 with a wavefront a token), the lists 9 (each block reads all
 // blocks' counts), the gradient 9 (11).
 #include <hip/hip_runtime.h>
 
@@ -478,14 +478,9 @@ __device__ __forceinline__ void scan_experts(const int* total, int E, int* first
   int before = 0;
   for (int e0 = 0; e0 < E; e0 += 64) {
     const int v = e0 + lane < E ? total[e0 + lane] : 0;
-    int upto = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(upto, d);
-      if (lane >= d) upto += o;
-    }
+    const int upto = wave_prefix(v);
     if (e0 + lane < E) first[e0 + lane] = before + upto - v;
-    before += __shfl(upto, 63);
+    before += __builtin_amdgcn_readlane(upto, 63);
   }
   if (lane == 0) first[E] = before;
 }
