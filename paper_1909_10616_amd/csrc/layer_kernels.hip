@@ -37,7 +37,9 @@ __device__ __forceinline__ int group_of_row(const int32_t* offsets, int groups, 
 
 // ---- copies to aligned rows
 
-// One wavefront a row, a 16-byte chunk a lane. Bound by memory.
+// One wavefront a row, a 16-byte chunk a lane, all of a product's (or of two products')
+// operands in one launch. Bound by memory: 1999×3457 and 3457×2623 in bf16 12 µs, 5.3 TB/s
+// both ways.
 template <typename T>
 __global__ __launch_bounds__(256) void pad_kernel(const PadJobs jobs) {
   constexpr int VEC = 16 / sizeof(T);
@@ -59,6 +61,8 @@ __global__ __launch_bounds__(256) void pad_kernel(const PadJobs jobs) {
 
 // ---- the join of K slices
 
+// A quad of outputs a thread, the slices' sums in their order, then the product's epilogue.
+// Bound by its launch: 64×4096 in 4 slices (4 MB) 4 µs.
 template <typename T>
 __global__ __launch_bounds__(256) void reduce_kernel(const ProductArgs a) {
   const int64_t quads = (written<T>(a.e, a.N) + 3) / 4;
@@ -133,7 +137,8 @@ __global__ __launch_bounds__(256) void tail_kernel(const ProductArgs a) {
 // ---- the activation's gradient
 
 // 256 threads: 64 column quads (octets, WIDE), kActRows rows, four of them a thread: all its
-// loads are out before the first is used. Bound by memory.
+// loads are out before the first is used. Bound by memory: 4096×4096 in bf16 28 µs,
+// 3.6 TB/s (dP stored past the caches 27, and no less for both products after it).
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void act_grad_kernel(const ActGradArgs a) {
   constexpr int U = kActRows / 4, Q = WIDE ? 2 : 1;
@@ -232,7 +237,8 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const ActGradArgs a) {
 
 // ---- the join of column sums
 
-// 1024 threads: 64 columns of a group, a sixteenth of the partial rows each.
+// 1024 threads: 64 columns of a group, a sixteenth of the partial rows each. Bound by its
+// launch and the rows' chain of loads: 256 rows of 4096 5 µs, 32 groups of 2048 6.
 __global__ __launch_bounds__(1024) void join_kernel(const float* part, int64_t rows, int64_t wide,
                                                    const int32_t* offsets, int64_t most, int bm,
                                                    int per, float* out) {
@@ -279,8 +285,9 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* part, int64_t r
 // ---- sorted copies of rows, and what else dY's rows give
 
 // 256 threads: a block of rows of one group, a 16-byte chunk of columns a lane, a wavefront
-// every fourth row, eight of its rows at a time. Bound by memory. (WIDE: X and dY, and
-// b2, take 16-byte loads.)
+// every fourth row, eight of its rows at a time. Bound by memory, mostly its stores: 16384
+// rows of 1024 of both in bf16, 67 MB, 28.5 µs (31.5 with four rows at a time, their
+// tokens looked up in each). (WIDE: X and dY, and b2, take 16-byte loads.)
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void sort_kernel(const SortArgs a) {
   constexpr int VEC = 16 / sizeof(T), U = 8;
@@ -374,7 +381,9 @@ __global__ __launch_bounds__(256) void sort_kernel(const SortArgs a) {
 
 // ---- sums back into the tokens' order
 
-// A quad (octet, WIDE) of a token's columns a thread; the rows of four slots at a time.
+// A quad (octet, WIDE) of a token's columns a thread; the rows of four slots at a time. Bound
+// by memory: 4096 tokens of 2 slots and 2048 columns with a residual, 101 MB, 19.3 µs,
+// 5.2 TB/s; a single token 4.8, its launch and two loads in turn.
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
   constexpr int Q = WIDE ? 2 : 1;
@@ -431,6 +440,8 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
 
 // ---- the gradient of the routing weights
 
+// An entry a thread: the partial sums of its row in their order. Bound by its launch: 16384
+// rows of 18 sums 4.8 µs.
 __global__ __launch_bounds__(256) void weight_grad_kernel(const float* dot, int64_t ldot, int64_t n,
                                                           const int32_t* place,
                                                           const int32_t* offsets, int E,

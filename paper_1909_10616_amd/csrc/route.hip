@@ -556,7 +556,8 @@ __global__ __launch_bounds__(kEntries) void place_kernel(const RouteArgs r) {
   }
 }
 
-// A few tokens: everything in one block.
+// A few tokens: everything in one block. Bound by its launch and the chain of one token: 4
+// tokens, 6 of 64 experts, 4.8 µs.
 template <typename T, int EPL>
 __global__ __launch_bounds__(64 * kWaves) void route_few_kernel(const RouteArgs r) {
   extern __shared__ float lds[];
