@@ -200,6 +200,18 @@ __device__ __forceinline__ f32x4 residual_quad(const Epilogue& e, int64_t row, i
   return e.R ? load4(static_cast<const T*>(e.R) + row * e.ldr + n, left) : f32x4{};
 }
 
+// A quad of a K slice's sums (gated: and the up values') to its place in `part`. A quad
+// that only pads a row has none: a half of a row of `part` ends with N's last quad, and the
+// launch that joins the slices writes the padding itself.
+template <bool G>
+__host__ __device__ __forceinline__ void part_quad(const ProductArgs& a, int slice, int64_t row,
+                                                   int64_t col, f32x4 v, f32x4 u) {
+  if (col >= a.N) return;
+  float* part = a.e.part + (static_cast<int64_t>(slice) * a.M + row) * a.e.ldpart + col;
+  *reinterpret_cast<f32x4*>(part) = v;
+  if constexpr (G) *reinterpret_cast<f32x4*>(part + a.e.ldpart / 2) = u;
+}
+
 // Where a wavefront's tile lies.
 struct EpiPlace {
   int64_t row, row_end;  // its first row, and the first row that is not the group's

@@ -147,9 +147,7 @@ __global__ __launch_bounds__(64 * slim_waves(G)) void slim_kernel(const ProductA
     if constexpr (G) u += *reinterpret_cast<const f32x4*>(mine + (s * H + 1) * 1024);
   }
   if (a.splits > 1) {
-    float* part = a.e.part + (static_cast<int64_t>(z) * a.M + out) * a.e.ldpart + col;
-    *reinterpret_cast<f32x4*>(part) = v;
-    if constexpr (G) *reinterpret_cast<f32x4*>(part + a.e.ldpart / 2) = u;
+    part_quad<G>(a, z, out, col, v, u);
     return;
   }
   const int left = a.N - col < 4 ? static_cast<int>(a.N - col) : 4;
