@@ -129,7 +129,7 @@ struct raw8 {   // as they lie in memory
   u32x4 w[sizeof(T) / 2];
 };
 template <typename T>
-__device__ __forceinline__ oct open8(const raw8<T>& r) {
+__host__ __device__ __forceinline__ oct open8(const raw8<T>& r) {
   oct v;
   if constexpr (sizeof(T) == 4) {
     v.a = __builtin_bit_cast(f32x4, r.w[0]);
@@ -147,13 +147,13 @@ __device__ __forceinline__ oct open8(const raw8<T>& r) {
   return v;
 }
 template <typename T>
-__device__ __forceinline__ oct load8(const T* p) {
+__host__ __device__ __forceinline__ oct load8(const T* p) {
   raw8<T> r;
   __builtin_memcpy(&r, p, sizeof(r));
   return open8<T>(r);
 }
 template <typename T>
-__device__ __forceinline__ void store8(T* p, const oct& v) {
+__host__ __device__ __forceinline__ void store8(T* p, const oct& v) {
   if constexpr (sizeof(T) == 4) {
     __builtin_memcpy(p, &v.a, 16);
     __builtin_memcpy(p + 4, &v.b, 16);

@@ -224,6 +224,14 @@ struct EpiSums {
   f32x4 g, u;  // a lane's columns of dP, summed over its rows
 };
 
+// Rows that the epilogue turns at a time, a wavefront having `region` bytes of LDS for them.
+constexpr int epilogue_rows(int WM, int WN, int region, int I) {
+  const int fit = region / (WN * 4) / I * I, rows = fit < WM ? fit : WM;
+  return rows < 64 ? rows : 64;
+}
+// XOR of the 16-byte chunks of such a row r: r & this.
+constexpr int epilogue_xor(int WN) { return (WN / 4 < 16 ? WN / 4 : 16) - 1; }
+
 // RP rows of a wavefront's tile of WM×WN, row h + r of it in LDS at mine + r·WN·4.
 template <int DT, int EPI, int WM, int WN, int XM, int RP, int BN>
 struct EpiRows {
@@ -236,11 +244,11 @@ struct EpiRows {
   const char* mine;
   int lane;
 
-  __device__ __forceinline__ f32x4 chunk(int r, int c) const {
+  __host__ __device__ __forceinline__ f32x4 chunk(int r, int c) const {
     return *reinterpret_cast<const f32x4*>(mine + r * (WN * 4) + ((c ^ (r & XM)) << 4));
   }
   // the column of chunk c (gated: of the gate's)
-  __device__ __forceinline__ int64_t col(int c) const {
+  __host__ __device__ __forceinline__ int64_t col(int c) const {
     return p.col + (G || c < CH / 2 ? 0 : BN / 2 - WN / 2) + c * 4;
   }
 
@@ -253,12 +261,13 @@ struct EpiRows {
   // The residuals of U rows are loaded before the first of them is stored (an output may
   // be the residual itself) and while the U rows before them are worked on.
   template <int ACT>
-  __device__ __forceinline__ void whole() const {
+  __host__ __device__ __forceinline__ void whole() const {
     const Epilogue& e = a.e;
     constexpr int LR = (G ? CH / 2 : CH) / 2;   // lanes a row
     constexpr int STEP = 64 / LR;
     constexpr int U = EPI == kEpiPlain ? 1 : RP / STEP >= 4 ? 4 : RP / STEP >= 1 ? RP / STEP : 1;
     const int c = lane % LR * 2, first = lane / LR;
+    if (STEP > RP && first >= RP) return;   // (32 gated columns: 32 rows a step, of 16)
     const int64_t n = col(c), row0 = p.row + h + first;
     oct bv{}, bu{};
     const T* R = nullptr;
@@ -1000,11 +1009,7 @@ __global__ __launch_bounds__(64 * NWM * NWN) void product_kernel(const ProductAr
   // ---- epilogue: the wavefront's accumulators through its own share of LDS, RP
   // rows at a time, 16-byte chunks XOR-ed by the row.
   constexpr int REGION = NS * STAGE / NW;
-  constexpr int CH = WN / 4;                       // 16-byte fp32 chunks of a row
-  constexpr int XM = (CH < 16 ? CH : 16) - 1;
-  constexpr int RPX = REGION / (WN * 4) / I * I;
-  constexpr int RPM = RPX < WM ? RPX : WM;
-  constexpr int RP = RPM < 64 ? RPM : 64;
+  constexpr int XM = epilogue_xor(WN), RP = epilogue_rows(WM, WN, REGION, I);
   static_assert(RP >= I && WM % RP == 0, "epilogue rows");
   __syncthreads();
   char* mine = smem + wave * REGION;
