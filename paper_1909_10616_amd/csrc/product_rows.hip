@@ -24,6 +24,7 @@ namespace {
 
 constexpr int kRowWaves = 16;
 constexpr int kRowCols = 64;
+constexpr int kRowStep = 64;   // k of a wavefront's loads in flight, at most
 
 // AL: W's rows are 16-byte aligned and whole chunks: loads by descriptor, zero beyond W.
 template <int DT, int MR, bool G, bool AL, int CW>
@@ -35,7 +36,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const ProductArgs 
   constexpr int H = G ? 2 : 1;
   // loads of a half in flight, and as many being used
   constexpr int U = !AL || H * MR == 8 ? 2 : G ? 4 : 8;
-  extern __shared__ float lds[];        // X: [MR][K], then the wavefronts' sums
+  static_assert(kRowStep % (U * KL) == 0);
+  extern __shared__ float lds[];        // X: [MR][the slice's k], then the wavefronts' sums
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
   int64_t m0 = static_cast<int64_t>(blockIdx.y) * MR, mend = a.M;
   int group = 0;
@@ -80,11 +82,12 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const ProductArgs 
     }
   };
   if (k0 < ke) load(k0);
-  const int slice = ke - kz;
+  // (whole loads' k: beyond K X is zero as W is, or an infinite X would meet W's zeros)
+  const int slice = all * (z + 1) / a.splits * (U * KL) - kz;
   for (int i = threadIdx.x; i < MR * slice; i += 64 * kRowWaves) {
     const int m = i / slice, k = kz + i - m * slice;
     float x = 0.0f;
-    if (m0 + m < mend) {
+    if (m0 + m < mend && k < K) {
       int64_t row = m0 + m;
       bool ok = true;
       if (a.gather) {
@@ -107,7 +110,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const ProductArgs 
     if (k + STEP < ke) load(k + STEP);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int row = min(k + u * KL + lane / CL, ke - 1) - kz;   // (past the end: W is zero)
+      const int row = k + u * KL + lane / CL - kz;
       float x[MR];
 #pragma unroll
       for (int m = 0; m < MR; ++m) x[m] = lds[m * slice + row];
@@ -202,7 +205,8 @@ hipError_t rows_of(int rows, const ProductArgs& a, hipStream_t s) {
 }  // namespace
 
 int64_t rows_lds(int64_t K, int rows, bool gated) {
-  return std::max<int64_t>(rows * K, int64_t{kRowWaves} * (gated ? 2 : 1) * rows * 64) * 4;
+  const int64_t whole = (K + kRowStep - 1) / kRowStep * kRowStep;
+  return std::max<int64_t>(rows * whole, int64_t{kRowWaves} * (gated ? 2 : 1) * rows * 64) * 4;
 }
 
 hipError_t launch_rows(int dtype, int rows, const ProductArgs& a, hipStream_t s) {
