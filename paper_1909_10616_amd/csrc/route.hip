@@ -133,7 +133,7 @@ __device__ __forceinline__ float sigmoid_ratio(float x, float m) {
 // an expert), before `scale`, and what else the gradient needs.
 struct Shares {
   float part;    // the weight over scale
-  float score;   // sigmoid: the score
+  float rest;    // sigmoid: 1 − score, formed as σ(−x): the difference has no bits left from x = 17 on
   float top, total;  // softmax: the largest logit, Σ exp(logit − top) over all
 };
 // x: this lane's logits of the row.
@@ -143,8 +143,8 @@ __device__ __forceinline__ Shares shares_of(int score, int renormalise, const fl
   Shares r{0.0f, 0.0f, 0.0f, 1.0f};
   const float ninf = -__builtin_inff();
   if (score == GT_SCORE_SIGMOID) {
-    r.score = 1.0f / (1.0f + expf(-chosen));
-    r.part = live ? r.score : 0.0f;
+    r.rest = 1.0f / (1.0f + expf(chosen));
+    r.part = live ? 1.0f / (1.0f + expf(-chosen)) : 0.0f;
     if (renormalise) {
       const float top = token_max<ROW>(live ? chosen : ninf);
       const float e = live ? sigmoid_ratio(chosen, top) : 0.0f;
@@ -608,7 +608,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const gt_route_grad_arg
   const float mean = wave_sum(live ? sh.part * g : 0.0f);
   float d;
   if (a.score == GT_SCORE_SIGMOID)
-    d = sh.part * (1.0f - sh.score) * (a.renormalise ? g - mean : g);
+    d = sh.part * sh.rest * (a.renormalise ? g - mean : g);
   else
     d = sh.part * (a.renormalise ? g - mean : g);
 #pragma unroll
@@ -659,7 +659,7 @@ __global__ __launch_bounds__(256) void route_grad_quad_kernel(const gt_route_gra
   const Shares sh = shares_of<true, KPL>(a.score, a.renormalise, x, chosen, live);
   const float mean = row_sum(live ? sh.part * g : 0.0f);
   float d = sh.part * (a.renormalise ? g - mean : g);
-  if (a.score == GT_SCORE_SIGMOID) d *= 1.0f - sh.score;
+  if (a.score == GT_SCORE_SIGMOID) d *= sh.rest;
 #pragma unroll
   for (int i = 0; i < KPL; ++i)
     row[e0 + i] = all && x[i] > -__builtin_inff() ? -mean * exp_below(x[i], sh.top) / sh.total : 0.0f;
