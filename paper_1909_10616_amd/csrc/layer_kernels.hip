@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const ActGradArgs a) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           float val, slope;
-          act_both(a.act, gate[i][j][c], &val, &slope);
+          act_both<T>(a.act, gate[i][j][c], &val, &slope);
           g[j][c] = dy[i][j][c] * slope;
           u[j][c] = dy[i][j][c] * val;
         }

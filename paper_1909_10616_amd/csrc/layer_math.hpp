@@ -12,16 +12,38 @@ namespace gt {
 
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
+// Exponentials of the activations. x·log2 e rounds at 2^-24 of itself, and so does x²: the
+// instruction's exponential of either is off by up to 4e-6 of itself at x = −80 and 7e-6 at
+// x = −12. bf16 rounds at 2^-9; fp32 takes the library's exponential, and what x² lost.
+template <typename T>
+__device__ __forceinline__ float exp_minus(float x) {   // exp(−x)
+  if constexpr (sizeof(T) == 4)
+    return expf(-x);
+  else
+    return __builtin_amdgcn_exp2f(x * -1.4426950408889634f);
+}
+template <typename T>
+__device__ __forceinline__ float exp_square(float x) {   // exp(−x²/2)
+  if constexpr (sizeof(T) == 4) {
+    const float y = fminf(fabsf(x), 16.0f), s = y * y;   // (0 from 14.5 on)
+    return expf(-0.5f * s) * fmaf(-0.5f, fmaf(y, y, -s), 1.0f);
+  } else {
+    return __builtin_amdgcn_exp2f(x * x * -0.72134752044448171f);
+  }
+}
+
+template <typename T>
 __device__ __forceinline__ float sigmoid_of(float x) {
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.4426950408889634f));
+  return __builtin_amdgcn_rcpf(1.0f + exp_minus<T>(x));
 }
 
 // Φ(x), the normal distribution function, and *e = exp(−x²/2). For x < 0, Φ = q·e with
 // q a polynomial in t = 1/(1 + 0.3·|x|), fitted by least squares to the scaled
 // complementary error function at 4500 points of [0, 14] with weights that even
-// out its relative error (1.5e-7; 5e-7 as evaluated here): a dozen instructions and
+// out its relative error (1.5e-7; 5e-7 as evaluated here, beside e's): a dozen instructions and
 // one exponential that the slope shares, where the library's error function
 // takes two branches of about fifty.
+template <typename T>
 __device__ __forceinline__ float normal_cdf(float x, float* e) {
   const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.3f, 1.0f));
   float q = 0.03567453473806381f;
@@ -32,31 +54,33 @@ __device__ __forceinline__ float normal_cdf(float x, float* e) {
   q = fmaf(q, t, 0.09991396218538284f);
   q = fmaf(q, t, 0.12075387686491013f);
   q = fmaf(q, t, 0.11962930113077164f);
-  *e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448171f);
+  *e = exp_square<T>(x);
   const float tail = q * t * *e;
   return x < 0.0f ? tail : 1.0f - tail;
 }
 
-// act(x)
+// act(x), of operands of type T
+template <typename T>
 __device__ __forceinline__ float act_value(int act, float x) {
-  if (act == GT_ACT_SILU) return x * sigmoid_of(x);
+  if (act == GT_ACT_SILU) return x * sigmoid_of<T>(x);
   if (act == GT_ACT_GELU) {
     float e;
-    return x * normal_cdf(x, &e);
+    return x * normal_cdf<T>(x, &e);
   }
   if (act == GT_ACT_RELU) return x < 0.0f ? 0.0f : x;
   return x;
 }
 
 // act(x) and act'(x)
+template <typename T>
 __device__ __forceinline__ void act_both(int act, float x, float* value, float* slope) {
   if (act == GT_ACT_SILU) {
-    const float s = sigmoid_of(x);
+    const float s = sigmoid_of<T>(x);
     *value = x * s;
     *slope = s * (1.0f + x * (1.0f - s));
   } else if (act == GT_ACT_GELU) {
     float e;
-    const float c = normal_cdf(x, &e);
+    const float c = normal_cdf<T>(x, &e);
     *value = x * c;
     *slope = fmaf(x * 0.39894228040143268f, e, c);
   } else if (act == GT_ACT_RELU) {
@@ -164,12 +188,12 @@ __host__ __device__ __forceinline__ void store8(T* p, const oct& v) {
     __builtin_memcpy(p, &w, 16);
   }
 }
-template <int ACT>
+template <typename T, int ACT>
 __device__ __forceinline__ void act8(oct& v) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    v.a[i] = act_value(ACT, v.a[i]);
-    v.b[i] = act_value(ACT, v.b[i]);
+    v.a[i] = act_value<T>(ACT, v.a[i]);
+    v.b[i] = act_value<T>(ACT, v.b[i]);
   }
 }
 

@@ -173,7 +173,7 @@ __device__ __forceinline__ void linear_quad(const Epilogue& e, int64_t N, int64_
     if (gated) store4(p + N, u, left);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = act_value(e.act, v[i]);
+  for (int i = 0; i < 4; ++i) v[i] = act_value<T>(e.act, v[i]);
   if (gated) v *= u;
   v += r;
   const int64_t at = group * e.sY + row * e.ldy + n;
@@ -310,7 +310,7 @@ struct EpiRows {
           if constexpr (G) store8(P + a.N, u);
           P += STEP * e.ldp;
         }
-        if constexpr (ACT != GT_ACT_NONE) act8<ACT>(v);
+        if constexpr (ACT != GT_ACT_NONE) act8<T, ACT>(v);
         if constexpr (G) {
           v.a *= u.a;
           v.b *= u.b;
@@ -440,7 +440,7 @@ struct EpiRows {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             float val, sl;
-            act_both(ACT, gq[j], &val, &sl);
+            act_both<T>(ACT, gq[j], &val, &sl);
             const float wv = w * v[j], H = val * uq[j];
             dot += live ? v[j] * H : 0.0f;
             dgq[j] = live ? wv * uq[j] * sl : 0.0f;
@@ -498,7 +498,7 @@ struct EpiRows {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           float val, sl;
-          act_both(e.act, gate[i][j], &val, &sl);
+          act_both<T>(e.act, gate[i][j], &val, &sl);
           const float wv = w * v[j], H = val * up[i][j];
           const bool in = live && j < left;
           dot += in ? v[j] * H : 0.0f;
