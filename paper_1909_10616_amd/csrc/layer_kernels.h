@@ -50,7 +50,8 @@ struct ActGradArgs {
 hipError_t launch_act_grad(int dtype, const ActGradArgs& a, hipStream_t s);
 
 // out[g][n] = Σ of part's rows of group g, in order. Rows: with offsets, group
-// g's rows of tiles of `bm` rows, `per` partial rows each; without, all `rows`.
+// g's rows of tiles of `bm` rows, `per` partial rows each, of the `rows` that there are;
+// without, all `rows`.
 hipError_t launch_join(const float* part, int64_t rows, int64_t wide, const int32_t* offsets,
                        int groups, int64_t most, int bm, int per, float* out, hipStream_t s);
 

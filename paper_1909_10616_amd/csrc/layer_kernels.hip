@@ -257,8 +257,10 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* part, int64_t r
       for (int d = 1; d < 64; d <<= 1) before += __shfl_xor(before, d);
       if (threadIdx.x == 0) {
         const int64_t lo = clamp_offset(offsets[g], most), hi = clamp_offset(offsets[g + 1], most);
-        span[0] = before * per;
-        span[1] = span[0] + (hi > lo ? (hi - lo + bm - 1) / bm : 0) * per;
+        // (offsets that do not ascend may name more tiles than there are)
+        const int64_t own = hi > lo ? (hi - lo + bm - 1) / bm : 0;
+        span[0] = before * per < rows ? before * per : rows;
+        span[1] = (before + own) * per < rows ? (before + own) * per : rows;
       }
     }
     __syncthreads();

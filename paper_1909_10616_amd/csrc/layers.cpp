@@ -706,6 +706,7 @@ int experts_grad_checks(const gt_experts_grad_args* a, bool pointers) {
 
 struct ExpertsGrad {
   int64_t R, wide, ldd, ldp, ldh, ldo, ndot = 0, nb2 = 0;
+  int64_t colrows = 0, sumrows = 0;   // partial rows of db1 and of db2
   Product dh, dw2, dx, dw1;
   void *Xs = nullptr, *dYs = nullptr, *dP = nullptr, *Hw = nullptr, *rest = nullptr;
   float *dXs = nullptr, *dot = nullptr, *colsum = nullptr, *sums = nullptr;
@@ -770,7 +771,8 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
     g.nb2 = q.b2 && q.dweights ? (g.ldd + 64 * vec - 1) / (64 * vec) : 0;
     e.ldot = g.ndot + g.nb2;
     g.dot = e.dot = s.take<float>(g.R * e.ldot * 4);
-    if (q.db1) g.colsum = e.colsum = s.take<float>(static_cast<int64_t>(a.tilesM) * t.NWM * g.wide * 4);
+    g.colrows = static_cast<int64_t>(a.tilesM) * t.NWM;
+    if (q.db1) g.colsum = e.colsum = s.take<float>(g.colrows * g.wide * 4);
   }
   if (q.dW2) {
     ProductArgs& a = common(g.dw2, kXtP);
@@ -817,7 +819,8 @@ ExpertsGrad experts_grad(const gt_experts_grad_args& q, void* ws) {
   }
   const int64_t rest = std::max({g.dh.scratch(), g.dw2.scratch(), g.dx.scratch(), g.dw1.scratch()});
   if (rest) g.rest = s.take(rest);
-  if (q.db2) g.sums = s.take<float>((g.R / kSortRows + std::min<int64_t>(q.E, g.R)) * q.D * 4);
+  g.sumrows = g.R / kSortRows + std::min<int64_t>(q.E, g.R);
+  if (q.db2) g.sums = s.take<float>(g.sumrows * q.D * 4);
   g.bytes = s.used;
   return g;
 }
@@ -1022,11 +1025,11 @@ int experts_backward_impl(const gt_experts_grad_args* a, void* ws, int64_t ws_by
   GT_TRY(launch_sort(a->dtype, q, s), "sorting the rows");
   if (g.dP) GT_CHECK(run(g.dh, g.rest, s));
   if (a->db1)
-    GT_TRY(launch_join(g.colsum, 0, g.wide, a->offsets, a->E, g.R, kTile[g.dh.tile].BM,
+    GT_TRY(launch_join(g.colsum, g.colrows, g.wide, a->offsets, a->E, g.R, kTile[g.dh.tile].BM,
                        tile_shape(a->dtype, g.dh.tile).NWM, a->db1, s),
            "gradient of b1");
   if (a->db2)
-    GT_TRY(launch_join(g.sums, 0, a->D, a->offsets, a->E, g.R, kSortRows, 1, a->db2, s),
+    GT_TRY(launch_join(g.sums, g.sumrows, a->D, a->offsets, a->E, g.R, kSortRows, 1, a->db2, s),
            "gradient of b2");
   if (a->dweights)
     GT_TRY(launch_weight_grad(g.dot, g.ndot + g.nb2, g.ndot + g.nb2, a->place, a->offsets, a->E, g.R,
