@@ -10,6 +10,10 @@
 
 namespace gt {
 
+// A launch has fewer work-items along a dimension than this; the runtime takes more modulo
+// 2^32 and reports nothing.
+constexpr int64_t kMaxItems = int64_t{1} << 32;
+
 // Sums the K slices of a product (a.e.part) in slice order and applies the linear
 // epilogue of a.e to every row (with groups along m: below the last offset).
 hipError_t launch_reduce(int dtype, const ProductArgs& a, hipStream_t s);

@@ -268,19 +268,21 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* part, int64_t r
     r1 = span[1];
   }
   const int c = threadIdx.x & 63, part16 = threadIdx.x >> 6;
-  const int64_t n = static_cast<int64_t>(blockIdx.x) * 64 + c;
-  float s = 0.0f;
-  if (n < wide) {
+  for (int64_t n = static_cast<int64_t>(blockIdx.x) * 64 + c; n - c < wide; n += int64_t{gridDim.x} * 64) {
+    float s = 0.0f;
+    if (n < wide) {
 #pragma unroll 4
-    for (int64_t r = r0 + part16; r < r1; r += 16) s += part[r * wide + n];
-  }
-  sums[part16][c] = s;
-  __syncthreads();
-  if (part16 == 0 && n < wide) {
-    float t = 0.0f;
+      for (int64_t r = r0 + part16; r < r1; r += 16) s += part[r * wide + n];
+    }
+    sums[part16][c] = s;
+    __syncthreads();
+    if (part16 == 0 && n < wide) {
+      float t = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t += sums[i][c];
-    out[g * wide + n] = t;
+      for (int i = 0; i < 16; ++i) t += sums[i][c];
+      out[g * wide + n] = t;
+    }
+    __syncthreads();
   }
 }
 
@@ -502,28 +504,35 @@ hipError_t launch_tail(int dtype, int tile, const ProductArgs& a, hipStream_t s)
   return tile == 0 ? tail_by<uint16_t, 0>(a, s) : tail_by<uint16_t, 1>(a, s);
 }
 
-hipError_t launch_act_grad(int dtype, const ActGradArgs& a, hipStream_t s) {
-  if (a.M == 0) return hipSuccess;
-  const int cols = a.wide ? 512 : 256;
-  const dim3 grid(static_cast<unsigned>((a.M + kActRows - 1) / kActRows),
-                  static_cast<unsigned>((a.N + cols - 1) / cols));
-  if (dtype == GT_BF16) {
+namespace {
+template <typename T>
+hipError_t act_grad_by(const ActGradArgs& q, hipStream_t s) {
+  const int cols = q.wide ? 512 : 256;
+  const int64_t most = int64_t{kActRows} << 20;   // rows of a launch: 2^28 work-items
+  for (int64_t m = 0; m < q.M; m += most) {
+    ActGradArgs a = q;
+    a.M = std::min(most, q.M - m);
+    a.dY = static_cast<const T*>(q.dY) + m * q.lddy;
+    if (q.P) a.P = static_cast<const T*>(q.P) + m * q.ldp;
+    if (q.dP) a.dP = static_cast<T*>(q.dP) + m * q.lddp;
+    if (q.part) a.part = q.part + m / kActRows * (q.gated ? 2 * q.N : q.N);
+    const dim3 grid(blocks_for(a.M, kActRows), static_cast<unsigned>((a.N + cols - 1) / cols));
     if (a.wide)
-      act_grad_kernel<uint16_t, true><<<grid, 256, 0, s>>>(a);
+      act_grad_kernel<T, true><<<grid, 256, 0, s>>>(a);
     else
-      act_grad_kernel<uint16_t, false><<<grid, 256, 0, s>>>(a);
-  } else {
-    if (a.wide)
-      act_grad_kernel<float, true><<<grid, 256, 0, s>>>(a);
-    else
-      act_grad_kernel<float, false><<<grid, 256, 0, s>>>(a);
+      act_grad_kernel<T, false><<<grid, 256, 0, s>>>(a);
   }
   return hipGetLastError();
+}
+}  // namespace
+hipError_t launch_act_grad(int dtype, const ActGradArgs& a, hipStream_t s) {
+  if (a.M == 0) return hipSuccess;
+  return dtype == GT_BF16 ? act_grad_by<uint16_t>(a, s) : act_grad_by<float>(a, s);
 }
 
 hipError_t launch_join(const float* part, int64_t rows, int64_t wide, const int32_t* offsets,
                        int groups, int64_t most, int bm, int per, float* out, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>((wide + 63) / 64), static_cast<unsigned>(groups));
+  const dim3 grid(blocks_for(wide, 64), static_cast<unsigned>(groups));
   join_kernel<<<grid, 1024, 0, s>>>(part, rows, wide, offsets, most, bm, per, out);
   return hipGetLastError();
 }

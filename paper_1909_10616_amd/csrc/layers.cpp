@@ -17,6 +17,7 @@ namespace gt {
 namespace {
 
 constexpr int64_t kMaxExtent = int64_t{1} << 31;
+constexpr int64_t kMaxEntries = int64_t{1} << 30;    // rows of experts: counted by tiles of them in 32 bits
 constexpr int64_t kMaxElements = int64_t{1} << 45;   // of one array: no size below leaves 64 bits
 
 int fail(const std::string& what) {
@@ -116,6 +117,7 @@ int few_rows(const Product& p) {
   }
   const int rows = each <= 1.3 ? 1 : each <= 2.3 ? 2 : each <= 4.0 ? 4 : 0;
   if (rows == 0 || rows_lds(a.K, rows, p.a.e.epi == kEpiGated) > 128 * 1024) return 0;
+  if ((a.N + 63) / 64 * kRowThreads >= kMaxItems) return 0;
   return a.M / rows + a.groups < 65536 ? rows : 0;
 }
 
@@ -162,8 +164,9 @@ int64_t slim_rows(const ProductArgs& a) {
 double slim_cost(const Product& p, int64_t z) {
   const ProductArgs& a = p.a;
   const int64_t rows = slim_rows(a), cols = (a.N + 63) / 64;
-  if (a.M < 1 || rows >= 65536 || rows * cols >= kMaxExtent) return 0.0;
   const bool bf16 = p.dtype == GT_BF16, gated = a.e.epi == kEpiGated;
+  if (a.M < 1 || rows >= 65536 || rows * cols >= kMaxExtent || cols * 64 * slim_waves(gated) >= kMaxItems)
+    return 0.0;
   const int64_t step = bf16 ? 32 : 16, steps = (a.K + step - 1) / step, waves = slim_waves(gated);
   if (z > 1 && steps < 16 * z) return 0.0;
   const double each = static_cast<double>(((steps + z - 1) / z + waves - 1) / waves);
@@ -245,7 +248,8 @@ void choose(Product* p, bool may_split) {
       tm = std::max<int64_t>(g, a.M / s.BM + g / 2);
     }
     const int64_t tiles = tm * tn * (a.along_k ? a.groups : 1);
-    if (most * tn >= kMaxExtent) continue;
+    const TileShape waves = tile_shape(p->dtype, t);
+    if (most * tn >= kMaxExtent || (most * tn + kUnits) * 64 * waves.NWM * waves.NWN >= kMaxItems) continue;
     const TileCost& c = kCost[p->dtype == GT_BF16 ? 1 : 0][t];
     const double memory = static_cast<double>(a.M * a.K + std::min(bgroups, std::max<int64_t>(1, a.M)) * a.K * wide) * sz / 5.2e6;
     for (int reg = 0; reg < 2; ++reg) {
@@ -346,11 +350,15 @@ void place_pads(const Product& p, char* at, ProductArgs* a, PadJobs* jobs) {
   if (p.pad_b) a->B = place(p.pad_b);
 }
 
+// Whether a form serves a product (called before the first launch of its operator).
+int planned(const Product& p) {
+  return p.a.M > 0 && p.a.splits < 1 ? fail("layer product: too many tiles") : GT_OK;
+}
+
 // Launches a product; ws: its scratch() bytes.
 int run(const Product& p, void* ws, hipStream_t s) {
   ProductArgs a = p.a;
   if (a.M == 0) return GT_OK;
-  if (a.splits < 1) return fail("layer product: too many tiles");
   char* at = static_cast<char*>(ws);
   if (p.pads() > 0) {
     PadJobs jobs{};
@@ -560,7 +568,7 @@ int experts_checks(int64_t T, int64_t D, int64_t H, int E, int k, int dtype, int
   GT_CHECK(extent(H, 1, "H"));
   if (act & GT_ACT_GATED) GT_CHECK(extent(2 * H, 1, "2H"));
   if (E < 1 || E > 1024 || k < 1 || k > 64) return fail("experts: E is 1 … 1024, k 1 … 64");
-  if (T * k >= kMaxExtent) return fail("experts: T·k out of range");
+  if (T * k >= kMaxEntries) return fail("experts: T·k out of range");
   if (!dtype_ok(dtype) || !act_ok(act)) return fail("experts: unknown dtype or activation");
   if (T * k > kMaxElements / std::max(D, 2 * H) || D > kMaxElements / (2 * H) / E)
     return fail("experts: the rows or the matrices are too large");
@@ -857,6 +865,7 @@ int linear_workspace_impl(const gt_linear_args* a, int64_t* bytes) {
 int linear_impl(const gt_linear_args* a, void* ws, int64_t ws_bytes, void* stream) {
   GT_CHECK(linear_checks(a, true));
   Product p = linear_product(*a);
+  GT_CHECK(planned(p));
   GT_CHECK(scratch_ok(ws, ws_bytes, p.scratch()));
   return run(p, ws, static_cast<hipStream_t>(stream));
 }
@@ -872,6 +881,7 @@ int linear_backward_impl(const gt_linear_grad_args* a, void* ws, int64_t ws_byte
   GT_CHECK(linear_grad_checks(a, true));
   const hipStream_t s = static_cast<hipStream_t>(stream);
   LinearGrad g = linear_grad(*a, ws);
+  for (const Product* p : {&g.dx, &g.dw}) GT_CHECK(planned(*p));
   GT_CHECK(scratch_ok(ws, ws_bytes, g.bytes));
   if (g.dP || a->db) {
     ActGradArgs q{};
@@ -969,6 +979,7 @@ int experts_impl(const gt_experts_args* a, void* ws, int64_t ws_bytes, void* str
   if (a->T == 0) return GT_OK;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   Experts x = experts(*a, ws);
+  for (const Product* p : {&x.up, &x.down}) GT_CHECK(planned(*p));
   GT_CHECK(scratch_ok(ws, ws_bytes, x.bytes));
   GT_CHECK(run(x.up, x.rest, s));
   GT_CHECK(run(x.down, x.rest, s));
@@ -1001,6 +1012,7 @@ int experts_backward_impl(const gt_experts_grad_args* a, void* ws, int64_t ws_by
   GT_CHECK(experts_grad_checks(a, true));
   const hipStream_t s = static_cast<hipStream_t>(stream);
   ExpertsGrad g = experts_grad(*a, ws);
+  for (const Product* p : {&g.dh, &g.dw2, &g.dx, &g.dw1}) GT_CHECK(planned(*p));
   GT_CHECK(scratch_ok(ws, ws_bytes, g.bytes));
   SortArgs q{};
   q.X = a->dW1 ? a->X : nullptr;

@@ -122,6 +122,7 @@ hipError_t launch_tail(int dtype, int tile, const ProductArgs& a, hipStream_t s)
 // The product of a few rows (1, 2 or 4 a workgroup; of a group, with groups along m) with a
 // matrix, kXW with kEpiLinear or kEpiGated, in one launch: tilesN of 64 columns, tilesM of
 // `rows` rows. The LDS it takes holds the rows.
+constexpr int kRowThreads = 1024;
 int64_t rows_lds(int64_t K, int rows, bool gated);
 hipError_t launch_rows(int dtype, int rows, const ProductArgs& a, hipStream_t s);
 constexpr int slim_waves(bool gated) { return gated ? 8 : 16; }   // (as registers allow)

@@ -22,13 +22,13 @@
 namespace gt {
 namespace {
 
-constexpr int kRowWaves = 16;
+constexpr int kRowWaves = kRowThreads / 64;
 constexpr int kRowCols = 64;
 constexpr int kRowStep = 64;   // k of a wavefront's loads in flight, at most
 
 // AL: W's rows are 16-byte aligned and whole chunks: loads by descriptor, zero beyond W.
 template <int DT, int MR, bool G, bool AL, int CW>
-__global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const ProductArgs a) {
+__global__ __launch_bounds__(kRowThreads) void rows_kernel(const ProductArgs a) {
   using T = typename Elem<DT>::T;
   constexpr int VEC = Elem<DT>::VEC;
   constexpr int CL = CW / VEC;          // lanes a row of CW columns
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const ProductArgs 
   if (k0 < ke) load(k0);
   // (whole loads' k: beyond K X is zero as W is, or an infinite X would meet W's zeros)
   const int slice = all * (z + 1) / a.splits * (U * KL) - kz;
-  for (int i = threadIdx.x; i < MR * slice; i += 64 * kRowWaves) {
+  for (int i = threadIdx.x; i < MR * slice; i += kRowThreads) {
     const int m = i / slice, k = kz + i - m * slice;
     float x = 0.0f;
     if (m0 + m < mend && k < K) {
@@ -183,7 +183,7 @@ hipError_t rows_by(const ProductArgs& a, hipStream_t s) {
   }
   const dim3 grid(static_cast<unsigned>(a.tilesN), static_cast<unsigned>(a.tilesM),
                   static_cast<unsigned>(a.splits));
-  rows_kernel<DT, MR, G, AL, kRowCols><<<grid, 64 * kRowWaves, lds, s>>>(a);
+  rows_kernel<DT, MR, G, AL, kRowCols><<<grid, kRowThreads, lds, s>>>(a);
   return hipGetLastError();
 }
 

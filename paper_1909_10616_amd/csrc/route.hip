@@ -736,18 +736,27 @@ hipError_t route_by(const gt_route_args& a, void* ws, hipStream_t s) {
 }
 
 template <typename T, int EPL>
-hipError_t grad_by(const gt_route_grad_args& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>((a.T + 15) / 16));
-  const int quad = quad_experts(a.E, a.k);
-  if (quad == 4)
-    route_grad_quad_kernel<T, 4><<<grid, 256, 0, s>>>(a);
-  else if (quad == 8)
-    route_grad_quad_kernel<T, 8><<<grid, 256, 0, s>>>(a);
-  else if (quad == 16)
-    route_grad_quad_kernel<T, 16><<<grid, 256, 0, s>>>(a);
-  else
-    route_grad_kernel<T, EPL>
-      <<<static_cast<unsigned>((a.T + 3) / 4), 256, 4 * a.E * sizeof(float), s>>>(a);
+hipError_t grad_by(const gt_route_grad_args& q, hipStream_t s) {
+  const int quad = quad_experts(q.E, q.k);
+  const int64_t most = int64_t{1} << 24;   // tokens of a launch: 2^30 work-items
+  for (int64_t t = 0; t < q.T; t += most) {
+    gt_route_grad_args a = q;
+    a.T = std::min(most, q.T - t);
+    a.logits = static_cast<const T*>(q.logits) + t * q.ldl;
+    a.experts = q.experts + t * q.k;
+    a.dweights = q.dweights + t * q.k;
+    a.dlogits = static_cast<T*>(q.dlogits) + t * q.lddl;
+    const dim3 grid(static_cast<unsigned>((a.T + 15) / 16));
+    if (quad == 4)
+      route_grad_quad_kernel<T, 4><<<grid, 256, 0, s>>>(a);
+    else if (quad == 8)
+      route_grad_quad_kernel<T, 8><<<grid, 256, 0, s>>>(a);
+    else if (quad == 16)
+      route_grad_quad_kernel<T, 16><<<grid, 256, 0, s>>>(a);
+    else
+      route_grad_kernel<T, EPL>
+        <<<static_cast<unsigned>((a.T + 3) / 4), 256, 4 * a.E * sizeof(float), s>>>(a);
+  }
   return hipGetLastError();
 }
 
