@@ -167,6 +167,7 @@ double slim_cost(const Product& p, int64_t z) {
   const bool bf16 = p.dtype == GT_BF16, gated = a.e.epi == kEpiGated;
   if (a.M < 1 || rows >= 65536 || rows * cols >= kMaxExtent || cols * 64 * slim_waves(gated) >= kMaxItems)
     return 0.0;
+  if (a.K >= kMaxExtent / 2) return 0.0;   // (its k are 32-bit numbers, past the last by a step)
   const int64_t step = bf16 ? 32 : 16, steps = (a.K + step - 1) / step, waves = slim_waves(gated);
   if (z > 1 && steps < 16 * z) return 0.0;
   const double each = static_cast<double>(((steps + z - 1) / z + waves - 1) / waves);

@@ -1,5 +1,5 @@
-"""Extents whose work-items, taken as a launch, would pass 2^32: a quarter of a billion and more rows
-or columns of one value, whose results are known."""
+"""Extents whose work-items, taken as a launch, would pass 2^32, and sums of almost 2^31 terms: a
+quarter of a billion and more rows or columns of few values, whose results are known."""
 import pytest
 import torch
 
@@ -42,6 +42,15 @@ def test_gated_linear_of_many_columns(L):  # noqa: F811
     Y = L.gt_linear(ones(1, 1), W, gated=True)
     held = every(Y == 3)
     assert held
+
+
+@pytest.mark.parametrize("K", [(1 << 31) - 8, (1 << 31) - 3])
+def test_linear_of_a_long_sum(L, K):  # noqa: F811
+    """The longest k there are: ones among zeros, the first and the last k among them."""
+    X, W = torch.zeros(1, K, dtype=BF16, device="cuda"), ones(K, 4)
+    at = torch.tensor([0, 1, 1 << 20, (1 << 30) + 7, K - 40, K - 33, K - 9, K - 1], device="cuda")
+    X[0, at] = 1
+    assert L.gt_linear(X, W).tolist() == [[8.0] * 4]
 
 
 def test_linear_of_many_rows(L):  # noqa: F811
