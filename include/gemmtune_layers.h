@@ -52,7 +52,7 @@ typedef struct gt_linear_args {
   int64_t M, N, K;
   int32_t dtype;      /* gt_dtype */
   int32_t act;        /* gt_act, | GT_ACT_GATED */
-  int32_t out_dtype;  /* gt_dtype of Y */
+  int32_t out_dtype;  /* gt_dtype of Y: dtype, or GT_F32 */
   int32_t reserved;
   const void* X;
   int64_t ldx;
@@ -77,7 +77,7 @@ int gt_linear(const gt_linear_args* a, void* ws, int64_t ws_bytes, void* stream)
 typedef struct gt_linear_grad_args {
   int64_t M, N, K;
   int32_t dtype, act;
-  int32_t dw_dtype;
+  int32_t dw_dtype;   /* dtype, or GT_F32 */
   int32_t reserved;
   const void* dY;
   int64_t lddy;

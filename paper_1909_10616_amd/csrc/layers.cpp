@@ -36,6 +36,8 @@ int hip_fail(hipError_t e, const char* what) {
 
 int64_t size_of(int dtype) { return dtype == GT_BF16 ? 2 : 4; }
 bool dtype_ok(int d) { return d == GT_F32 || d == GT_BF16; }
+// What the epilogues store: the operands' type, or fp32.
+bool out_ok(int out, int dtype) { return out == dtype || out == GT_F32; }
 bool act_ok(int a) { return (a & ~(GT_ACT_GATED | 3)) == 0; }
 bool aligned(const void* p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
@@ -423,6 +425,7 @@ int linear_checks(const gt_linear_args* a, bool pointers) {
   GT_CHECK(extent(a->K, 1, "K"));
   if (!dtype_ok(a->dtype) || !dtype_ok(a->out_dtype) || !act_ok(a->act))
     return fail("gt_linear: unknown dtype or activation");
+  if (!out_ok(a->out_dtype, a->dtype)) return fail("gt_linear: Y is in dtype or in fp32");
   const int64_t wide = a->act & GT_ACT_GATED ? 2 * a->N : a->N;
   GT_CHECK(extent(wide, 1, "2N"));
   if (pointers && a->M > 0 && (!a->X || !a->W || !a->Y)) return fail("gt_linear: null X, W or Y");
@@ -474,6 +477,7 @@ int linear_grad_checks(const gt_linear_grad_args* a, bool pointers) {
   GT_CHECK(extent(a->K, 1, "K"));
   if (!dtype_ok(a->dtype) || !dtype_ok(a->dw_dtype) || !act_ok(a->act))
     return fail("gt_linear_backward: unknown dtype or activation");
+  if (!out_ok(a->dw_dtype, a->dtype)) return fail("gt_linear_backward: dW is in dtype or in fp32");
   const int64_t wide = a->act & GT_ACT_GATED ? 2 * a->N : a->N;
   GT_CHECK(extent(wide, 1, "2N"));
   if (pointers && a->M > 0) {

@@ -165,6 +165,13 @@ def _one(t, name, like, shape, dtype=None):
     return None if t is None else _whole(t, name, like, shape, dtype)
 
 
+def _result_type(t, name, like):
+    """The type of an output that is in like's type or in float32."""
+    if t.dtype is not like.dtype and _type(t, name) != F32:
+        raise ValueError(f"{name} must be {like.dtype} or torch.float32")
+    return _type(t, name)
+
+
 def _gpu(t, name, dims):
     if not t.is_cuda or t.dim() != dims:
         raise ValueError(f"{name} must be a GPU tensor of {dims} dimensions")
@@ -247,7 +254,7 @@ def gt_linear(X, W, bias=None, residual=None, act="none", gated=False, Y=None, P
     w, ldw = _tensor(W, "W", X, (K, wide))
     b = _one(bias, "bias", X, (wide,))
     r, ldr = _pair(residual, "residual", X, (M, N))
-    out = _type(Y, "Y")
+    out = _result_type(Y, "Y", X)
     y, ldy = _tensor(Y, "Y", X, (M, N), Y.dtype)
     p, ldp = _pair(P, "P", X, (M, wide))
     _call("gt_linear", gt_linear_args(M, N, K, dt, _act(act, gated), out, 0, x, ldx, w, ldw, b, r,
@@ -283,7 +290,7 @@ def gt_linear_backward(dY, X, W, P=None, act="none", gated=False, bias=True, dX=
     w, ldw = _tensor(W, "W", X, (K, wide))
     p, ldp = _pair(P if code else None, "P", X, (M, wide))
     dx, lddx = _pair(dX, "dX", X, (M, K))
-    dwt = F32 if dW is None else _type(dW, "dW")
+    dwt = F32 if dW is None else _result_type(dW, "dW", W)
     dw, lddw = _pair(dW, "dW", X, (K, wide), None if dW is None else dW.dtype)
     _call("gt_linear_backward",
           gt_linear_grad_args(M, N, K, dt, code, dwt, 0, dy, lddy, x, ldx, w, ldw, p, ldp, dx, lddx,
