@@ -16,7 +16,7 @@
  *   - Matrices are row-major with a leading dimension (`ld*`, elements between
  *     rows, at least the row's length); any extents, alignment and leading
  *     dimensions are served (16-byte aligned rows of whole 16-byte chunks are
- *     the fast case). No output may overlap an input or another output, but for
+ *     the fast case; for experts, and an X of less than 2 GiB). No output may overlap an input or another output, but for
  *     a residual R, which may be Y itself.
  *   - Sums are fp32, in an order fixed by the arguments: the same call gives
  *     the same bits. Values are rounded once, where they are stored; the
@@ -105,6 +105,11 @@ int gt_linear_backward(const gt_linear_grad_args* a, void* ws, int64_t ws_bytes,
  *   chosen: the k largest keys, largest first; equals (runs too) lowest index
  *           first. A token with fewer than k experts to choose has −1 in the
  *           remaining slots, with weight 0.
+ *   The key is the logit's, so that the choice holds no exponential and is the same bits
+ *           in any implementation. Routers that choose by score + bias, or rank their
+ *           groups by scores, choose other experts: a bias trained for scores, and
+ *           groups of such a router, cannot be served. Without bias and groups the
+ *           choice by scores is the same.
  *   score = softmax of the token's logits (over all E; without the bias) or
  *           sigmoid of the logit; weight = scale·score, with `renormalise`
  *           scale·score / Σ of the chosen scores.

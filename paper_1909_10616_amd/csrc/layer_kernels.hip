@@ -139,6 +139,9 @@ __global__ __launch_bounds__(256) void tail_kernel(const ProductArgs a) {
 // 256 threads: 64 column quads (octets, WIDE), kActRows rows, four of them a thread: all its
 // loads are out before the first is used. Bound by memory: 4096×4096 in bf16 28 µs,
 // 3.6 TB/s (dP stored past the caches 27, and no less for both products after it).
+// dP is stored in the operands' type, since the matrix instructions of both products take no
+// other: its rounding adds to the outputs' own (bf16 dX, dW 0.0024 of their norm from 64 bits,
+// 0.0017 without). The column sums are of dP before it.
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void act_grad_kernel(const ActGradArgs a) {
   constexpr int U = kActRows / 4, Q = WIDE ? 2 : 1;

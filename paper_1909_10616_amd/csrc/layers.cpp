@@ -629,7 +629,8 @@ Experts experts(const gt_experts_args& q, void* ws) {
   Scratch s(ws);
   x.H = s.take(R * ldh * sz);
   x.O = s.take<float>(R * x.ldo * 4);
-  {   // the rows' tokens are read from X where they lie
+  {   // the rows' tokens are read from X where they lie; the activated rows are stored in the
+      // operands' type, which the down product's matrix instructions take
     x.up.dtype = q.dtype;
     x.up.layout = kXW;
     ProductArgs& a = x.up.a;

@@ -27,11 +27,11 @@ constexpr int kRowCols = 64;
 constexpr int kRowStep = 64;   // k of a wavefront's loads in flight, at most
 
 // AL: W's rows are 16-byte aligned and whole chunks: loads by descriptor, zero beyond W.
-template <int DT, int MR, bool G, bool AL, int CW>
+template <int DT, int MR, bool G, bool AL>
 __global__ __launch_bounds__(kRowThreads) void rows_kernel(const ProductArgs a) {
   using T = typename Elem<DT>::T;
   constexpr int VEC = Elem<DT>::VEC;
-  constexpr int CL = CW / VEC;          // lanes a row of CW columns
+  constexpr int CW = kRowCols, CL = CW / VEC;   // columns, and lanes a row of them
   constexpr int KL = 64 / CL;           // rows of W a load
   constexpr int H = G ? 2 : 1;
   // loads of a half in flight, and as many being used
@@ -176,14 +176,14 @@ template <int DT, int MR, bool G, bool AL>
 hipError_t rows_by(const ProductArgs& a, hipStream_t s) {
   const size_t lds = static_cast<size_t>(rows_lds(a.K, MR, G));
   if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(rows_kernel<DT, MR, G, AL, kRowCols>),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(rows_kernel<DT, MR, G, AL>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize,
                                              static_cast<int>(lds));
     if (e != hipSuccess) return e;
   }
   const dim3 grid(static_cast<unsigned>(a.tilesN), static_cast<unsigned>(a.tilesM),
                   static_cast<unsigned>(a.splits));
-  rows_kernel<DT, MR, G, AL, kRowCols><<<grid, kRowThreads, lds, s>>>(a);
+  rows_kernel<DT, MR, G, AL><<<grid, kRowThreads, lds, s>>>(a);
   return hipGetLastError();
 }
 

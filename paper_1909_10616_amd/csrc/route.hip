@@ -687,7 +687,7 @@ int32_t block_tokens(int64_t T) {
 }
 
 // Whether one block does all: one launch, no scratch, and the keys of its wavefronts'
-// tokens in 64 KiB of LDS.
+// tokens in 48 KiB of LDS (beside 10 of lists, a launch's 64 without asking for more).
 bool few(int64_t T, int E, int k, int groups) {
   return T == 0 || (T <= 64 && T * k <= kEntries && group_floats(E, groups) * kWaves * 4 <= 48 * 1024);
 }

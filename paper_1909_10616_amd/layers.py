@@ -7,6 +7,9 @@ current stream (or ``stream``). Outputs and scratch memory come from PyTorch's
 allocator, for that stream, unless given. Matrices may have any row stride;
 their rows must be contiguous. Tensors given to a call on a stream other than
 their own are the caller's to keep alive, as with any asynchronous call.
+
+Outside autograd: results carry no graph, also where an operand requires a
+gradient. The gradients are the _backward calls.
 """
 from __future__ import annotations
 
@@ -303,7 +306,9 @@ def gt_route(logits, k, bias=None, score="softmax", groups=1, keep=1, renormalis
              workspace=None, stream=None) -> Route:
     """The k experts of every token by logit + bias, their weights and the lists of
     the experts' rows. logits [T, E] float32 or bfloat16; bias [E] float32,
-    for the choice only. With groups > 1 the choice is among the `keep` groups of
+    for the choice only. The choice is by logit + bias, not by score + bias: a bias
+    trained for scores chooses other experts here, and so do groups ranked by
+    scores. With groups > 1 the choice is among the `keep` groups of
     E/groups experts whose two largest keys have the largest sum. weights: scale
     times the softmax over the logits or the sigmoid of each, divided by the sum over
     the chosen if renormalise."""
