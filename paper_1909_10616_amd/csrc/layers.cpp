@@ -127,8 +127,8 @@ int few_rows(const Product& p) {
 // memory at 24 GB/s (30 gated, 35 in fp32, where a row gives two lines of memory) after
 // 3 µs, the whole chip at 5.2 TB/s, so W comes sooner if more of them share it, for the
 // launch that joins their sums and its host time: taken where a sixth is to be won
-// (bf16, W past the caches: 1×4096×4096 by 64 workgroups 22.4 µs, 256 in 4 slices
-// 15.5; 1×4096×11008 51.7 and 25.3; 1×11008×4096, 172 workgroups, 23.5 and in 2 slices 29.3).
+// (bf16, W past the caches: 1×4096×4096 by 64 workgroups 22.5 µs, 256 in 4 slices
+// 15.2; 1×4096×11008 52.2 and 25.3; 1×11008×4096, 172 workgroups, 23.5 and in 2 slices 29.3).
 int rows_slices(const Product& p) {
   const ProductArgs& a = p.a;
   const bool gated = a.e.epi == kEpiGated;
@@ -161,8 +161,8 @@ int64_t slim_rows(const ProductArgs& a) {
 // workgroup that a compute unit gets, or W once for every tile row, at 10 TB/s while
 // the last cache holds it. Fitted to 60 shapes from 1×7×3 to 512×4096×4096, plain and gated,
 // with 1 to 16 slices; it is chosen up to 64 rows or so, or more of small matrices
-// (13×1021×777 in fp32: 9.6 µs, the best tile with its join 14.2; 64×1024×1024 in bf16 6.4
-// and 8.5; 256×1024×1024 6.9 and 8.9; but 64×11008×4096 59 and 25).
+// (13×1021×777 in fp32: 9.8 µs, the best tile with its join 12.1; 64×1024×1024 in bf16 6.1
+// and 8.0; 256×1024×1024 6.5 and 8.3; but 64×11008×4096 59 and 25).
 double slim_cost(const Product& p, int64_t z) {
   const ProductArgs& a = p.a;
   const int64_t rows = slim_rows(a), cols = (a.N + 63) / 64;
@@ -188,7 +188,7 @@ double slim_cost(const Product& p, int64_t z) {
 // 48 shapes from 1×4096×4096 to 2048×4096×4096, 14 of them odd, in every layout and
 // type, each at every tile and 1 to 32 K slices (bf16, K = 4096, one slice:
 // 256×256 tiles 76 µs for 16 of them, 114 for 256; 128×128 43, 75 for 512; 64×64 28, 114
-// for 2048; 16×128 22, 221 for 4096). Of 376 choices five in six are within 5 % of the best form
+// for 2048; 16×128 22, 221 for 4096). Of 254 choices four in five are within 5 % of the best form
 // measured, nine in ten within 10 %; the furthest are few rows whose K slices would save 3 to 5 µs
 // in a graph and cost as much of host time in a second launch without one.
 struct TileCost {

@@ -9,7 +9,7 @@
 // 16 rows of X). The sums meet in the workgroup, lanes first, then wavefronts in
 // order, so one launch gives the layer's output, but for narrow layers, whose few
 // workgroups cannot draw W fast enough: K is sliced over more of them then.
-// 1×11008×4096 gated in bf16: 38.5 µs, 4.7 TB/s; 1×4096×4096 past the caches 15.5 in 4
+// 1×11008×4096 gated in bf16: 39 µs, 4.6 TB/s; 1×4096×4096 past the caches 15.2 in 4
 // slices, 4 of it the join.
 #include <hip/hip_runtime.h>
 

@@ -9,8 +9,8 @@
 // lanes holds, and instruction j multiplies column j of every quad (bf16: pairs of rows are
 // merged by one byte permutation a register). The result then lies in quads of
 // neighbouring columns. The wavefronts' sums meet in LDS and are added in their order.
-// 13×1021×777 in fp32: 10.4 µs, where 16×128 tiles in 4 K slices took 12.0 and their join
-// 4.1; 64×1024×1024 in bf16 6.4 (8.5), 16×4096×4096 in 4 slices 10.7 (11.9).
+// 13×1021×777 in fp32: 9.8 µs, where the best tiles with the join of their K slices take
+// 12.1; 64×1024×1024 in bf16 6.1 (8.0), 16×4096×4096 in 4 slices 10.2 (11.3).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
