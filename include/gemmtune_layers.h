@@ -162,7 +162,7 @@ int gt_route_backward(const gt_route_grad_args* a, void* stream);
  * e = experts[t][s], slots without an expert left out. X, R, Y: T×D; W1:
  * E×D×H (E×D×2H gated), W2: E×H×D, each expert's matrix contiguous rows of ldw
  * elements, the experts' sw* elements apart; b1: E×H (E×2H) or NULL, b2: E×D or
- * NULL, contiguous. E ≤ 1024, k ≤ 64, T·k < 2^30. weights, offsets, order, place as
+ * NULL, contiguous. E ≤ 1024, k ≤ 64, T·k < 2^29. weights, offsets, order, place as
  * gt_route gives them (entries outside their range are taken as no expert; which rows
  * offsets name that do not ascend is the caller's affair, but no access leaves the arrays). P (optional, for the
  * gradients): the pre-activations X·W1 + b1, T·k rows of H (2H) in the order of

@@ -17,7 +17,7 @@ namespace gt {
 namespace {
 
 constexpr int64_t kMaxExtent = int64_t{1} << 31;
-constexpr int64_t kMaxEntries = int64_t{1} << 30;    // rows of experts: counted by tiles of them in 32 bits
+constexpr int64_t kMaxEntries = int64_t{1} << 29;    // rows of experts: counted by tiles of them in 32 bits
 constexpr int64_t kMaxElements = int64_t{1} << 45;   // of one array: no size below leaves 64 bits
 
 int fail(const std::string& what) {
