@@ -1,7 +1,8 @@
 /*
  * gemmtune_layers.h — layer operators of libgemmtune for AMD Instinct MI355X
  * (gfx950): perceptron layers with their epilogue fused into the product,
- * their gradients, the routing of tokens to experts, and layers of experts.
+ * their gradients, the routing of tokens to experts, layers of experts, and layers
+ * in 8-bit floating point with the norm before them.
  *
  * Conventions (beside those of gemmtune.h, whose status codes, gt_dtype and
  * gt_last_error() apply):
@@ -230,6 +231,127 @@ typedef struct gt_experts_grad_args {
 } gt_experts_grad_args;
 int gt_experts_backward_workspace(const gt_experts_grad_args* a, int64_t* bytes);
 int gt_experts_backward(const gt_experts_grad_args* a, void* ws, int64_t ws_bytes, void* stream);
+
+/* ---- Layers in 8-bit floating point ----------------------------------------
+ *
+ * Codes: a matrix of rows×cols values as 8-bit codes q (`gt_code`, OCP E4M3: largest
+ * 448, no infinity; E5M2: largest 57344) and fp32 scales s; it stands for q·s. The scales lie in rows
+ * of ceil(cols/128): that of q[r][c] is s[r / block][c / 128], block 1 (128 values of a
+ * row share a scale) or 128 (squares of 128×128).
+ *
+ * From values x, with m the largest |x| of a block (NaN left out):
+ *   s = m / largest, at least 2^-126, and 1 where m is 0; with `pow2` the next power
+ *   of two; q = x·(1/s), every step rounded to fp32 and the last to the nearest code,
+ *   ties to even.
+ * A NaN is the code of NaN. An infinity makes its block's scale infinite and itself NaN, the
+ * block's finite values 0: what they stand for is NaN. */
+typedef enum { GT_E4M3 = 0, GT_E5M2 = 1 } gt_code;
+
+/* Codes of X (M×N, dtype), and of its transpose: Q, S: M×N codes and their scales; Qt, St: N×M
+ * codes and their scales, along M. Either pair may be NULL. With block 128 both have
+ * the same codes. */
+typedef struct gt_quantise_args {
+  int64_t M, N;
+  int32_t dtype;   /* gt_dtype of X */
+  int32_t code;    /* gt_code */
+  int32_t block;   /* 1 or 128 */
+  int32_t pow2;    /* scales are powers of two */
+  const void* X;
+  int64_t ldx;
+  void* Q;
+  int64_t ldq;     /* bytes, as are codes */
+  float* S;
+  int64_t lds;
+  void* Qt;
+  int64_t ldqt;
+  float* St;
+  int64_t ldst;
+} gt_quantise_args;
+int gt_quantise(const gt_quantise_args* a, void* stream);
+
+/* Y = act(X·Wᵀ + bias) + R of codes: X M×K, W N×K (gated: 2N×K, the gate's rows, then the
+ * up's), K along the rows of both, so that blocks of 128 lie along the sum:
+ *   (X·Wᵀ)[m][n] = Σ_b sx[m][b]·sw[n][b]·Σ_{k in block b} X[m][k]·W[n][k].
+ * A block's sum and the sum over blocks are fp32. The gradients are the same product of
+ * other codes: dX = dY·W takes codes of dY and of W's transpose, dW = dYᵀ·X codes of both
+ * transposes. bias: N (2N) or NULL, R: M×N or NULL, both in dtype; Y in dtype or fp32, and it may be R
+ * (dW += …). Rows of X and W at 16-byte aligned addresses are the fast case. */
+typedef struct gt_linear_fp8_args {
+  int64_t M, N, K;
+  int32_t dtype;             /* gt_dtype of bias and R */
+  int32_t act;               /* gt_act, | GT_ACT_GATED */
+  int32_t out_dtype;         /* gt_dtype of Y: dtype, or GT_F32 */
+  int32_t xcode, wcode;      /* gt_code */
+  int32_t xblock, wblock;    /* rows that share a scale: 1 or 128 */
+  int32_t reserved;
+  const void* X;
+  int64_t ldx;
+  const float* sx;
+  int64_t ldsx;
+  const void* W;
+  int64_t ldw;
+  const float* sw;
+  int64_t ldsw;
+  const void* bias;
+  const void* R;
+  int64_t ldr;
+  void* Y;
+  int64_t ldy;
+} gt_linear_fp8_args;
+int gt_linear_fp8_workspace(const gt_linear_fp8_args* a, int64_t* bytes);
+int gt_linear_fp8(const gt_linear_fp8_args* a, void* ws, int64_t ws_bytes, void* stream);
+
+/* Layer norm of M rows: Y = (X − mean)·rstd·w + b, mean = ΣX/N, rstd = 1/√(Σ(X − mean)²/N +
+ * eps) of each row. X: M×N in dtype; w, b: N in wtype, or NULL for 1 and 0. Outputs, each
+ * NULL where it is not wanted: Y (M×N, dtype); mean, rstd (M, fp32: what the gradients
+ * need); Q, S: codes of Y before its rounding to dtype, block 1, as gt_quantise gives them. Y may
+ * be X. */
+typedef struct gt_norm_args {
+  int64_t M, N;
+  int32_t dtype;
+  int32_t wtype;   /* gt_dtype of w and b: dtype, or GT_F32 */
+  int32_t code;    /* of Q */
+  int32_t pow2;
+  float eps;       /* ≥ 0, finite */
+  int32_t reserved;
+  const void* X;
+  int64_t ldx;
+  const void* w;
+  const void* b;
+  void* Y;
+  int64_t ldy;
+  float* mean;
+  float* rstd;
+  void* Q;
+  int64_t ldq;
+  float* S;
+  int64_t lds;
+} gt_norm_args;
+int gt_norm(const gt_norm_args* a, void* stream);
+
+/* Gradients of gt_norm. With h = (X − mean)·rstd and g = dY·w: dX = rstd·(g − mean of g −
+ * h·mean of g·h) + R (the means over the row; M×N, dtype), dw = Σ over rows of dY·h and db = Σ of dY
+ * (N, fp32). Any of the three may be NULL. R (M×N in dtype or NULL): the gradient that
+ * reaches X by another way; dX may be R, or dY. mean, rstd as gt_norm gave them. */
+typedef struct gt_norm_grad_args {
+  int64_t M, N;
+  int32_t dtype, wtype;
+  const void* dY;
+  int64_t lddy;
+  const void* X;
+  int64_t ldx;
+  const void* w;
+  const float* mean;
+  const float* rstd;
+  const void* R;
+  int64_t ldr;
+  void* dX;
+  int64_t lddx;
+  float* dw;
+  float* db;
+} gt_norm_grad_args;
+int gt_norm_backward_workspace(const gt_norm_grad_args* a, int64_t* bytes);
+int gt_norm_backward(const gt_norm_grad_args* a, void* ws, int64_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -44,6 +44,9 @@ def _units():
     units += [("layers", "layers.cpp", []), ("layer_kernels", "layer_kernels.hip", []),
               ("route", "route.hip", []), ("product_rows", "product_rows.hip", []),
               ("product_slim", "product_slim.hip", [])]
+    # layers in 8 bits and the norm
+    units += [("layers8", "layers8.cpp", []), ("norm", "norm.hip", []), ("quantise", "quantise.hip", []),
+              ("rows8", "rows8.hip", [])]
     units += [(f"product_{dn}_{lay}", "product_inst.hip", [f"-DLP_DT={dt}", f"-DLP_LAY={lay}"])
               for dt, dn in ((0, "f32"), (1, "bf16")) for lay in (0, 1, 2)]
     for dt, dn in ((0, "f32"), (1, "bf16")):

@@ -1,0 +1,36 @@
+// Launchers of the norm, of the quantising kernels and of the 8-bit products.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "gemmtune_layers.h"
+#include "product_args.h"
+
+namespace gt {
+
+hipError_t launch_quantise(const gt_quantise_args& a, hipStream_t s);
+
+hipError_t launch_norm(const gt_norm_args& a, hipStream_t s);
+
+// Partial rows of the column sums (0 where neither dw nor db is wanted), each of N of dw and
+// N of db.
+int64_t norm_parts(const gt_norm_grad_args& a);
+hipError_t launch_norm_grad(const gt_norm_grad_args& a, float* part, hipStream_t s);
+
+// An 8-bit product: p.A and p.B are codes, rows lda and ldb bytes apart, both along k; row r
+// of A has its scales at sa + (r >> xshift)·ldsa, B's likewise. p.N: columns of Y; B has the up
+// values' rows from N on when gated.
+struct Product8 {
+  ProductArgs p;
+  const float* sa;
+  const float* sb;
+  int64_t ldsa, ldsb;
+  int32_t xshift, wshift;
+  int32_t acode, bcode;
+};
+
+// Few rows, straight from memory: `rows` (16, 32 or 64) a workgroup.
+hipError_t launch_rows8(int dtype, int rows, const Product8& a, hipStream_t s);
+
+}  // namespace gt

@@ -1,0 +1,483 @@
+// Layer norm and its gradients, a row in the registers of 64 to 512 threads.
+//
+// Forward: the mean, then Σ(X − mean)² of the values that the registers hold, so that a large
+// mean costs no digits, then the outputs: each row is read once and written once.
+// Backward: both means of a row in one exchange; every thread keeps the column sums of dw
+// and db for its own columns over all rows that its workgroup takes, and a second launch
+// adds the workgroups' sums in their order.
+// Thread t of a row has the octets t, t + TH, …, so that 16 neighbours hold 128 columns, a
+// block of codes.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "fp8.hpp"
+#include "layer8_kernels.h"
+#include "layer_kernels.h"
+
+namespace gt {
+namespace {
+
+// ---- sums over a row's threads
+
+__device__ __forceinline__ float wave_sum(float s) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d);
+  return s;
+}
+// The sum over TH threads, the same in each; `box`: LDS that the exchange before did not use.
+template <int TH>
+__device__ __forceinline__ float row_sum(float s, float* box) {
+  s = wave_sum(s);
+  if constexpr (TH > 64) {
+    if ((threadIdx.x & 63) == 0) box[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < TH / 64; ++i) s += box[i];
+  }
+  return s;
+}
+
+template <typename W>
+__device__ __forceinline__ oct open_or(const void* p, const raw8<W>& r, float none) {
+  return p ? open8<W>(r) : oct{f32x4{none, none, none, none}, f32x4{none, none, none, none}};
+}
+
+__device__ __forceinline__ oct times(const oct& v, float f) { return oct{v.a * f, v.b * f}; }
+__device__ __forceinline__ float sum8(const oct& v) {
+  return ((v.a[0] + v.a[1]) + (v.a[2] + v.a[3])) + ((v.b[0] + v.b[1]) + (v.b[2] + v.b[3]));
+}
+// v − m in the first n columns, zero in the others
+__device__ __forceinline__ oct centred(const oct& v, float m, int64_t n) {
+  oct d;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    d.a[i] = i < n ? v.a[i] - m : 0.0f;
+    d.b[i] = i + 4 < n ? v.b[i] - m : 0.0f;
+  }
+  return d;
+}
+
+// ---- forward
+
+// An octet of a row's outputs from X − mean.
+template <typename T, int CODE>
+__device__ __forceinline__ void norm_out(const gt_norm_args& a, int64_t row, int64_t c, const oct& d,
+                                         float rstd, const oct& w, const oct& b) {
+  const int64_t left = a.N - c;
+  oct y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y.a[i] = fmaf(d.a[i] * rstd, w.a[i], b.a[i]);
+    y.b[i] = fmaf(d.b[i] * rstd, w.b[i], b.b[i]);
+  }
+  if (a.Y && left > 0) store8n(static_cast<T*>(a.Y) + row * a.ldy + c, y, left);
+  if constexpr (CODE >= 0) {
+    const float s = block_scale<CODE>(max16(left > 0 ? most8(y) : 0.0f), a.pow2 != 0);
+    if (left <= 0) return;
+    store_codes(static_cast<uint8_t*>(a.Q) + row * a.ldq + c, code8<CODE>(y, 1.0f / s), left);
+    if (c % kBlock == 0) a.S[row * a.lds + c / kBlock] = s;
+  }
+}
+
+template <typename T, typename W, int TH, int NV, int CODE>
+__global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_kernel(const gt_norm_args a) {
+  constexpr int RB = TH < 256 ? 256 / TH : 1;   // rows of a workgroup
+  __shared__ float box[2][16];
+  const int t = threadIdx.x % TH, rb = threadIdx.x / TH;
+  const W* wp = static_cast<const W*>(a.w);
+  const W* bp = static_cast<const W*>(a.b);
+  raw8<W> w[NV], b[NV];
+  raw8<T> next[NV];
+  const int64_t step = int64_t{gridDim.x} * RB;
+  auto col = [&](int v) { return (static_cast<int64_t>(v) * TH + t) * 8; };
+  auto load = [&](int64_t row) __attribute__((always_inline)) {
+    const T* x = static_cast<const T*>(a.X) + row * a.ldx;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) next[v] = raw_of<T>(x + col(v), row < a.M ? a.N - col(v) : 0);
+  };
+  int64_t row = int64_t{blockIdx.x} * RB + rb;
+  load(row);
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    w[v] = raw_of<W>(wp + col(v), wp ? a.N - col(v) : 0);
+    b[v] = raw_of<W>(bp + col(v), bp ? a.N - col(v) : 0);
+  }
+  const float n = static_cast<float>(a.N);
+  for (; row < a.M; row += step) {
+    oct x[NV];
+    float s = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      x[v] = open8<T>(next[v]);
+      s += sum8(x[v]);
+    }
+    load(row + step);
+    const float mean = row_sum<TH>(s, box[0]) / n;
+    s = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      x[v] = centred(x[v], mean, a.N - col(v));
+      s += sum8(oct{x[v].a * x[v].a, x[v].b * x[v].b});
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<TH>(s, box[1]) / n + a.eps);
+    if (t == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+      norm_out<T, CODE>(a, row, col(v), x[v], rstd, open_or<W>(wp, w[v], 1.0f), open_or<W>(bp, b[v], 0.0f));
+  }
+}
+
+// Rows longer than the registers: read three times.
+template <typename T, typename W, int CODE>
+__global__ __launch_bounds__(1024) void norm_long_kernel(const gt_norm_args a) {
+  constexpr int TH = 1024;
+  __shared__ float box[2][16];
+  const W* wp = static_cast<const W*>(a.w);
+  const W* bp = static_cast<const W*>(a.b);
+  const float n = static_cast<float>(a.N);
+  for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
+    const T* x = static_cast<const T*>(a.X) + row * a.ldx;
+    float s = 0.0f;
+    for (int64_t c = threadIdx.x * 8; c < a.N; c += TH * 8) s += sum8(open8<T>(raw_of<T>(x + c, a.N - c)));
+    const float mean = row_sum<TH>(s, box[0]) / n;
+    s = 0.0f;
+    for (int64_t c = threadIdx.x * 8; c < a.N; c += TH * 8) {
+      const oct d = centred(open8<T>(raw_of<T>(x + c, a.N - c)), mean, a.N - c);
+      s += sum8(oct{d.a * d.a, d.b * d.b});
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<TH>(s, box[1]) / n + a.eps);
+    if (threadIdx.x == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+    for (int64_t c0 = 0; c0 < a.N; c0 += TH * 8) {   // (all lanes, for the blocks' maxima)
+      const int64_t c = c0 + threadIdx.x * 8, left = a.N - c;
+      norm_out<T, CODE>(a, row, c, centred(open8<T>(raw_of<T>(x + c, left)), mean, left), rstd,
+                        open_or<W>(wp, raw_of<W>(wp + c, wp ? left : 0), 1.0f),
+                        open_or<W>(bp, raw_of<W>(bp + c, bp ? left : 0), 0.0f));
+    }
+  }
+}
+
+// ---- backward
+
+// dw and db of a thread's columns, from its workgroup's rows, to the workgroup's partial row.
+template <typename T, typename W, int TH, int NV, bool SUMS>
+__global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_grad_kernel(const gt_norm_grad_args a,
+                                                                        float* part) {
+  constexpr int RB = TH < 256 ? 256 / TH : 1;
+  __shared__ float box[2][2][16];
+  __shared__ f32x4 join[SUMS && RB > 1 ? RB : 1][SUMS && RB > 1 ? 2 * TH : 1];
+  const int t = threadIdx.x % TH, rb = threadIdx.x / TH;
+  const W* wp = static_cast<const W*>(a.w);
+  const int64_t step = int64_t{gridDim.x} * RB;
+  auto col = [&](int v) { return (static_cast<int64_t>(v) * TH + t) * 8; };
+  raw8<W> w[NV];
+  raw8<T> nx[NV], ny[NV];
+  float nmean, nrstd;
+  auto load = [&](int64_t row) __attribute__((always_inline)) {
+    const T* x = static_cast<const T*>(a.X) + row * a.ldx;
+    const T* y = static_cast<const T*>(a.dY) + row * a.lddy;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int64_t left = row < a.M ? a.N - col(v) : 0;
+      nx[v] = raw_of<T>(x + col(v), left);
+      ny[v] = raw_of<T>(y + col(v), left);
+    }
+    nmean = row < a.M ? a.mean[row] : 0.0f;
+    nrstd = row < a.M ? a.rstd[row] : 0.0f;
+  };
+  int64_t row = int64_t{blockIdx.x} * RB + rb;
+  load(row);
+#pragma unroll
+  for (int v = 0; v < NV; ++v) w[v] = raw_of<W>(wp + col(v), wp ? a.N - col(v) : 0);
+  oct dw[SUMS ? NV : 1], db[SUMS ? NV : 1];
+#pragma unroll
+  for (int v = 0; v < (SUMS ? NV : 1); ++v) dw[v] = db[v] = oct{};
+  const float n = static_cast<float>(a.N);
+  for (int it = 0; row < a.M; row += step, it ^= 1) {
+    oct h[NV], g[NV];
+    const float mean = nmean, rstd = nrstd;
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const oct x = open8<T>(nx[v]), y = open8<T>(ny[v]);
+      h[v] = oct{(x.a - mean) * rstd, (x.b - mean) * rstd};
+      if constexpr (SUMS) {
+        dw[v].a += y.a * h[v].a;
+        dw[v].b += y.b * h[v].b;
+        db[v].a += y.a;
+        db[v].b += y.b;
+      }
+      const oct wv = open_or<W>(wp, w[v], 1.0f);
+      g[v] = oct{y.a * wv.a, y.b * wv.b};
+      s1 += sum8(g[v]);
+      s2 += sum8(oct{g[v].a * h[v].a, g[v].b * h[v].b});
+    }
+    load(row + step);
+    if (!a.dX) continue;
+    raw8<T> r[NV];
+    if (a.R) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        r[v] = raw_of<T>(static_cast<const T*>(a.R) + row * a.ldr + col(v), a.N - col(v));
+    }
+    s1 = wave_sum(s1);
+    s2 = wave_sum(s2);
+    if constexpr (TH > 64) {
+      float(*mine)[16] = box[it];
+      if ((threadIdx.x & 63) == 0) {
+        mine[0][threadIdx.x >> 6] = s1;
+        mine[1][threadIdx.x >> 6] = s2;
+      }
+      __syncthreads();
+      s1 = s2 = 0.0f;
+#pragma unroll
+      for (int i = 0; i < TH / 64; ++i) {
+        s1 += mine[0][i];
+        s2 += mine[1][i];
+      }
+    }
+    const float m1 = s1 / n, m2 = s2 / n;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      oct d{(g[v].a - m1 - h[v].a * m2) * rstd, (g[v].b - m1 - h[v].b * m2) * rstd};
+      if (a.R) {
+        const oct q = open8<T>(r[v]);
+        d.a += q.a;
+        d.b += q.b;
+      }
+      const int64_t left = a.N - col(v);
+      if (left > 0) store8n(static_cast<T*>(a.dX) + row * a.lddx + col(v), d, left);
+    }
+  }
+  if constexpr (SUMS) {
+    float* out = part + int64_t{blockIdx.x} * 2 * a.N;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        oct s = k == 0 ? dw[v] : db[v];
+        if constexpr (RB > 1) {
+          __syncthreads();
+          join[rb][t] = s.a;
+          join[rb][TH + t] = s.b;
+          __syncthreads();
+          if (rb > 0) continue;
+#pragma unroll
+          for (int i = 1; i < RB; ++i) {
+            s.a += join[i][t];
+            s.b += join[i][TH + t];
+          }
+        }
+        if (a.N > col(v)) store8n(out + k * a.N + col(v), s, a.N - col(v));
+      }
+    }
+  }
+}
+
+// Long rows: dX alone, read twice.
+template <typename T, typename W>
+__global__ __launch_bounds__(1024) void norm_grad_long_kernel(const gt_norm_grad_args a) {
+  constexpr int TH = 1024;
+  __shared__ float box[2][16];
+  const W* wp = static_cast<const W*>(a.w);
+  const float n = static_cast<float>(a.N);
+  for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
+    const T* x = static_cast<const T*>(a.X) + row * a.ldx;
+    const T* y = static_cast<const T*>(a.dY) + row * a.lddy;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float s1 = 0.0f, s2 = 0.0f;
+    auto both = [&](int64_t c, oct* g, oct* h) __attribute__((always_inline)) {
+      const int64_t left = a.N - c;
+      const oct xv = open8<T>(raw_of<T>(x + c, left)), yv = open8<T>(raw_of<T>(y + c, left));
+      const oct wv = open_or<W>(wp, raw_of<W>(wp + c, wp ? left : 0), 1.0f);
+      *h = oct{(xv.a - mean) * rstd, (xv.b - mean) * rstd};
+      *g = oct{yv.a * wv.a, yv.b * wv.b};
+    };
+    oct g, h;
+    for (int64_t c = threadIdx.x * 8; c < a.N; c += TH * 8) {
+      both(c, &g, &h);
+      s1 += sum8(g);
+      s2 += sum8(oct{g.a * h.a, g.b * h.b});
+    }
+    const float m1 = row_sum<TH>(s1, box[0]) / n, m2 = row_sum<TH>(s2, box[1]) / n;
+    for (int64_t c = threadIdx.x * 8; c < a.N; c += TH * 8) {
+      both(c, &g, &h);
+      oct d{(g.a - m1 - h.a * m2) * rstd, (g.b - m1 - h.b * m2) * rstd};
+      if (a.R) {
+        const oct q = open8<T>(raw_of<T>(static_cast<const T*>(a.R) + row * a.ldr + c, a.N - c));
+        d.a += q.a;
+        d.b += q.b;
+      }
+      store8n(static_cast<T*>(a.dX) + row * a.lddx + c, d, a.N - c);
+    }
+  }
+}
+
+// … and the column sums: 256 threads, 512 columns of every gridDim.y-th run of 4 rows.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_sums_kernel(const gt_norm_grad_args a, float* part) {
+  __shared__ f32x4 join[4][2][64];
+  const int q = threadIdx.x & 63, rb = threadIdx.x >> 6;
+  const int64_t c = (int64_t{blockIdx.x} * 64 + q) * 8, left = a.N - c;
+  oct dw{}, db{};
+  for (int64_t row = int64_t{blockIdx.y} * 4 + rb; row < a.M; row += int64_t{gridDim.y} * 4) {
+    const oct x = open8<T>(raw_of<T>(static_cast<const T*>(a.X) + row * a.ldx + c, left));
+    const oct y = open8<T>(raw_of<T>(static_cast<const T*>(a.dY) + row * a.lddy + c, left));
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    dw.a += y.a * ((x.a - mean) * rstd);
+    dw.b += y.b * ((x.b - mean) * rstd);
+    db.a += y.a;
+    db.b += y.b;
+  }
+  float* out = part + int64_t{blockIdx.y} * 2 * a.N;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    oct s = k == 0 ? dw : db;
+    __syncthreads();
+    join[rb][0][q] = s.a;
+    join[rb][1][q] = s.b;
+    __syncthreads();
+    if (rb > 0) continue;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+      s.a += join[i][0][q];
+      s.b += join[i][1][q];
+    }
+    if (left > 0) store8n(out + k * a.N + c, s, left);
+  }
+}
+
+// out[n] = Σ of the partial rows, in order: 64 columns of dw (blockIdx.y 0) or db, a sixteenth of
+// the rows a wavefront.
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float* part, int64_t rows, int64_t N,
+                                                        float* dw, float* db) {
+  __shared__ float sums[16][64];
+  const int c = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float* out = blockIdx.y == 0 ? dw : db;
+  if (!out) return;
+  for (int64_t n = int64_t{blockIdx.x} * 64 + c; n - c < N; n += int64_t{gridDim.x} * 64) {
+    float s = 0.0f;
+    if (n < N) {
+      const float* p = part + blockIdx.y * N + n;
+#pragma unroll 8
+      for (int64_t r = wave; r < rows; r += 16) s += p[r * 2 * N];
+    }
+    sums[wave][c] = s;
+    __syncthreads();
+    if (wave == 0 && n < N) {
+      s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s += sums[i][c];
+      out[n] = s;
+    }
+    __syncthreads();
+  }
+}
+
+// ---- choices
+
+// Threads a row, octets a thread. 0: a long row.
+struct Rows {
+  int threads, octets;
+};
+Rows rows_of(int64_t N) {
+  const int64_t oct = (N + 7) / 8;
+  for (const Rows r : {Rows{64, 1}, Rows{64, 2}, Rows{256, 1}, Rows{256, 2}, Rows{512, 2}, Rows{512, 4}})
+    if (oct <= int64_t{r.threads} * r.octets) return r;
+  return Rows{0, 0};
+}
+unsigned grid_of(int64_t M, const Rows& r) {
+  const int each = r.threads == 64 ? 4 : 1;
+  return static_cast<unsigned>(std::min<int64_t>((M + each - 1) / each, kUnits * (r.threads == 512 ? 4 : 8)));
+}
+
+template <typename T, typename W, int CODE>
+hipError_t norm_by(const gt_norm_args& a, hipStream_t s) {
+  const Rows r = rows_of(a.N);
+  if (r.threads == 0) {
+    norm_long_kernel<T, W, CODE><<<static_cast<unsigned>(std::min<int64_t>(a.M, 4096)), 1024, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  const unsigned grid = grid_of(a.M, r);
+  if (r.threads == 64 && r.octets == 1) norm_kernel<T, W, 64, 1, CODE><<<grid, 256, 0, s>>>(a);
+  else if (r.threads == 64) norm_kernel<T, W, 64, 2, CODE><<<grid, 256, 0, s>>>(a);
+  else if (r.threads == 256 && r.octets == 1) norm_kernel<T, W, 256, 1, CODE><<<grid, 256, 0, s>>>(a);
+  else if (r.threads == 256) norm_kernel<T, W, 256, 2, CODE><<<grid, 256, 0, s>>>(a);
+  else if (r.octets == 2) norm_kernel<T, W, 512, 2, CODE><<<grid, 512, 0, s>>>(a);
+  else norm_kernel<T, W, 512, 4, CODE><<<grid, 512, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <typename T, typename W>
+hipError_t norm_by_code(const gt_norm_args& a, hipStream_t s) {
+  if (!a.Q) return norm_by<T, W, -1>(a, s);
+  return a.code == GT_E4M3 ? norm_by<T, W, GT_E4M3>(a, s) : norm_by<T, W, GT_E5M2>(a, s);
+}
+
+unsigned grad_grid(int64_t M, const Rows& r) {
+  const int each = r.threads == 64 ? 4 : 1;
+  return static_cast<unsigned>(std::min<int64_t>((M + each - 1) / each, kUnits * (r.threads == 512 ? 2 : 4)));
+}
+unsigned long_parts(int64_t M) { return static_cast<unsigned>(std::min<int64_t>((M + 3) / 4, 64)); }
+
+template <typename T, typename W, bool SUMS>
+hipError_t grad_by(const gt_norm_grad_args& a, float* part, hipStream_t s) {
+  const Rows r = rows_of(a.N);
+  const unsigned grid = grad_grid(a.M, r);
+  if (r.threads == 64 && r.octets == 1) norm_grad_kernel<T, W, 64, 1, SUMS><<<grid, 256, 0, s>>>(a, part);
+  else if (r.threads == 64) norm_grad_kernel<T, W, 64, 2, SUMS><<<grid, 256, 0, s>>>(a, part);
+  else if (r.threads == 256 && r.octets == 1) norm_grad_kernel<T, W, 256, 1, SUMS><<<grid, 256, 0, s>>>(a, part);
+  else if (r.threads == 256) norm_grad_kernel<T, W, 256, 2, SUMS><<<grid, 256, 0, s>>>(a, part);
+  else if (r.octets == 2) norm_grad_kernel<T, W, 512, 2, SUMS><<<grid, 512, 0, s>>>(a, part);
+  else norm_grad_kernel<T, W, 512, 4, SUMS><<<grid, 512, 0, s>>>(a, part);
+  return hipGetLastError();
+}
+
+template <typename T, typename W>
+hipError_t grad(const gt_norm_grad_args& a, float* part, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (a.M > 0 && rows_of(a.N).threads == 0) {
+    if (part) {   // (before dX, which may be dY)
+      norm_sums_kernel<T><<<dim3(static_cast<unsigned>((a.N + 511) / 512), long_parts(a.M)), 256, 0, s>>>(a, part);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    if (a.dX) {
+      norm_grad_long_kernel<T, W><<<static_cast<unsigned>(std::min<int64_t>(a.M, 4096)), 1024, 0, s>>>(a);
+      e = hipGetLastError();
+    }
+  } else if (a.M > 0 && (part || a.dX)) {
+    e = part ? grad_by<T, W, true>(a, part, s) : grad_by<T, W, false>(a, part, s);
+  }
+  if (e != hipSuccess || (!a.dw && !a.db)) return e;
+  const unsigned columns = static_cast<unsigned>(std::min<int64_t>((a.N + 63) / 64, int64_t{1} << 20));
+  norm_join_kernel<<<dim3(columns, 2), 1024, 0, s>>>(part, norm_parts(a), a.N, a.dw, a.db);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_norm(const gt_norm_args& a, hipStream_t s) {
+  if (a.dtype == GT_F32) return norm_by_code<float, float>(a, s);
+  return a.wtype == GT_F32 ? norm_by_code<uint16_t, float>(a, s) : norm_by_code<uint16_t, uint16_t>(a, s);
+}
+
+int64_t norm_parts(const gt_norm_grad_args& a) {
+  if (a.M == 0 || (!a.dw && !a.db)) return 0;
+  const Rows r = rows_of(a.N);
+  return r.threads == 0 ? long_parts(a.M) : grad_grid(a.M, r);
+}
+
+hipError_t launch_norm_grad(const gt_norm_grad_args& a, float* part, hipStream_t s) {
+  if (a.dtype == GT_F32) return grad<float, float>(a, part, s);
+  return a.wtype == GT_F32 ? grad<uint16_t, float>(a, part, s) : grad<uint16_t, uint16_t>(a, part, s);
+}
+
+}  // namespace gt

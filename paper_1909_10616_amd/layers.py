@@ -1,6 +1,7 @@
 """Layer operators of libgemmtune (include/gemmtune_layers.h), same names as the
 C ABI: perceptron layers with their epilogue, their gradients, the routing of
-tokens to experts and layers of experts.
+tokens to experts, layers of experts, and layers in 8-bit floating point with the
+norm before them.
 
 Argument checks and marshalling only; every step runs in the library, on the
 current stream (or ``stream``). Outputs and scratch memory come from PyTorch's
@@ -22,6 +23,8 @@ from .gemmtune import BF16, F32, _check, _stream
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 GATED = 16
 SCORES = {"softmax": 0, "sigmoid": 1}
+CODES = {"e4m3": 0, "e5m2": 1}
+BLOCKS = {"row": 1, "square": 128}   # rows that share a scale
 
 _i64, _i32, _P, _f32 = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_float
 
@@ -63,11 +66,31 @@ class gt_experts_grad_args(ctypes.Structure):
                        "p:dW1 dW2 db1 db2 dweights")
 
 
+class gt_quantise_args(ctypes.Structure):
+    _fields_ = _fields("l:M N;i:dtype code block pow2;p:X;l:ldx;p:Q;l:ldq;p:S;l:lds;p:Qt;l:ldqt;p:St;l:ldst")
+
+
+class gt_linear_fp8_args(ctypes.Structure):
+    _fields_ = _fields("l:M N K;i:dtype act out_dtype xcode wcode xblock wblock reserved;p:X;l:ldx;p:sx;"
+                       "l:ldsx;p:W;l:ldw;p:sw;l:ldsw;p:bias R;l:ldr;p:Y;l:ldy")
+
+
+class gt_norm_args(ctypes.Structure):
+    _fields_ = _fields("l:M N;i:dtype wtype code pow2;f:eps;i:reserved;p:X;l:ldx;p:w b Y;l:ldy;p:mean rstd "
+                       "Q;l:ldq;p:S;l:lds")
+
+
+class gt_norm_grad_args(ctypes.Structure):
+    _fields_ = _fields("l:M N;i:dtype wtype;p:dY;l:lddy;p:X;l:ldx;p:w mean rstd R;l:ldr;p:dX;l:lddx;p:dw db")
+
+
 # entry point → its argument structure; those with a scratch have a _workspace
 EXPORTS = {"gt_linear": gt_linear_args, "gt_linear_backward": gt_linear_grad_args,
            "gt_route": gt_route_args, "gt_route_backward": gt_route_grad_args,
-           "gt_experts": gt_experts_args, "gt_experts_backward": gt_experts_grad_args}
-NO_SCRATCH = ("gt_route_backward",)
+           "gt_experts": gt_experts_args, "gt_experts_backward": gt_experts_grad_args,
+           "gt_quantise": gt_quantise_args, "gt_linear_fp8": gt_linear_fp8_args,
+           "gt_norm": gt_norm_args, "gt_norm_backward": gt_norm_grad_args}
+NO_SCRATCH = ("gt_route_backward", "gt_quantise", "gt_norm")
 
 
 class Route(typing.NamedTuple):
@@ -87,6 +110,24 @@ class ExpertGrads(typing.NamedTuple):
     db1: typing.Any
     db2: typing.Any
     dweights: typing.Any
+
+
+class Codes(typing.NamedTuple):
+    """A matrix in 8-bit floating point: it stands for values·scales, a scale for 128 values
+    of a row, or for a square of 128×128."""
+    values: typing.Any    # float8_e4m3fn or float8_e5m2 [R, C]
+    scales: typing.Any    # float32 [R, ceil(C/128)], or [ceil(R/128), ceil(C/128)]
+
+
+class Quantised(typing.NamedTuple):
+    codes: typing.Any        # Codes of X, None if not wanted
+    transposed: typing.Any   # Codes of its transpose
+
+
+class NormGrads(typing.NamedTuple):
+    dX: typing.Any
+    dweight: typing.Any
+    dbias: typing.Any
 
 
 _lib = None
@@ -438,3 +479,187 @@ def gt_experts_backward(dY, X, route, W1, W2, P, b2=None, act="silu", gated=Fals
                                _one(b2, "b2", X, (E, D)), p, ldp, weights, offsets, order, place,
                                ptr[0], D, *ptr[1:]), X, workspace, stream)
     return g
+
+
+# ---- layers in 8-bit floating point
+
+def _blocks(n):
+    return (n + 127) // 128
+
+
+def _code(code):
+    if code not in CODES:
+        raise ValueError(f"unknown code {code!r}: one of {', '.join(CODES)}")
+    return CODES[code]
+
+
+def _code_of(t, name):
+    import torch
+    if t.dtype is torch.float8_e4m3fn:
+        return CODES["e4m3"]
+    if t.dtype is torch.float8_e5m2:
+        return CODES["e5m2"]
+    raise ValueError(f"{name} must be float8_e4m3fn or float8_e5m2")
+
+
+def _new_codes(rows, cols, code, block, device, stream):
+    """Codes to be filled: rows of whole 16-byte chunks, which the products read fastest."""
+    import torch
+    dtype = torch.float8_e4m3fn if code == CODES["e4m3"] else torch.float8_e5m2
+    wide = (cols + 15) // 16 * 16
+    q = _empty((rows, wide), dtype, device, stream)
+    return Codes(q if wide == cols else q[:, :cols],
+                 _empty((rows if block == 1 else _blocks(rows), _blocks(cols)), torch.float32, device, stream))
+
+
+def _codes(c, name, like, shape):
+    """A matrix of codes: its type, the rows that share a scale, both pointers and row strides."""
+    import torch
+    try:
+        values, scales = c
+    except (TypeError, ValueError):
+        raise ValueError(f"{name} must be Codes: values and their scales") from None
+    code = _code_of(values, name)
+    q, ldq = _tensor(values, name, like, shape, values.dtype)
+    rows, cols = shape
+    block = 1 if scales.dim() == 2 and scales.shape[0] == rows else 128
+    s, lds = _tensor(scales, f"the scales of {name}", like, (rows if block == 1 else _blocks(rows), _blocks(cols)),
+                     torch.float32)
+    return code, block, q, ldq, s, lds
+
+
+def gt_quantise(X, block="row", code="e4m3", pow2=False, need=("codes",), stream=None) -> Quantised:
+    """8-bit codes of X [M, N] with a scale for each 128 values of a row (block "row") or each
+    square of 128×128 ("square"). A scale is the block's largest magnitude over the type's (448;
+    57344 for code "e5m2"), with pow2 the next power of two. need: "codes" of X, and "transposed",
+    codes of its transpose with blocks along M, as the products of the gradients take them."""
+    _gpu(X, "X", 2)
+    M, N = X.shape
+    if block not in BLOCKS:
+        raise ValueError(f"unknown block {block!r}: one of {', '.join(BLOCKS)}")
+    need = (need,) if isinstance(need, str) else tuple(need)
+    if not need or set(need) - {"codes", "transposed"}:
+        raise ValueError('need is "codes", "transposed" or both')
+    c, b = _code(code), BLOCKS[block]
+    x, ldx = _tensor(X, "X", X, (M, N))
+    dt = _type(X, "X")
+    q = _new_codes(M, N, c, b, X.device, stream) if "codes" in need else None
+    t = _new_codes(N, M, c, b, X.device, stream) if "transposed" in need else None
+    _call("gt_quantise",
+          gt_quantise_args(M, N, dt, c, b, int(bool(pow2)), x, ldx, *_places(q), *_places(t)), X, None, stream)
+    return Quantised(q, t)
+
+
+def _places(c):
+    if c is None:
+        return None, 0, None, 0
+    values, scales = c
+    return (values.data_ptr(), max(values.stride(0), values.shape[1]), scales.data_ptr(),
+            max(scales.stride(0), scales.shape[1]))
+
+
+def gt_linear_fp8(X, W, bias=None, residual=None, act="none", gated=False, Y=None, workspace=None,
+                  stream=None):
+    """Y = act(X·Wᵀ + bias) + residual of Codes X [M, K] and W [N, K], fused into the product: K
+    lies along the rows of both, blocks of 128 of it are summed and scaled in fp32. gated: W [2N, K]
+    and bias [2N] hold a gate's rows, then the up's, Y = act(gate)·up + residual. bias and residual
+    [M, N] float32 or bfloat16, of one type; Y in that type (bfloat16 without either) unless given,
+    in float32 or in theirs; it may be the residual itself. The gradients are products of
+    codes too: dX = gt_linear_fp8(codes of dY, transposed codes of W), dW [N, K] =
+    gt_linear_fp8(transposed codes of dY, transposed codes of X)."""
+    import torch
+    try:
+        like, (wide, K) = X[0], W[0].shape
+    except (TypeError, ValueError, IndexError, AttributeError):
+        raise ValueError("X and W must be Codes of matrices") from None
+    _gpu(like, "X", 2)
+    M = like.shape[0]
+    N = wide // 2 if gated else wide
+    if gated and wide % 2:
+        raise ValueError("a gated W has an even number of rows")
+    xc, xb, x, ldx, sx, ldsx = _codes(X, "X", like, (M, K))
+    wc, wb, w, ldw, sw, ldsw = _codes(W, "W", like, (wide, K))
+    typed = bias if bias is not None else residual
+    if Y is None:
+        Y = _empty((M, N), torch.bfloat16 if typed is None else typed.dtype, like.device, stream)
+    typed = Y if typed is None else typed
+    dt = _type(typed, "Y" if typed is Y else "bias" if typed is bias else "residual")
+    b = _one(bias, "bias", like, (wide,), typed.dtype)
+    r, ldr = _pair(residual, "residual", like, (M, N), typed.dtype)
+    out = _result_type(Y, "Y", typed)
+    y, ldy = _tensor(Y, "Y", like, (M, N), Y.dtype)
+    _call("gt_linear_fp8",
+          gt_linear_fp8_args(M, N, K, dt, _act(act, gated), out, xc, wc, xb, wb, 0, x, ldx, sx, ldsx, w, ldw,
+                             sw, ldsw, b, r, ldr, y, ldy), like, workspace, stream)
+    return Y
+
+
+def _norm(X, weight, bias, eps, Y, mean, rstd, codes, code, pow2, stream):
+    import torch
+    M, N = X.shape
+    dt = _type(X, "X")
+    eps = float(eps)
+    if not 0.0 <= eps < float("inf"):
+        raise ValueError(f"eps is {eps}: finite and not negative")
+    x, ldx = _tensor(X, "X", X, (M, N))
+    typed = weight if weight is not None else bias if bias is not None else X
+    wt = _result_type(typed, "weight" if typed is weight else "bias", X)
+    w = _one(weight, "weight", X, (N,), typed.dtype)
+    b = _one(bias, "bias", X, (N,), typed.dtype)
+    y, ldy = _pair(Y, "Y", X, (M, N))
+    _call("gt_norm",
+          gt_norm_args(M, N, dt, wt, code, int(bool(pow2)), eps, 0, x, ldx, w, b, y, ldy,
+                       _one(mean, "mean", X, (M,), torch.float32), _one(rstd, "rstd", X, (M,), torch.float32),
+                       *_places(codes)), X, None, stream)
+
+
+def gt_norm(X, weight=None, bias=None, eps=1e-5, Y=None, mean=None, rstd=None, stream=None):
+    """Layer norm: Y = (X − mean)·rstd·weight + bias over the rows of X [M, N], rstd =
+    1/√(variance + eps). weight, bias [N]: in X's type or float32. mean, rstd: float32 tensors
+    [M] that receive the rows' statistics for the gradients. Y may be X itself."""
+    _gpu(X, "X", 2)
+    if Y is None:
+        Y = _empty(X.shape, X.dtype, X.device, stream)
+    _norm(X, weight, bias, eps, Y, mean, rstd, None, 0, False, stream)
+    return Y
+
+
+def gt_norm_fp8(X, weight=None, bias=None, eps=1e-5, code="e4m3", pow2=False, Y=None, mean=None, rstd=None,
+                stream=None) -> Codes:
+    """gt_norm whose result leaves as Codes with a scale for each 128 values of a row, as
+    gt_quantise would give them of the unrounded values: what gt_linear_fp8 takes. Y: a tensor that
+    receives the values as well."""
+    _gpu(X, "X", 2)
+    c = _code(code)
+    codes = _new_codes(*X.shape, c, 1, X.device, stream)
+    _norm(X, weight, bias, eps, Y, mean, rstd, codes, c, pow2, stream)
+    return codes
+
+
+def gt_norm_backward(dY, X, mean, rstd, weight=None, residual=None, bias=True, dX=None,
+                     need=("dX", "dweight"), workspace=None, stream=None) -> NormGrads:
+    """The gradients of gt_norm from dY [M, N] and the statistics it kept: dX in X's type, dweight
+    and dbias (None unless bias) [N] in float32. residual [M, N]: a gradient that reaches X by
+    another way, added to dX. dX may be the residual or dY itself. need: which of dX and
+    dweight are wanted."""
+    import torch
+    _gpu(dY, "dY", 2)
+    _gpu(X, "X", 2)
+    M, N = X.shape
+    dt = _type(X, "X")
+    if dX is None and "dX" in need:
+        dX = _empty((M, N), X.dtype, X.device, stream)
+    dw = _empty((N,), torch.float32, X.device, stream) if "dweight" in need else None
+    db = _empty((N,), torch.float32, X.device, stream) if bias else None
+    dy, lddy = _tensor(dY, "dY", X, (M, N))
+    x, ldx = _tensor(X, "X", X, (M, N))
+    wt = dt if weight is None else _result_type(weight, "weight", X)
+    w = None if weight is None else _whole(weight, "weight", X, (N,), weight.dtype)
+    r, ldr = _pair(residual, "residual", X, (M, N))
+    dx, lddx = _pair(dX, "dX", X, (M, N))
+    _call("gt_norm_backward",
+          gt_norm_grad_args(M, N, dt, wt, dy, lddy, x, ldx, w, _whole(mean, "mean", X, (M,), torch.float32),
+                            _whole(rstd, "rstd", X, (M,), torch.float32), r, ldr, dx, lddx,
+                            None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr()),
+          X, workspace, stream)
+    return NormGrads(dX, dw, db)
