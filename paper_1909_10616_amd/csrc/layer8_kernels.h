@@ -30,6 +30,17 @@ struct Product8 {
   int32_t acode, bcode;
 };
 
+// The tiles: rows, columns, wavefronts along each; bytes of LDS of a stage, its codes and scales.
+struct Tile8 {
+  int BM, BN, NWM, NWN;
+};
+constexpr int kTiles8 = 2;
+constexpr Tile8 tile8(int tile) { return tile == 0 ? Tile8{256, 256, 2, 4} : Tile8{128, 128, 2, 2}; }
+constexpr unsigned kStage8(int tile) { return (tile8(tile).BM + tile8(tile).BN) * 132u; }
+// exact: sums of all that fp32 holds (tile 1 alone), else a bf16 Y's; uni: the rows of B in
+// either half of a wavefront's columns share their scales.
+hipError_t launch_product8(int dtype, int tile, bool exact, bool uni, const Product8& a, hipStream_t s);
+
 // Few rows, straight from memory: `rows` (16, 32 or 64) a workgroup.
 hipError_t launch_rows8(int dtype, int rows, const Product8& a, hipStream_t s);
 

@@ -13,6 +13,25 @@
 #include "layer_kernels.h"
 
 namespace gt {
+
+#define P8_DECLARE(t, a, b) hipError_t product8_##t##_##a##_##b(int, bool, bool, const Product8&, hipStream_t);
+P8_DECLARE(0, 0, 0)
+P8_DECLARE(0, 0, 1)
+P8_DECLARE(0, 1, 0)
+P8_DECLARE(0, 1, 1)
+P8_DECLARE(1, 0, 0)
+P8_DECLARE(1, 0, 1)
+P8_DECLARE(1, 1, 0)
+P8_DECLARE(1, 1, 1)
+#undef P8_DECLARE
+
+hipError_t launch_product8(int dtype, int tile, bool exact, bool uni, const Product8& a, hipStream_t s) {
+  using Fn = hipError_t (*)(int, bool, bool, const Product8&, hipStream_t);
+  constexpr Fn kFn[kTiles8][2][2] = {{{product8_0_0_0, product8_0_0_1}, {product8_0_1_0, product8_0_1_1}},
+                                     {{product8_1_0_0, product8_1_0_1}, {product8_1_1_0, product8_1_1_1}}};
+  return kFn[tile][a.acode][a.bcode](dtype, exact, uni, a, s);
+}
+
 namespace {
 
 bool code_ok(int c) { return c == GT_E4M3 || c == GT_E5M2; }
@@ -140,6 +159,8 @@ int linear8_checks(const gt_linear_fp8_args* a, bool pointers) {
 struct Linear8 {
   Product8 q{};
   int rows = 0;   // > 0: the kernel of a few rows, so many a workgroup
+  int tile = 0;
+  bool exact = false, uni = false;
 };
 
 Linear8 linear8(const gt_linear_fp8_args& g) {
@@ -173,10 +194,24 @@ Linear8 linear8(const gt_linear_fp8_args& g) {
   e.R = g.R;
   e.ldr = g.ldr;
   e.ldpart = up(a.N, 4) * (e.gated ? 2 : 1);
+  a.splits = 1;
+  l.exact = g.out_dtype == GT_F32;
+  l.uni = g.wblock == 128 && (!e.gated || a.N % 128 == 0);
+  const bool tiles = a.M > 64 && aligned(a.A, 16) && aligned(a.B, 16) && a.lda % 16 == 0 && a.ldb % 16 == 0 &&
+                     256 * std::max(a.lda, a.ldb) < kMaxExtent && a.K < kMaxExtent - 1024;
+  if (tiles) {
+    l.tile = l.exact || a.M <= 1024 ? 1 : 0;
+    const Tile8 t = tile8(l.tile);
+    const int64_t wide = e.gated ? 2 * a.N : a.N, tm = (a.M + t.BM - 1) / t.BM, tn = (wide + t.BN - 1) / t.BN;
+    if (tm * tn * 64 * t.NWM * t.NWN < kMaxItems) {
+      a.tilesM = static_cast<int>(tm);
+      a.tilesN = static_cast<int>(tn);
+      return l;
+    }
+  }
   l.rows = g.M <= 16 ? 16 : g.M <= 32 || e.gated ? 32 : 64;
   a.tilesN = static_cast<int>((a.N + 15) / 16);
   a.tilesM = static_cast<int>((a.M + l.rows - 1) / l.rows);
-  a.splits = 1;
   return l;
 }
 
@@ -192,7 +227,10 @@ int linear_fp8_impl(const gt_linear_fp8_args* a, void* ws, int64_t ws_bytes, voi
   GT_CHECK(scratch_ok(ws, ws_bytes, 0));
   if (a->M == 0) return GT_OK;
   const Linear8 l = linear8(*a);
-  GT_TRY(launch_rows8(a->dtype, l.rows, l.q, static_cast<hipStream_t>(stream)), "8-bit product");
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  GT_TRY(l.rows > 0 ? launch_rows8(a->dtype, l.rows, l.q, s)
+                    : launch_product8(a->dtype, l.tile, l.exact, l.uni, l.q, s),
+         "8-bit product");
   return GT_OK;
 }
 

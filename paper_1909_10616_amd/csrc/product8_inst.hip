@@ -1,0 +1,64 @@
+// One translation unit of the 8-bit products: a tile and both operands' codes
+// (-DP8_TILE=<0|1> -DP8_AC=<0|1> -DP8_BC=<0|1>).
+#include <atomic>
+
+#include "product8.hpp"
+
+#if !defined(P8_TILE) || !defined(P8_AC) || !defined(P8_BC)
+#error "compile with -DP8_TILE=<0|1> -DP8_AC=<0|1> -DP8_BC=<0|1>"
+#endif
+
+#define P8_CAT(t, a, b) product8_##t##_##a##_##b
+#define P8_NAME(t, a, b) P8_CAT(t, a, b)
+
+namespace gt {
+namespace {
+
+template <int DT, bool EXACT, int EPI, bool UNI>
+hipError_t go(const Product8& a, hipStream_t s) {
+  constexpr auto* fn = product8_kernel<DT, EXACT, P8_AC, P8_BC, P8_TILE, EPI, UNI>;
+  constexpr Tile8 t = tile8(P8_TILE);
+  // the dynamic LDS limit is raised once per kernel and device
+  static std::atomic<uint64_t> attr{0};
+  constexpr size_t lds = 2 * kStage8(P8_TILE);
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t{1} << dev : 0;
+  if (!bit || !(attr.load(std::memory_order_acquire) & bit)) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
+                            static_cast<int>(lds));
+    if (e != hipSuccess) return e;
+    attr.fetch_or(bit, std::memory_order_release);
+  }
+  const dim3 grid(static_cast<unsigned>(a.p.tilesM) * static_cast<unsigned>(a.p.tilesN),
+                  static_cast<unsigned>(a.p.splits));
+  hipLaunchKernelGGL(fn, grid, dim3(64 * t.NWM * t.NWN), lds, s, a);
+  return hipGetLastError();
+}
+
+template <int DT, bool EXACT, bool UNI>
+hipError_t by_epilogue(const Product8& a, hipStream_t s) {
+  if (a.p.e.epi == kEpiGated) return go<DT, EXACT, kEpiGated, UNI>(a, s);
+  if (a.p.e.epi == kEpiLinear) return go<DT, EXACT, kEpiLinear, UNI>(a, s);
+  // (a K slice's sums have no type)
+  if constexpr (DT == 1) return go<1, EXACT, kEpiPart, UNI>(a, s);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t P8_NAME(P8_TILE, P8_AC, P8_BC)(int dtype, bool exact, bool uni, const Product8& a, hipStream_t s) {
+  if (!exact) {
+    if (dtype != GT_BF16) return hipErrorInvalidValue;
+    return uni ? by_epilogue<1, false, true>(a, s) : by_epilogue<1, false, false>(a, s);
+  }
+#if P8_TILE == 1
+  if (dtype == GT_BF16 || a.p.e.epi == kEpiPart) return by_epilogue<1, true, false>(a, s);
+  return by_epilogue<0, true, false>(a, s);
+#else
+  return hipErrorInvalidValue;
+#endif
+}
+
+}  // namespace gt
