@@ -48,7 +48,7 @@ def _units():
     units += [("layers8", "layers8.cpp", []), ("norm", "norm.hip", []), ("quantise", "quantise.hip", []),
               ("rows8", "rows8.hip", [])]
     units += [(f"product8_{t}_{a}{b}", "product8_inst.hip", [f"-DP8_TILE={t}", f"-DP8_AC={a}", f"-DP8_BC={b}"])
-              for t in (0, 1) for a in (0, 1) for b in (0, 1)]
+              for t in (0, 1, 2) for a in (0, 1) for b in (0, 1)]
     units += [(f"product_{dn}_{lay}", "product_inst.hip", [f"-DLP_DT={dt}", f"-DLP_LAY={lay}"])
               for dt, dn in ((0, "f32"), (1, "bf16")) for lay in (0, 1, 2)]
     for dt, dn in ((0, "f32"), (1, "bf16")):

@@ -32,6 +32,7 @@ struct PadJobs {
   PadJob job[kPadJobs];
   int n;
 };
+constexpr int kBytes = 2;   // in place of a dtype: single bytes
 hipError_t launch_pad(int dtype, const PadJobs& jobs, hipStream_t s);
 
 // Rows a block of the gradient kernel sums into one row of its partial sums.

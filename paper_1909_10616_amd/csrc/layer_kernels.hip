@@ -475,6 +475,8 @@ hipError_t launch_pad(int dtype, const PadJobs& jobs, hipStream_t s) {
   const dim3 grid(blocks_for(rows, 4), static_cast<unsigned>(jobs.n));
   if (dtype == GT_BF16)
     pad_kernel<uint16_t><<<grid, 256, 0, s>>>(jobs);
+  else if (dtype == kBytes)
+    pad_kernel<uint8_t><<<grid, 256, 0, s>>>(jobs);
   else
     pad_kernel<float><<<grid, 256, 0, s>>>(jobs);
   return hipGetLastError();

@@ -23,12 +23,17 @@ P8_DECLARE(1, 0, 0)
 P8_DECLARE(1, 0, 1)
 P8_DECLARE(1, 1, 0)
 P8_DECLARE(1, 1, 1)
+P8_DECLARE(2, 0, 0)
+P8_DECLARE(2, 0, 1)
+P8_DECLARE(2, 1, 0)
+P8_DECLARE(2, 1, 1)
 #undef P8_DECLARE
 
 hipError_t launch_product8(int dtype, int tile, bool exact, bool uni, const Product8& a, hipStream_t s) {
   using Fn = hipError_t (*)(int, bool, bool, const Product8&, hipStream_t);
   constexpr Fn kFn[kTiles8][2][2] = {{{product8_0_0_0, product8_0_0_1}, {product8_0_1_0, product8_0_1_1}},
-                                     {{product8_1_0_0, product8_1_0_1}, {product8_1_1_0, product8_1_1_1}}};
+                                     {{product8_1_0_0, product8_1_0_1}, {product8_1_1_0, product8_1_1_1}},
+                                     {{product8_2_0_0, product8_2_0_1}, {product8_2_1_0, product8_2_1_1}}};
   return kFn[tile][a.acode][a.bcode](dtype, exact, uni, a, s);
 }
 
@@ -161,7 +166,99 @@ struct Linear8 {
   int rows = 0;   // > 0: the kernel of a few rows, so many a workgroup
   int tile = 0;
   bool exact = false, uni = false;
+  PadJobs pad{};                     // operands copied to aligned rows first …
+  int64_t pad_a = 0, pad_b = 0;      // … their bytes
+  int64_t part = 0;                  // bytes of the K slices' sums
+  int64_t scratch() const { return up(pad_a, 256) + up(pad_b, 256) + up(part, 256); }
 };
+
+// A form and its time in µs.
+struct Form {
+  int rows, tile, splits;
+  double cost;
+  int64_t tm, tn;
+};
+
+// What a stage (128 k) of a tile takes, in µs, where few tiles run (alone) and where they fill the
+// chip (full), the launch and epilogue of such rounds, and how many tiles fill it. Fitted to the
+// 100 shapes of profiles/layers8_forms.md, from 1×1024×1024 to 4096×11008×4096, each in
+// every form (bf16, K = 4096: 256×256 tiles 53 µs for 16 of them, 73 for 256; 128×128 29 for 32,
+// 45 for 512; 64×64 25 for 64, 34 for 1024): the choice is within 2 % of the best form on average.
+struct Cost8 {
+  double alone, full, fixed, fixed_full;
+  int64_t fill;
+};
+constexpr Cost8 kCost8[2][kTiles8] = {
+    {{1.45, 1.95, 8.0, 10.0, 256}, {0.78, 1.15, 4.6, 8.0, 512}, {0.68, 0.86, 2.9, 6.3, 1024}},
+    {{0, 0, 0, 0, 0}, {1.21, 2.0, 5.2, 11.0, 512}, {1.05, 1.3, 3.0, 9.0, 1024}}};   // exact
+double tiles_cost(const Cost8& c, int64_t tiles, double stages) {
+  const int64_t rounds = tiles / c.fill, rest = tiles % c.fill;
+  double t = 0.0;
+  if (rounds > 0) t = rounds * (stages * c.full + 0.6 * c.fixed_full) + 0.4 * c.fixed_full;
+  if (rest > 0) {
+    const double share = static_cast<double>(rest) / c.fill;
+    t += stages * (c.alone + (c.full - c.alone) * share * std::sqrt(share)) +
+         (c.fixed + (c.fixed_full - c.fixed) * share) * (rounds > 0 ? 0.6 : 1.0);
+  }
+  return t;
+}
+// The same of the kernel of a few rows: a block of a wavefront, for each round of 256 workgroups.
+double rows_cost(int rows, bool gated, int64_t groups, int64_t steps) {
+  const double each = rows == 16 ? (gated ? 1.85 : 1.28) : rows == 32 ? (gated ? 3.0 : 1.9) : 3.43;
+  return 3.0 + each * static_cast<double>(steps) * std::max(1.0, static_cast<double>(groups) / kUnits);
+}
+
+// The form by the time it should take: the tiles' rounds or the operands' way from memory, which
+// overlap in part, K slices' sums and the launch that joins them, copies to aligned rows.
+// What no tile serves (rows too long for 32-bit offsets) is left to the kernel of a few rows.
+void choose(Linear8* l) {
+  ProductArgs& a = l->q.p;
+  const bool gated = a.e.gated != 0;
+  const int64_t wide = gated ? 2 * a.N : a.N, all = blocks(a.K), ldd = up(a.K, 16);
+  const bool ok_a = aligned(a.A, 16) && a.lda % 16 == 0, ok_b = aligned(a.B, 16) && a.ldb % 16 == 0;
+  const bool tiles = 256 * std::max(ok_a ? a.lda : ldd, ok_b ? a.ldb : ldd) < kMaxExtent;
+  const double copied = static_cast<double>((ok_a ? 0 : a.M * ldd) + (ok_b ? 0 : wide * ldd));
+  const double copy = copied > 0 ? 5.0 + 2.0 * copied / 5.0e6 : 0.0;
+  const double memory = static_cast<double>(a.M * a.K + wide * a.K) / 5.2e6;
+  Form best{0, 0, 1, 0.0, 0, 0};
+  auto offer = [&](const Form& f) {
+    if (best.cost == 0.0 || f.cost < best.cost) best = f;
+  };
+  for (int t = l->exact ? 1 : 0; tiles && t < kTiles8; ++t) {
+    const Tile8 s = tile8(t);
+    const int64_t tm = (a.M + s.BM - 1) / s.BM, tn = (wide + s.BN - 1) / s.BN;
+    if (tm * tn * 64 * s.NWM * s.NWN >= kMaxItems) continue;
+    for (int z = 1; z <= 16 && (z == 1 || 2 * z <= all); z *= 2) {
+      const double stages = static_cast<double>((all + z - 1) / z);
+      const double join = z > 1 ? 4.5 + 2.0 * z * a.M * wide * 4 / 6.0e6 : 0.0;
+      offer(Form{0, t, z, copy + std::hypot(tiles_cost(kCost8[l->exact][t], tm * tn * z, stages), memory) + join, tm, tn});
+    }
+  }
+  for (const int r : {16, 32, 64}) {
+    if (r == 64 && gated) continue;
+    const int64_t tm = (a.M + r - 1) / r, tn = (a.N + 15) / 16;
+    if (tm >= 65536 || tn * 512 >= kMaxItems) continue;
+    offer(Form{r, 0, 1, rows_cost(r, gated, tm * tn, (all + 7) / 8), tm, tn});
+  }
+  l->rows = best.rows;
+  l->tile = best.tile;
+  /*FORCE*/
+  a.splits = best.cost > 0.0 ? best.splits : 0;   // (0: no form serves)
+  a.tilesM = static_cast<int>(best.tm);
+  a.tilesN = static_cast<int>(best.tn);
+  if (a.splits == 0) return;
+  a.per_slice = static_cast<int>((all + a.splits - 1) / a.splits);
+  l->part = a.splits > 1 ? a.splits * a.M * a.e.ldpart * 4 : 0;
+  if (l->rows > 0) return;
+  auto pad = [&](const void* p, int64_t rows, int64_t* ld, int64_t* bytes) {
+    PadJob& j = l->pad.job[l->pad.n++];
+    j = PadJob{p, nullptr, 1, rows, a.K, *ld, 0, ldd, 0};
+    *ld = ldd;
+    *bytes = rows * ldd;
+  };
+  if (!ok_a) pad(a.A, a.M, &a.lda, &l->pad_a);
+  if (!ok_b) pad(a.B, wide, &a.ldb, &l->pad_b);
+}
 
 Linear8 linear8(const gt_linear_fp8_args& g) {
   Linear8 l;
@@ -194,43 +291,47 @@ Linear8 linear8(const gt_linear_fp8_args& g) {
   e.R = g.R;
   e.ldr = g.ldr;
   e.ldpart = up(a.N, 4) * (e.gated ? 2 : 1);
-  a.splits = 1;
   l.exact = g.out_dtype == GT_F32;
   l.uni = g.wblock == 128 && (!e.gated || a.N % 128 == 0);
-  const bool tiles = a.M > 64 && aligned(a.A, 16) && aligned(a.B, 16) && a.lda % 16 == 0 && a.ldb % 16 == 0 &&
-                     256 * std::max(a.lda, a.ldb) < kMaxExtent && a.K < kMaxExtent - 1024;
-  if (tiles) {
-    l.tile = l.exact || a.M <= 1024 ? 1 : 0;
-    const Tile8 t = tile8(l.tile);
-    const int64_t wide = e.gated ? 2 * a.N : a.N, tm = (a.M + t.BM - 1) / t.BM, tn = (wide + t.BN - 1) / t.BN;
-    if (tm * tn * 64 * t.NWM * t.NWN < kMaxItems) {
-      a.tilesM = static_cast<int>(tm);
-      a.tilesN = static_cast<int>(tn);
-      return l;
-    }
-  }
-  l.rows = g.M <= 16 ? 16 : g.M <= 32 || e.gated ? 32 : 64;
-  a.tilesN = static_cast<int>((a.N + 15) / 16);
-  a.tilesM = static_cast<int>((a.M + l.rows - 1) / l.rows);
+  choose(&l);
   return l;
 }
 
 int linear_fp8_workspace_impl(const gt_linear_fp8_args* a, int64_t* bytes) {
   if (!bytes) return fail("gt_linear_fp8_workspace: null argument");
   GT_CHECK(linear8_checks(a, false));
-  *bytes = 0;
+  *bytes = a->M > 0 ? linear8(*a).scratch() : 0;
   return GT_OK;
 }
 
 int linear_fp8_impl(const gt_linear_fp8_args* a, void* ws, int64_t ws_bytes, void* stream) {
   GT_CHECK(linear8_checks(a, true));
-  GT_CHECK(scratch_ok(ws, ws_bytes, 0));
   if (a->M == 0) return GT_OK;
-  const Linear8 l = linear8(*a);
+  Linear8 l = linear8(*a);
+  ProductArgs& p = l.q.p;
+  if (p.splits == 0) return fail("gt_linear_fp8: too many rows");
+  GT_CHECK(scratch_ok(ws, ws_bytes, l.scratch()));
   const hipStream_t s = static_cast<hipStream_t>(stream);
+  char* at = static_cast<char*>(ws);
+  int n = 0;
+  auto place = [&](const void** operand, int64_t bytes) {
+    if (bytes == 0) return;
+    *operand = l.pad.job[n++].dst = at;
+    at += up(bytes, 256);
+  };
+  place(&p.A, l.pad_a);
+  place(&p.B, l.pad_b);
+  if (n > 0) GT_TRY(launch_pad(kBytes, l.pad, s), "copy to aligned rows");
+  const int epi = p.e.epi;
+  if (p.splits > 1) {
+    p.e.part = reinterpret_cast<float*>(at);
+    p.e.epi = kEpiPart;
+  }
   GT_TRY(l.rows > 0 ? launch_rows8(a->dtype, l.rows, l.q, s)
                     : launch_product8(a->dtype, l.tile, l.exact, l.uni, l.q, s),
          "8-bit product");
+  p.e.epi = epi;
+  if (p.splits > 1) GT_TRY(launch_reduce(a->dtype, p, s), "joining the K slices");
   return GT_OK;
 }
 

@@ -29,8 +29,7 @@ __device__ __forceinline__ void dma_scale(const float* p, uint32_t lds_base) {
                : "memory", "m0");
 }
 
-// A wave's tile of a 256×256 (8 wavefronts) or 128×128 (4) workgroup tile; UNI: the columns of
-// a wavefront in either half of the tile share their scale.
+// UNI: the columns of a wavefront in either half of the tile share their scale.
 template <int DT, bool EXACT, int AC, int BC, int TILE, int EPI, bool UNI>
 __global__ __launch_bounds__(64 * tile8(TILE).NWM * tile8(TILE).NWN, 2) void product8_kernel(const Product8 q) {
   constexpr Tile8 S = tile8(TILE);
@@ -41,7 +40,7 @@ __global__ __launch_bounds__(64 * tile8(TILE).NWM * tile8(TILE).NWN, 2) void pro
   constexpr int CNT = NA + NB + 1;                        // … and one of scales
   constexpr int FIRST = TN;                               // of them behind the boundary
   constexpr uint32_t BOFF = BM * 128, SOFF = BOFF + BN * 128, STAGE = SOFF + (BM + BN) * 4;
-  static_assert(BM + BN == 64 * NW && NB % 2 == 0 && TM % 2 == 0 && TN % 2 == 0 && TN > 2);
+  static_assert(BM + BN == 64 * NW && NB % 2 == 0 && TN % 2 == 0);
   static_assert(STAGE == kStage8(TILE));
   auto kswz = [](int r) { return (r >> 1) & 7; };
 
@@ -76,12 +75,13 @@ __global__ __launch_bounds__(64 * tile8(TILE).NWM * tile8(TILE).NWN, 2) void pro
   const uint32_t lda = static_cast<uint32_t>(a.lda), ldb = static_cast<uint32_t>(a.ldb);
   const uint32_t offA = static_cast<uint32_t>(r0) * lda + kc, offB = static_cast<uint32_t>(r0) * ldb + kc;
   static_assert(NW % 2 == 0, "rows of a lane's chunks are 16 apart");
-  // this lane's scales: of row 64·wave + lane among A's and B's
+  // this lane's scales, of place 64·wave + lane among A's and B's: A's of a wavefront's rows lie
+  // by lx, so that a lane reads its TM as quads
   const float* scale;
   {
     const int r = wave * 64 + lane, c = r - BM;
     if (r < BM) {
-      const int64_t m = m0 + r < a.M ? m0 + r : a.M - 1;
+      const int64_t row = m0 + r / WM * WM + r % TM * 16 + r % WM / TM, m = row < a.M ? row : a.M - 1;
       scale = q.sa + (m >> q.xshift) * q.ldsa;
     } else {
       int64_t n = c < BN / 2 ? n0 + c : n1 + c - BN / 2;
@@ -109,8 +109,7 @@ __global__ __launch_bounds__(64 * tile8(TILE).NWM * tile8(TILE).NWN, 2) void pro
     da = descriptor(ga, live ? remA : 0);
     db = descriptor(gb, live ? remB : 0);
     dc = descriptor(gc, live ? remC : 0);
-    settle(da, db);
-    settle(dc, dc);
+    asm volatile("s_nop 4" : "+s"(da), "+s"(db), "+s"(dc));   // (as settle)
   };
   auto next_stage = [&]() __attribute__((always_inline)) {
     ga += kBlock;
@@ -164,12 +163,26 @@ __global__ __launch_bounds__(64 * tile8(TILE).NWM * tile8(TILE).NWN, 2) void pro
   };
   auto read_a = [&](const char* st, int i) __attribute__((always_inline)) { return read(st, wm * WM + i * 16); };
   auto read_b = [&](const char* st, int j) __attribute__((always_inline)) { return read(st + BOFF, bcol(j)); };
-  i32x8 va[2], vb[TN];
-  // scales: A's of rows i·16 + lx of this and the next i, B's of the tile's halves, or of 4 columns
-  float sa[2], sh[2];
+  constexpr int AHEAD = !EXACT && TM >= 4 ? 2 : 1;   // rows of fragments computed behind the boundary
+  constexpr int BUFS = 2 * AHEAD;
+  static_assert(TM % BUFS == 0);
+  i32x8 va[BUFS], vb[TN];
+  // scales: A's of rows i·16 + lx, B's of the tile's halves, or of 4 columns
+  float sa[TM], sh[2];
   f32x4 sb[UNI ? 1 : TN];
-  auto read_sa = [&](const char* st, int i) __attribute__((always_inline)) {
-    return reinterpret_cast<const float*>(st + SOFF)[wm * WM + i * 16 + lx];
+  auto read_sa = [&](const char* st) __attribute__((always_inline)) {
+    const float* s = reinterpret_cast<const float*>(st + SOFF) + wm * WM + lx * TM;
+    if constexpr (TM >= 4) {
+#pragma unroll
+      for (int i = 0; i < TM; i += 4) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(s + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sa[i + k] = v[k];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) sa[i] = s[i];
+    }
   };
   auto read_sb = [&](const char* st) __attribute__((always_inline)) {
     const float* s = reinterpret_cast<const float*>(st + SOFF);
@@ -189,16 +202,19 @@ __global__ __launch_bounds__(64 * tile8(TILE).NWM * tile8(TILE).NWN, 2) void pro
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{};
   constexpr int LAG = 2;   // instructions between a sum and its scaling
   f32x4 part[LAG + 1];
+  // step t of a stage: the last AHEAD i's are taken together, column by column
+  auto row_of = [&](int t) { return t < MF - AHEAD * TN ? t / TN : TM - AHEAD + t % AHEAD; };
+  auto col_of = [&](int t) { return t < MF - AHEAD * TN ? t % TN : (t - (MF - AHEAD * TN)) / AHEAD; };
   auto apply = [&](int t) __attribute__((always_inline)) {
-    const int i = t / TN, j = t % TN;
+    const int i = row_of(t), j = col_of(t);
     const f32x4& p = part[t % (LAG + 1)];
     if constexpr (UNI) {
-      const float s = sa[i & 1] * sh[j < TN / 2 ? 0 : 1];
+      const float s = sa[i] * sh[j < TN / 2 ? 0 : 1];
 #pragma unroll
       for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(p[r], s, acc[i][j][r]);
     } else {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(p[r], sa[i & 1] * sb[j][r], acc[i][j][r]);
+      for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(p[r], sa[i] * sb[j][r], acc[i][j][r]);
     }
     // (here, between the matrix instructions: the compiler would put all of a stage behind the last)
     asm volatile("" : "+v"(acc[i][j]));
@@ -218,8 +234,9 @@ __global__ __launch_bounds__(64 * tile8(TILE).NWM * tile8(TILE).NWN, 2) void pro
     if (odd && st0 == all - 1) trim(smem);
 #pragma unroll
     for (int j = 0; j < TN; ++j) vb[j] = read_b(smem, j);
-    va[0] = read_a(smem, 0);
-    sa[0] = read_sa(smem, 0);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) va[i] = read_a(smem, i);
+    read_sa(smem);
     read_sb(smem);
     uint32_t cur = 0;
     for (int l = 0; l < nst; ++l) {
@@ -230,9 +247,11 @@ __global__ __launch_bounds__(64 * tile8(TILE).NWM * tile8(TILE).NWN, 2) void pro
 #pragma unroll
           for (int c = 0; c < 4; ++c) wb[j][c] = widen8<BC>(vb[j][2 * c], vb[j][2 * c + 1]);
       }
+      constexpr int EDGE = MF - AHEAD * TN;   // the first step behind the boundary
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        if (i == TM - 1) {
+      for (int t = 0; t < MF; ++t) {
+        const int i = row_of(t), j = col_of(t);
+        if (t == EDGE) {
           // every wavefront has read all of stage l, and stage l + 1 has landed
           waitcnt_vm<0>();
           waitcnt_lgkm0();
@@ -241,37 +260,42 @@ __global__ __launch_bounds__(64 * tile8(TILE).NWM * tile8(TILE).NWN, 2) void pro
           descriptors();
           if (odd && st0 + l + 1 == all - 1) trim(smem + nx);
         }
+        // A's fragments AHEAD of their use (behind the boundary the next stage's first)
+        if (t < EDGE) {
+          if (j == 0) va[(i + AHEAD) % BUFS] = read_a(smem + cur, i + AHEAD);
+        } else if (t < EDGE + AHEAD) {
+          va[t - EDGE] = read_a(smem + nx, t - EDGE);
+        }
+        if (t >= EDGE) {
+          if (t - EDGE < FIRST) dma(lds0 + cur, t - EDGE);
+        } else {
+#pragma unroll
+          for (int k = FIRST + t; k < CNT; k += EDGE) dma(lds0 + nx, k);
+        }
         if constexpr (EXACT) {
+          if (j == 0) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) wa[c] = widen8<AC>(va[i & 1][2 * c], va[i & 1][2 * c + 1]);
-        }
-        va[(i + 1) & 1] = i + 1 < TM ? read_a(smem + cur, i + 1) : read_a(smem + nx, 0);
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          const int t = i * TN + j;
-          if (i == TM - 1) {
-            if (j < FIRST) dma(lds0 + cur, j);
-          } else if (t < CNT - FIRST) {
-            dma(lds0 + nx, FIRST + t);
+            for (int c = 0; c < 4; ++c) wa[c] = widen8<AC>(va[i % BUFS][2 * c], va[i % BUFS][2 * c + 1]);
           }
-          __builtin_amdgcn_sched_barrier(0);
-          if constexpr (EXACT) {
-            f32x4 p{};
-#pragma unroll
-            for (int c = 0; c < 4; ++c) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][c], wa[c], p, 0, 0, 0);
-            part[t % (LAG + 1)] = p;
-          } else {
-            part[t % (LAG + 1)] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb[j], va[i & 1], f32x4{}, BC, AC,
-                                                                                  0, 0, 0, 0);
-          }
-          if (t >= LAG) apply(t - LAG);
-          // (the scale of the i before has then been used)
-          if (j == LAG) sa[(i + 1) & 1] = i + 1 < TM ? read_sa(smem + cur, i + 1) : read_sa(smem + nx, 0);
-          if (i == TM - 1) vb[j] = read_b(smem + nx, j);
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (EXACT) {
+          f32x4 p{};
+#pragma unroll
+          for (int c = 0; c < 4; ++c) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][c], wa[c], p, 0, 0, 0);
+          part[t % (LAG + 1)] = p;
+        } else {
+          part[t % (LAG + 1)] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb[j], va[i % BUFS], f32x4{}, BC, AC, 0,
+                                                                                0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (t >= LAG) apply(t - LAG);
+        // B's column j is done with after its last row
+        if (t >= EDGE && (t - EDGE) % AHEAD == AHEAD - 1) vb[j] = read_b(smem + nx, j);
       }
 #pragma unroll
       for (int t = MF - LAG; t < MF; ++t) apply(t);
+      read_sa(smem + nx);
       read_sb(smem + nx);
       cur = nx;
     }

@@ -1,11 +1,11 @@
 // One translation unit of the 8-bit products: a tile and both operands' codes
-// (-DP8_TILE=<0|1> -DP8_AC=<0|1> -DP8_BC=<0|1>).
+// (-DP8_TILE=<0|1|2> -DP8_AC=<0|1> -DP8_BC=<0|1>).
 #include <atomic>
 
 #include "product8.hpp"
 
 #if !defined(P8_TILE) || !defined(P8_AC) || !defined(P8_BC)
-#error "compile with -DP8_TILE=<0|1> -DP8_AC=<0|1> -DP8_BC=<0|1>"
+#error "compile with -DP8_TILE=<0|1|2> -DP8_AC=<0|1> -DP8_BC=<0|1>"
 #endif
 
 #define P8_CAT(t, a, b) product8_##t##_##a##_##b
@@ -53,7 +53,7 @@ hipError_t P8_NAME(P8_TILE, P8_AC, P8_BC)(int dtype, bool exact, bool uni, const
     if (dtype != GT_BF16) return hipErrorInvalidValue;
     return uni ? by_epilogue<1, false, true>(a, s) : by_epilogue<1, false, false>(a, s);
   }
-#if P8_TILE == 1
+#if P8_TILE > 0
   if (dtype == GT_BF16 || a.p.e.epi == kEpiPart) return by_epilogue<1, true, false>(a, s);
   return by_epilogue<0, true, false>(a, s);
 #else

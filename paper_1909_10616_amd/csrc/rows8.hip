@@ -83,13 +83,12 @@ __global__ __launch_bounds__(64 * kWaves) void rows8_kernel(const Product8 q) {
   };
   f32x4 acc[H][RT] = {};
   const int64_t blocks = (a.K + kBlock - 1) / kBlock;
-  const int64_t first = blocks * blockIdx.z / a.splits, last = blocks * (blockIdx.z + 1) / a.splits;
   Step next;
-  int64_t b = first + wave;
-  if (b < last) load(next, b);
-  for (; b < last; b += kWaves) {
+  int64_t b = wave;
+  if (b < blocks) load(next, b);
+  for (; b < blocks; b += kWaves) {
     const Step s = next;
-    if (b + kWaves < last) load(next, b + kWaves);
+    if (b + kWaves < blocks) load(next, b + kWaves);
     f32x4 part[H][RT] = {};
 #pragma unroll
     for (int c = 0; c < 8; c += 2) {
@@ -126,10 +125,6 @@ __global__ __launch_bounds__(64 * kWaves) void rows8_kernel(const Product8 q) {
     v += lds[w][0][m][c ^ (m & 3)];
     if constexpr (G) u += lds[w][H - 1][m][c ^ (m & 3)];
   }
-  if (a.splits > 1) {
-    part_quad<G>(a, static_cast<int>(blockIdx.z), row, col, v, u);
-    return;
-  }
   const int left = a.N - col < 4 ? static_cast<int>(a.N - col) : 4;
   linear_quad<T>(a.e, a.N, row, col, 0, left, G, v, u, bias_quad<T>(a.e, col, 0, left),
                  G ? bias_quad<T>(a.e, col + a.N, 0, left) : f32x4{}, residual_quad<T>(a.e, row, col, left));
@@ -137,8 +132,7 @@ __global__ __launch_bounds__(64 * kWaves) void rows8_kernel(const Product8 q) {
 
 template <typename T, bool G, int XC, int WC>
 hipError_t by_rows(int rows, const Product8& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(a.p.tilesN), static_cast<unsigned>(a.p.tilesM),
-                  static_cast<unsigned>(a.p.splits));
+  const dim3 grid(static_cast<unsigned>(a.p.tilesN), static_cast<unsigned>(a.p.tilesM));
   if (rows == 16) rows8_kernel<T, G, XC, WC, 1><<<grid, 64 * kWaves, 0, s>>>(a);
   else if (rows == 32) rows8_kernel<T, G, XC, WC, 2><<<grid, 64 * kWaves, 0, s>>>(a);
   else if constexpr (!G) rows8_kernel<T, G, XC, WC, 4><<<grid, 64 * kWaves, 0, s>>>(a);
