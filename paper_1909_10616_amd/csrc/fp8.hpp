@@ -86,11 +86,30 @@ __device__ __forceinline__ float most8(const oct& v) {
   for (int i = 0; i < 4; ++i) m = fmaxf(m, fmaxf(fabsf(v.a[i]), fabsf(v.b[i])));
   return m;
 }
-// The maximum over rows of 16 lanes.
+// A value from N lanes further on, around a row of 16 lanes.
+template <int N>
+__device__ __forceinline__ float turned(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, false));
+}
+// The maximum over rows of 16 lanes (all active).
 __device__ __forceinline__ float max16(float m) {
-#pragma unroll
-  for (int d = 1; d < 16; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-  return m;
+  m = fmaxf(m, turned<8>(m));
+  m = fmaxf(m, turned<4>(m));
+  m = fmaxf(m, turned<2>(m));
+  return fmaxf(m, turned<1>(m));
+}
+// The sum over the wavefront, the same bits in every lane (all active).
+__device__ __forceinline__ float wave_sum(float s) {
+  s += turned<8>(s);
+  s += turned<4>(s);
+  s += turned<2>(s);
+  s += turned<1>(s);
+  const int v = __builtin_bit_cast(int, s);
+  const float a = __builtin_bit_cast(float, __builtin_amdgcn_readlane(v, 0));
+  const float b = __builtin_bit_cast(float, __builtin_amdgcn_readlane(v, 16));
+  const float c = __builtin_bit_cast(float, __builtin_amdgcn_readlane(v, 32));
+  const float d = __builtin_bit_cast(float, __builtin_amdgcn_readlane(v, 48));
+  return (a + b) + (c + d);
 }
 
 // The first n (≤ 0: none) of 8 values from p, zero beyond.

@@ -21,11 +21,6 @@ namespace {
 
 // ---- sums over a row's threads
 
-__device__ __forceinline__ float wave_sum(float s) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d);
-  return s;
-}
 // The sum over TH threads, the same in each; `box`: LDS that the exchange before did not use.
 template <int TH>
 __device__ __forceinline__ float row_sum(float s, float* box) {
@@ -202,23 +197,33 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_grad_kernel(const gt
   for (int v = 0; v < (SUMS ? NV : 1); ++v) dw[v] = db[v] = oct{};
   const float n = static_cast<float>(a.N);
   for (int it = 0; row < a.M; row += step, it ^= 1) {
-    oct h[NV], g[NV];
     const float mean = nmean, rstd = nrstd;
+    raw8<T> x[NV], y[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      x[v] = nx[v];
+      y[v] = ny[v];
+    }
+    // g and h of an octet
+    auto both = [&](int v, oct* g, oct* h) __attribute__((always_inline)) {
+      const oct xv = open8<T>(x[v]), yv = open8<T>(y[v]), wv = open_or<W>(wp, w[v], 1.0f);
+      *h = oct{(xv.a - mean) * rstd, (xv.b - mean) * rstd};
+      *g = oct{yv.a * wv.a, yv.b * wv.b};
+    };
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const oct x = open8<T>(nx[v]), y = open8<T>(ny[v]);
-      h[v] = oct{(x.a - mean) * rstd, (x.b - mean) * rstd};
+      oct g, h;
+      both(v, &g, &h);
       if constexpr (SUMS) {
-        dw[v].a += y.a * h[v].a;
-        dw[v].b += y.b * h[v].b;
-        db[v].a += y.a;
-        db[v].b += y.b;
+        const oct yv = open8<T>(y[v]);
+        dw[v].a += yv.a * h.a;
+        dw[v].b += yv.b * h.b;
+        db[v].a += yv.a;
+        db[v].b += yv.b;
       }
-      const oct wv = open_or<W>(wp, w[v], 1.0f);
-      g[v] = oct{y.a * wv.a, y.b * wv.b};
-      s1 += sum8(g[v]);
-      s2 += sum8(oct{g[v].a * h[v].a, g[v].b * h[v].b});
+      s1 += sum8(g);
+      s2 += sum8(oct{g.a * h.a, g.b * h.b});
     }
     load(row + step);
     if (!a.dX) continue;
@@ -247,7 +252,9 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_grad_kernel(const gt
     const float m1 = s1 / n, m2 = s2 / n;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      oct d{(g[v].a - m1 - h[v].a * m2) * rstd, (g[v].b - m1 - h[v].b * m2) * rstd};
+      oct g, h;
+      both(v, &g, &h);
+      oct d{(g.a - m1 - h.a * m2) * rstd, (g.b - m1 - h.b * m2) * rstd};
       if (a.R) {
         const oct q = open8<T>(r[v]);
         d.a += q.a;
@@ -394,9 +401,12 @@ Rows rows_of(int64_t N) {
     if (oct <= int64_t{r.threads} * r.octets) return r;
   return Rows{0, 0};
 }
+// As many workgroups as are resident at once, each with the parameters in its registers for all its
+// rows (16384×4096 in bf16: 5 a unit 48.8 µs, 4 49.1, 6 52.7; 2048×16384: 1 25.5, 2 28.7, 4 34.6).
 unsigned grid_of(int64_t M, const Rows& r) {
   const int each = r.threads == 64 ? 4 : 1;
-  return static_cast<unsigned>(std::min<int64_t>((M + each - 1) / each, kUnits * (r.threads == 512 ? 4 : 8)));
+  const int a_unit = r.threads == 512 ? (r.octets == 4 ? 1 : 2) : r.octets == 2 && r.threads == 256 ? 5 : 8;
+  return static_cast<unsigned>(std::min<int64_t>((M + each - 1) / each, kUnits * a_unit));
 }
 
 template <typename T, typename W, int CODE>
@@ -421,11 +431,16 @@ hipError_t norm_by_code(const gt_norm_args& a, hipStream_t s) {
   return a.code == GT_E4M3 ? norm_by<T, W, GT_E4M3>(a, s) : norm_by<T, W, GT_E5M2>(a, s);
 }
 
+// Each workgroup writes and the join reads 8·N bytes of sums (16384×4096 in bf16: 2 a unit 106 µs,
+// 3 110, 4 125).
 unsigned grad_grid(int64_t M, const Rows& r) {
   const int each = r.threads == 64 ? 4 : 1;
-  return static_cast<unsigned>(std::min<int64_t>((M + each - 1) / each, kUnits * (r.threads == 512 ? 2 : 4)));
+  return static_cast<unsigned>(std::min<int64_t>((M + each - 1) / each, kUnits * (r.threads >= 512 ? 1 : 2)));
 }
-unsigned long_parts(int64_t M) { return static_cast<unsigned>(std::min<int64_t>((M + 3) / 4, 64)); }
+// Rows too wide for the sums' registers beside their own: the sums by a kernel of their own, which
+// reads X and dY again (2048×16384 in bf16 78 µs, 124 with spilled sums in one).
+bool sums_apart(const Rows& r) { return r.threads == 0 || r.octets == 4; }
+unsigned apart_parts(int64_t M) { return static_cast<unsigned>(std::min<int64_t>((M + 3) / 4, 64)); }
 
 template <typename T, typename W, bool SUMS>
 hipError_t grad_by(const gt_norm_grad_args& a, float* part, hipStream_t s) {
@@ -435,27 +450,22 @@ hipError_t grad_by(const gt_norm_grad_args& a, float* part, hipStream_t s) {
   else if (r.threads == 64) norm_grad_kernel<T, W, 64, 2, SUMS><<<grid, 256, 0, s>>>(a, part);
   else if (r.threads == 256 && r.octets == 1) norm_grad_kernel<T, W, 256, 1, SUMS><<<grid, 256, 0, s>>>(a, part);
   else if (r.threads == 256) norm_grad_kernel<T, W, 256, 2, SUMS><<<grid, 256, 0, s>>>(a, part);
-  else if (r.octets == 2) norm_grad_kernel<T, W, 512, 2, SUMS><<<grid, 512, 0, s>>>(a, part);
-  else norm_grad_kernel<T, W, 512, 4, SUMS><<<grid, 512, 0, s>>>(a, part);
+  else if (r.threads == 512 && r.octets == 2) norm_grad_kernel<T, W, 512, 2, SUMS><<<grid, 512, 0, s>>>(a, part);
+  else if (r.threads == 512) norm_grad_kernel<T, W, 512, 4, false><<<grid, 512, 0, s>>>(a, part);
+  else norm_grad_long_kernel<T, W><<<static_cast<unsigned>(std::min<int64_t>(a.M, 4096)), 1024, 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <typename T, typename W>
 hipError_t grad(const gt_norm_grad_args& a, float* part, hipStream_t s) {
   hipError_t e = hipSuccess;
-  if (a.M > 0 && rows_of(a.N).threads == 0) {
-    if (part) {   // (before dX, which may be dY)
-      norm_sums_kernel<T><<<dim3(static_cast<unsigned>((a.N + 511) / 512), long_parts(a.M)), 256, 0, s>>>(a, part);
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
-    }
-    if (a.dX) {
-      norm_grad_long_kernel<T, W><<<static_cast<unsigned>(std::min<int64_t>(a.M, 4096)), 1024, 0, s>>>(a);
-      e = hipGetLastError();
-    }
-  } else if (a.M > 0 && (part || a.dX)) {
-    e = part ? grad_by<T, W, true>(a, part, s) : grad_by<T, W, false>(a, part, s);
+  const bool apart = sums_apart(rows_of(a.N));
+  if (a.M > 0 && part && apart) {   // (before dX, which may be dY)
+    norm_sums_kernel<T><<<dim3(static_cast<unsigned>((a.N + 511) / 512), apart_parts(a.M)), 256, 0, s>>>(a, part);
+    e = hipGetLastError();
   }
+  if (e == hipSuccess && a.M > 0 && (a.dX || (part && !apart)))
+    e = part && !apart ? grad_by<T, W, true>(a, part, s) : grad_by<T, W, false>(a, part, s);
   if (e != hipSuccess || (!a.dw && !a.db)) return e;
   const unsigned columns = static_cast<unsigned>(std::min<int64_t>((a.N + 63) / 64, int64_t{1} << 20));
   norm_join_kernel<<<dim3(columns, 2), 1024, 0, s>>>(part, norm_parts(a), a.N, a.dw, a.db);
@@ -472,7 +482,7 @@ hipError_t launch_norm(const gt_norm_args& a, hipStream_t s) {
 int64_t norm_parts(const gt_norm_grad_args& a) {
   if (a.M == 0 || (!a.dw && !a.db)) return 0;
   const Rows r = rows_of(a.N);
-  return r.threads == 0 ? long_parts(a.M) : grad_grid(a.M, r);
+  return sums_apart(r) ? apart_parts(a.M) : grad_grid(a.M, r);
 }
 
 hipError_t launch_norm_grad(const gt_norm_grad_args& a, float* part, hipStream_t s) {

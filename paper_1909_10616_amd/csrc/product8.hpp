@@ -200,7 +200,7 @@ __global__ __launch_bounds__(64 * tile8(TILE).NWM * tile8(TILE).NWN, 2) void pro
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{};
-  constexpr int LAG = 2;   // instructions between a sum and its scaling
+  constexpr int LAG = UNI ? 4 : 2;   // instructions between a sum and its scaling, as registers allow
   f32x4 part[LAG + 1];
   // step t of a stage: the last AHEAD i's are taken together, column by column
   auto row_of = [&](int t) { return t < MF - AHEAD * TN ? t / TN : TM - AHEAD + t % AHEAD; };

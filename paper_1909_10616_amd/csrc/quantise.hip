@@ -2,7 +2,8 @@
 //
 // A workgroup takes a square of 128×128 values, 256 threads an 8×8 of them each, read
 // once: rows' scales are maxima over 16 lanes, columns' and the square's meet in LDS. A
-// thread's 8 codes of a row, or of a column for the transpose, are 8 bytes.
+// thread's 8 codes of a row are 8 bytes; those of a column go through LDS, so that the
+// transpose is written 128 bytes of a row at a time.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -19,6 +20,7 @@ template <typename T, int CODE, bool SQUARE, bool Q, bool QT>
 __global__ __launch_bounds__(256) void quantise_kernel(const gt_quantise_args a, int64_t tilesN,
                                                        int64_t tiles) {
   __shared__ float most[4][16][8];
+  __shared__ uint2 turn[QT ? kBlock : 1][16];   // [column][octet of rows ^ 2·(column / 8)]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;
   const bool pow2 = a.pow2 != 0;
@@ -63,6 +65,13 @@ __global__ __launch_bounds__(256) void quantise_kernel(const gt_quantise_args a,
     }
     if constexpr (QT) {
       float col[8];
+      if constexpr (sizeof(T) == 2) {   // (widened anew: the 32 registers they lie in are half as many)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          asm volatile("" : "+v"(raw[i].w[0]));
+          v[i] = open8<T>(raw[i]);
+        }
+      }
       if constexpr (!SQUARE) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -84,10 +93,8 @@ __global__ __launch_bounds__(256) void quantise_kernel(const gt_quantise_args a,
           col[j] = block_scale<CODE>(col[j], pow2);
         }
       }
-      uint8_t* q = static_cast<uint8_t*>(a.Qt) + n0 * a.ldqt + m0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (n0 + j >= a.N) continue;
         const float s = SQUARE ? square : col[j];
         oct w;
 #pragma unroll
@@ -95,9 +102,26 @@ __global__ __launch_bounds__(256) void quantise_kernel(const gt_quantise_args a,
           w.a[i] = j < 4 ? v[i].a[j & 3] : v[i].b[j & 3];
           w.b[i] = j < 4 ? v[i + 4].a[j & 3] : v[i + 4].b[j & 3];
         }
-        store_codes(q + j * a.ldqt, code8<CODE>(w, 1.0f / s), a.M - m0);
-        if (!SQUARE && rg == 0) a.St[(n0 + j) * a.ldst + tm] = s;
+        turn[cg * 8 + j][rg ^ (cg * 2 & 14)] = code8<CODE>(w, 1.0f / s);
+        if (!SQUARE && rg == 0 && n0 + j < a.N) a.St[(n0 + j) * a.ldst + tm] = s;
       }
+      __syncthreads();
+      const int64_t c0 = tn * kBlock, r0 = tm * kBlock + (threadIdx.x & 7) * 16;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = i * 32 + (threadIdx.x >> 3), at = (threadIdx.x & 7) * 2 ^ (c / 8 * 2 & 14);
+        if (c0 + c >= a.N) continue;
+        uint8_t* q = static_cast<uint8_t*>(a.Qt) + (c0 + c) * a.ldqt + r0;
+        const uint2 lo = turn[c][at], hi = turn[c][at + 1];
+        if (r0 + 16 <= a.M) {
+          const u32x4 w{lo.x, lo.y, hi.x, hi.y};
+          __builtin_memcpy(q, &w, 16);
+        } else {
+          store_codes(q, lo, a.M - r0);
+          store_codes(q + 8, hi, a.M - r0 - 8);
+        }
+      }
+      __syncthreads();
     }
   }
 }
