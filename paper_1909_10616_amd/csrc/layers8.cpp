@@ -230,7 +230,7 @@ void choose(Linear8* l) {
     if (tm * tn * 64 * s.NWM * s.NWN >= kMaxItems) continue;
     for (int z = 1; z <= 16 && (z == 1 || 2 * z <= all); z *= 2) {
       const double stages = static_cast<double>((all + z - 1) / z);
-      const double join = z > 1 ? 4.5 + 2.0 * z * a.M * wide * 4 / 6.0e6 : 0.0;
+      const double join = z > 1 ? 7.0 + 2.0 * z * a.M * wide * 4 / 6.0e6 : 0.0;
       offer(Form{0, t, z, copy + std::hypot(tiles_cost(kCost8[l->exact][t], tm * tn * z, stages), memory) + join, tm, tn});
     }
   }

@@ -52,9 +52,9 @@ __global__ __launch_bounds__(64 * kWaves) void rows8_kernel(const Product8 q) {
     i32x8 x[RT], w[H];
     float sx[RT], sw[H][4];
   };
-  auto codes = [&](const uint8_t* p, int64_t k) __attribute__((always_inline)) {
+  auto codes = [&](const uint8_t* p, int64_t k, bool whole) __attribute__((always_inline)) {
     i32x8 v;
-    if (k + kBlock <= a.K) {
+    if (whole) {
       __builtin_memcpy(&v, p + k, 32);
     } else {   // the last block, where it ends inside
       const u32x4 lo = load_chunk<uint8_t, 16>(p + k, a.K - k - 32 * grp);
@@ -67,28 +67,22 @@ __global__ __launch_bounds__(64 * kWaves) void rows8_kernel(const Product8 q) {
     }
     return v;
   };
-  auto load = [&](Step& s, int64_t b) __attribute__((always_inline)) {
+  auto load = [&](Step& s, int64_t b, bool whole) __attribute__((always_inline)) {
     const int64_t k = b * kBlock;
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-      s.w[h] = codes(W[h], k);
+      s.w[h] = codes(W[h], k, whole);
 #pragma unroll
       for (int r = 0; r < 4; ++r) s.sw[h][r] = sw[h][r][b];
     }
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
-      s.x[i] = codes(X[i], k);
+      s.x[i] = codes(X[i], k, whole);
       s.sx[i] = sx[i][b];
     }
   };
   f32x4 acc[H][RT] = {};
-  const int64_t blocks = (a.K + kBlock - 1) / kBlock;
-  Step next;
-  int64_t b = wave;
-  if (b < blocks) load(next, b);
-  for (; b < blocks; b += kWaves) {
-    const Step s = next;
-    if (b + kWaves < blocks) load(next, b + kWaves);
+  auto multiply = [&](const Step& s) __attribute__((always_inline)) {
     f32x4 part[H][RT] = {};
 #pragma unroll
     for (int c = 0; c < 8; c += 2) {
@@ -109,6 +103,32 @@ __global__ __launch_bounds__(64 * kWaves) void rows8_kernel(const Product8 q) {
       for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[h][i][r] = fmaf(part[h][i][r], s.sx[i] * s.sw[h][r], acc[h][i][r]);
+  };
+  // A wavefront's next block is on its way while it multiplies one. The blocks that are whole in a
+  // loop of their own, two by two, so that no step is copied and no load checked (1×11008×4096 15.6
+  // → 12.3 µs); gated, whose registers then leave one workgroup a unit, not (22.2 µs, 26.0 so).
+  const int64_t whole = a.K / kBlock, blocks = (a.K + kBlock - 1) / kBlock;
+  if constexpr (G) {
+    Step next;
+    if (wave < blocks) load(next, wave, wave < whole);
+    for (int64_t b = wave; b < blocks; b += kWaves) {
+      const Step s = next;
+      if (b + kWaves < blocks) load(next, b + kWaves, b + kWaves < whole);
+      multiply(s);
+    }
+  } else {
+    Step step[2];
+    if (wave < whole) load(step[0], wave, true);
+    for (int64_t b = wave; b < whole; b += 2 * kWaves) {
+      if (b + kWaves < whole) load(step[1], b + kWaves, true);
+      multiply(step[0]);
+      if (b + 2 * kWaves < whole) load(step[0], b + 2 * kWaves, true);
+      if (b + kWaves < whole) multiply(step[1]);
+    }
+    if (whole < blocks && wave == whole % kWaves) {
+      load(step[0], whole, false);
+      multiply(step[0]);
+    }
   }
   // a lane's sums: row 16·i + lx, columns 4·grp …
 #pragma unroll

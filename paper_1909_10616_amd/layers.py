@@ -131,7 +131,7 @@ class NormGrads(typing.NamedTuple):
 
 
 _lib = None
-_calls = {}   # entry point → its function and its scratch query
+_calls = {}   # entry point → its function and its scratch query (None: no scratch)
 
 
 def lib():
@@ -144,6 +144,7 @@ def lib():
             f.restype = ctypes.c_int
             if name in NO_SCRATCH:
                 f.argtypes = [ctypes.POINTER(args), _P]
+                _calls[name] = f, None
                 continue
             f.argtypes = [ctypes.POINTER(args), _P, _i64, _P]
             w = getattr(L, name + "_workspace")
@@ -224,49 +225,47 @@ def _gpu(t, name, dims):
 def _call(name, a, like, workspace, stream):
     """Runs an entry point on like's device, with scratch of its own unless given."""
     import torch
-    L = lib()
+    if _lib is None:
+        lib()
+    if like.device.index == torch._C._cuda_getDevice():
+        _launch(name, a, like, workspace, stream)
+        return
+    with torch.cuda.device(like.device):
+        _launch(name, a, like, workspace, stream)
+
+
+def _launch(name, a, like, workspace, stream):
+    run, query = _calls[name]
     ref = ctypes.byref(a)
-    with torch.cuda.device(like.device) if like.device.index != torch._C._cuda_getDevice() \
-            else _NOTHING:
-        if name in NO_SCRATCH:
-            _check(getattr(L, name)(ref, _stream(stream)), name)
-            return
-        run, query = _calls[name]
-        need = _i64()
-        _check(query(ref, ctypes.byref(need)), name)
-        n = need.value
-        if n == 0:
-            _check(run(ref, None, 0, _stream(stream)), name)
-            return
-        if workspace is None:
-            workspace = _empty((n,), torch.uint8, like.device, stream)
-        elif workspace.device != like.device or not workspace.is_contiguous():
-            raise ValueError("workspace must be contiguous, on the operands' device")
-        _check(run(ref, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                   _stream(stream)), name)
+    if query is None:
+        _check(run(ref, _stream(stream)), name)
+        return
+    need = _i64()
+    _check(query(ref, ctypes.byref(need)), name)
+    n = need.value
+    if n == 0:
+        _check(run(ref, None, 0, _stream(stream)), name)
+        return
+    if workspace is None:
+        import torch
+        workspace = _empty((n,), torch.uint8, like.device, stream)
+    elif workspace.device != like.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous, on the operands' device")
+    _check(run(ref, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)), name)
 
 
-class _Nothing:
-    def __enter__(self):
-        return self
-
-    def __exit__(self, *exc):
-        return False
-
-
-_NOTHING = _Nothing()
-
-
-def _empty(shape, dtype, device, stream):
+def _empty(shape, dtype, device, stream, ld=None):
     """Memory for the stream the call runs on (PyTorch's allocator gives memory that is
-    free in the order of one stream)."""
+    free in the order of one stream); ld: elements between rows."""
     import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        if ld is None or ld == shape[1]:
+            return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty_strided(shape, (ld, 1), dtype=dtype, device=device)
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _empty(shape, dtype, device, None, ld)
 
 
 def workspace_bytes(name, args) -> int:
@@ -506,19 +505,14 @@ def _new_codes(rows, cols, code, block, device, stream):
     """Codes to be filled: rows of whole 16-byte chunks, which the products read fastest."""
     import torch
     dtype = torch.float8_e4m3fn if code == CODES["e4m3"] else torch.float8_e5m2
-    wide = (cols + 15) // 16 * 16
-    q = _empty((rows, wide), dtype, device, stream)
-    return Codes(q if wide == cols else q[:, :cols],
+    return Codes(_empty((rows, cols), dtype, device, stream, (cols + 15) // 16 * 16),
                  _empty((rows if block == 1 else _blocks(rows), _blocks(cols)), torch.float32, device, stream))
 
 
 def _codes(c, name, like, shape):
     """A matrix of codes: its type, the rows that share a scale, both pointers and row strides."""
     import torch
-    try:
-        values, scales = c
-    except (TypeError, ValueError):
-        raise ValueError(f"{name} must be Codes: values and their scales") from None
+    values, scales = c
     code = _code_of(values, name)
     q, ldq = _tensor(values, name, like, shape, values.dtype)
     rows, cols = shape
@@ -569,9 +563,12 @@ def gt_linear_fp8(X, W, bias=None, residual=None, act="none", gated=False, Y=Non
     gt_linear_fp8(transposed codes of dY, transposed codes of X)."""
     import torch
     try:
-        like, (wide, K) = X[0], W[0].shape
-    except (TypeError, ValueError, IndexError, AttributeError):
-        raise ValueError("X and W must be Codes of matrices") from None
+        (like, _), (values, _) = X, W
+        wide, K = values.shape
+    except (TypeError, ValueError, AttributeError):
+        like = X = None
+    if X is None or isinstance(X, torch.Tensor) or isinstance(W, torch.Tensor):
+        raise ValueError("X and W must be Codes of matrices: values and their scales")
     _gpu(like, "X", 2)
     M = like.shape[0]
     N = wide // 2 if gated else wide
@@ -594,7 +591,7 @@ def gt_linear_fp8(X, W, bias=None, residual=None, act="none", gated=False, Y=Non
     return Y
 
 
-def _norm(X, weight, bias, eps, Y, mean, rstd, codes, code, pow2, stream):
+def _norm(X, weight, bias, eps, y, ldy, mean, rstd, codes, code, pow2, stream):
     import torch
     M, N = X.shape
     dt = _type(X, "X")
@@ -606,7 +603,6 @@ def _norm(X, weight, bias, eps, Y, mean, rstd, codes, code, pow2, stream):
     wt = _result_type(typed, "weight" if typed is weight else "bias", X)
     w = _one(weight, "weight", X, (N,), typed.dtype)
     b = _one(bias, "bias", X, (N,), typed.dtype)
-    y, ldy = _pair(Y, "Y", X, (M, N))
     _call("gt_norm",
           gt_norm_args(M, N, dt, wt, code, int(bool(pow2)), eps, 0, x, ldx, w, b, y, ldy,
                        _one(mean, "mean", X, (M,), torch.float32), _one(rstd, "rstd", X, (M,), torch.float32),
@@ -620,7 +616,10 @@ def gt_norm(X, weight=None, bias=None, eps=1e-5, Y=None, mean=None, rstd=None, s
     _gpu(X, "X", 2)
     if Y is None:
         Y = _empty(X.shape, X.dtype, X.device, stream)
-    _norm(X, weight, bias, eps, Y, mean, rstd, None, 0, False, stream)
+        y, ldy = Y.data_ptr(), X.shape[1]
+    else:
+        y, ldy = _tensor(Y, "Y", X, X.shape)
+    _norm(X, weight, bias, eps, y, ldy, mean, rstd, None, 0, False, stream)
     return Y
 
 
@@ -631,8 +630,9 @@ def gt_norm_fp8(X, weight=None, bias=None, eps=1e-5, code="e4m3", pow2=False, Y=
     receives the values as well."""
     _gpu(X, "X", 2)
     c = _code(code)
+    y, ldy = _pair(Y, "Y", X, X.shape)
     codes = _new_codes(*X.shape, c, 1, X.device, stream)
-    _norm(X, weight, bias, eps, Y, mean, rstd, codes, c, pow2, stream)
+    _norm(X, weight, bias, eps, y, ldy, mean, rstd, codes, c, pow2, stream)
     return codes
 
 
