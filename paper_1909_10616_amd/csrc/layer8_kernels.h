@@ -43,7 +43,8 @@ constexpr unsigned kStage8(int tile) { return (tile8(tile).BM + tile8(tile).BN) 
 // either half of a wavefront's columns share their scales.
 hipError_t launch_product8(int dtype, int tile, bool exact, bool uni, const Product8& a, hipStream_t s);
 
-// Few rows, straight from memory: `rows` (16, 32 or 64) a workgroup.
-hipError_t launch_rows8(int dtype, int rows, const Product8& a, hipStream_t s);
+// Few rows: `rows` (16, 32 or 64) a workgroup; staged: both operands at 16-byte aligned rows that
+// 32-bit offsets reach.
+hipError_t launch_rows8(int dtype, int rows, bool staged, const Product8& a, hipStream_t s);
 
 }  // namespace gt

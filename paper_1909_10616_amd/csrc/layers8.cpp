@@ -163,7 +163,8 @@ int linear8_checks(const gt_linear_fp8_args* a, bool pointers) {
 
 struct Linear8 {
   Product8 q{};
-  int rows = 0;   // > 0: the kernel of a few rows, so many a workgroup
+  int rows = 0;   // > 0: the kernels of a few rows, so many a workgroup
+  bool staged = false;   // … through LDS
   int tile = 0;
   bool exact = false, uni = false;
   PadJobs pad{};                     // operands copied to aligned rows first …
@@ -180,17 +181,16 @@ struct Form {
 };
 
 // What a stage (128 k) of a tile takes, in µs, where few tiles run (alone) and where they fill the
-// chip (full), the launch and epilogue of such rounds, and how many tiles fill it. Fitted to the
-// 100 shapes of profiles/layers8_forms.md, from 1×1024×1024 to 4096×11008×4096, each in
-// every form (bf16, K = 4096: 256×256 tiles 53 µs for 16 of them, 73 for 256; 128×128 29 for 32,
-// 45 for 512; 64×64 25 for 64, 34 for 1024): the choice is within 2 % of the best form on average.
+// chip (full), the launch and epilogue of such rounds, and how many tiles fill it. Fitted to
+// 100 shapes from 1×1024×1024 to 4096×11008×4096, each in every form (bf16, K = 4096: 256×256 tiles 53 µs for 16 of them, 73 for 256; 128×128 29 for 32,
+// 45 for 512; 64×64 25 for 64, 34 for 1024): 94 choices are within 5 % of the best form.
 struct Cost8 {
   double alone, full, fixed, fixed_full;
   int64_t fill;
 };
 constexpr Cost8 kCost8[2][kTiles8] = {
     {{1.45, 1.95, 8.0, 10.0, 256}, {0.78, 1.15, 4.6, 8.0, 512}, {0.68, 0.86, 2.9, 6.3, 1024}},
-    {{0, 0, 0, 0, 0}, {1.21, 2.0, 5.2, 11.0, 512}, {1.05, 1.3, 3.0, 9.0, 1024}}};   // exact
+    {{0, 0, 0, 0, 0}, {1.21, 2.0, 5.2, 11.0, 512}, {1.1, 1.3, 3.0, 9.0, 1024}}};   // exact
 double tiles_cost(const Cost8& c, int64_t tiles, double stages) {
   const int64_t rounds = tiles / c.fill, rest = tiles % c.fill;
   double t = 0.0;
@@ -202,10 +202,13 @@ double tiles_cost(const Cost8& c, int64_t tiles, double stages) {
   }
   return t;
 }
-// The same of the kernel of a few rows: a block of a wavefront, for each round of 256 workgroups.
-double rows_cost(int rows, bool gated, int64_t groups, int64_t steps) {
-  const double each = rows == 16 ? (gated ? 1.85 : 1.28) : rows == 32 ? (gated ? 3.0 : 1.9) : 3.43;
-  return 3.0 + each * static_cast<double>(steps) * std::max(1.0, static_cast<double>(groups) / kUnits);
+// The same of the kernels of a few rows: a wavefront's block of 128 k for each round of 256 workgroups,
+// and W's way from memory. (few: through LDS, or X a few rows that all lanes share.)
+double rows_cost(int rows, bool gated, bool few, int64_t groups, int64_t steps, double memory) {
+  // [few][gated][rows / 32]
+  constexpr double kEach[2][2][3] = {{{1.28, 2.1, 3.43}, {1.85, 3.0, 0.0}}, {{0.85, 1.25, 1.7}, {1.41, 2.0, 0.0}}};
+  const double each = kEach[few][gated][rows / 32];
+  return 3.0 + std::hypot(each * static_cast<double>(steps) * std::max(1.0, static_cast<double>(groups) / kUnits), memory);
 }
 
 // The form by the time it should take: the tiles' rounds or the operands' way from memory, which
@@ -220,6 +223,8 @@ void choose(Linear8* l) {
   const double copied = static_cast<double>((ok_a ? 0 : a.M * ldd) + (ok_b ? 0 : wide * ldd));
   const double copy = copied > 0 ? 5.0 + 2.0 * copied / 5.0e6 : 0.0;
   const double memory = static_cast<double>(a.M * a.K + wide * a.K) / 5.2e6;
+  // (a row or four take no more from memory directly: 1×11008×4096 gated 22.2 µs, 24.4 through LDS)
+  const bool staged = a.M > 4 && ok_a && ok_b && 64 * std::max(a.lda, a.ldb) < kMaxExtent;
   Form best{0, 0, 1, 0.0, 0, 0};
   auto offer = [&](const Form& f) {
     if (best.cost == 0.0 || f.cost < best.cost) best = f;
@@ -230,17 +235,20 @@ void choose(Linear8* l) {
     if (tm * tn * 64 * s.NWM * s.NWN >= kMaxItems) continue;
     for (int z = 1; z <= 16 && (z == 1 || 2 * z <= all); z *= 2) {
       const double stages = static_cast<double>((all + z - 1) / z);
-      const double join = z > 1 ? 7.0 + 2.0 * z * a.M * wide * 4 / 6.0e6 : 0.0;
-      offer(Form{0, t, z, copy + std::hypot(tiles_cost(kCost8[l->exact][t], tm * tn * z, stages), memory) + join, tm, tn});
+      double cost = copy + std::hypot(tiles_cost(kCost8[l->exact][t], tm * tn * z, stages), memory);
+      // (two launches and the scratch are 18 µs of the host's)
+      if (z > 1) cost = std::max(18.0, cost + 4.5 + 2.0 * z * a.M * wide * 4 / 6.0e6);
+      offer(Form{0, t, z, cost, tm, tn});
     }
   }
   for (const int r : {16, 32, 64}) {
     if (r == 64 && gated) continue;
     const int64_t tm = (a.M + r - 1) / r, tn = (a.N + 15) / 16;
     if (tm >= 65536 || tn * 512 >= kMaxItems) continue;
-    offer(Form{r, 0, 1, rows_cost(r, gated, tm * tn, (all + 7) / 8), tm, tn});
+    offer(Form{r, 0, 1, rows_cost(r, gated, staged || a.M <= 4, tm * tn, (all + 7) / 8, memory), tm, tn});
   }
   l->rows = best.rows;
+  l->staged = staged;
   l->tile = best.tile;
   /*FORCE*/
   a.splits = best.cost > 0.0 ? best.splits : 0;   // (0: no form serves)
@@ -327,7 +335,7 @@ int linear_fp8_impl(const gt_linear_fp8_args* a, void* ws, int64_t ws_bytes, voi
     p.e.part = reinterpret_cast<float*>(at);
     p.e.epi = kEpiPart;
   }
-  GT_TRY(l.rows > 0 ? launch_rows8(a->dtype, l.rows, l.q, s)
+  GT_TRY(l.rows > 0 ? launch_rows8(a->dtype, l.rows, l.staged, l.q, s)
                     : launch_product8(a->dtype, l.tile, l.exact, l.uni, l.q, s),
          "8-bit product");
   p.e.epi = epi;

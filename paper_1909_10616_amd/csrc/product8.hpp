@@ -13,6 +13,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 #include "fp8.hpp"
@@ -20,6 +21,18 @@
 #include "product.hpp"
 
 namespace gt {
+
+// Raises a kernel's dynamic LDS limit, once per kernel and device (attr: where it has been).
+inline hipError_t raise_lds(const void* fn, size_t lds, std::atomic<uint64_t>& attr) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t{1} << dev : 0;
+  if (bit && (attr.load(std::memory_order_acquire) & bit)) return hipSuccess;
+  e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+  if (e == hipSuccess) attr.fetch_or(bit, std::memory_order_release);
+  return e;
+}
 
 // 64 lanes × 4 bytes, lane j's from its address to LDS byte lds_base + 4·j.
 __device__ __forceinline__ void dma_scale(const float* p, uint32_t lds_base) {

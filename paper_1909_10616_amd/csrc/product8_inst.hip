@@ -1,7 +1,5 @@
 // One translation unit of the 8-bit products: a tile and both operands' codes
 // (-DP8_TILE=<0|1|2> -DP8_AC=<0|1> -DP8_BC=<0|1>).
-#include <atomic>
-
 #include "product8.hpp"
 
 #if !defined(P8_TILE) || !defined(P8_AC) || !defined(P8_BC)
@@ -18,19 +16,10 @@ template <int DT, bool EXACT, int EPI, bool UNI>
 hipError_t go(const Product8& a, hipStream_t s) {
   constexpr auto* fn = product8_kernel<DT, EXACT, P8_AC, P8_BC, P8_TILE, EPI, UNI>;
   constexpr Tile8 t = tile8(P8_TILE);
-  // the dynamic LDS limit is raised once per kernel and device
   static std::atomic<uint64_t> attr{0};
   constexpr size_t lds = 2 * kStage8(P8_TILE);
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
+  const hipError_t e = raise_lds(reinterpret_cast<const void*>(fn), lds, attr);
   if (e != hipSuccess) return e;
-  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t{1} << dev : 0;
-  if (!bit || !(attr.load(std::memory_order_acquire) & bit)) {
-    e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
-                            static_cast<int>(lds));
-    if (e != hipSuccess) return e;
-    attr.fetch_or(bit, std::memory_order_release);
-  }
   const dim3 grid(static_cast<unsigned>(a.p.tilesM) * static_cast<unsigned>(a.p.tilesN),
                   static_cast<unsigned>(a.p.splits));
   hipLaunchKernelGGL(fn, grid, dim3(64 * t.NWM * t.NWN), lds, s, a);

@@ -18,7 +18,7 @@ from test_layers_code_object import M0_READERS, _kernels, _scalars, _split
 
 def _units():
     from paper_1909_10616_amd import build
-    return [u[0] for u in build._units() if u[1] == "product8_inst.hip"]
+    return [u[0] for u in build._units() if u[1] in ("product8_inst.hip", "rows8.hip")]
 
 
 @pytest.fixture(scope="module")
@@ -36,8 +36,8 @@ READERS = re.compile(M0_READERS.pattern.replace("|global_load_lds", ""))
 
 @pytest.mark.parametrize("unit", _units())
 def test_loads_into_lds_are_sound(objects, unit, tmp_path):
-    kernels = {k: v for k, v in _kernels(objects[unit], tmp_path).items() if "product8_kernel" in k}
-    assert len(kernels) == (6 if unit.startswith("product8_0") else 11)
+    kernels = {k: v for k, v in _kernels(objects[unit], tmp_path).items() if "product8_kernel" in k or "staged8" in k}
+    assert len(kernels) == (40 if unit == "rows8" else 6 if unit.startswith("product8_0") else 11)
     for fn, (ins, targets) in kernels.items():
         loads = [i for i, x in enumerate(ins) if re.search(r"\blds\b", x) or "load_lds" in x]
         assert sum("global_load_lds" in ins[i] for i in loads) >= 2 and len(loads) > 8
@@ -65,6 +65,8 @@ def test_loads_into_lds_are_sound(objects, unit, tmp_path):
             if at not in inside:
                 assert not re.search(r"\bm0\b", i) and not READERS.match(i), f"{unit} {fn}: {i}"
         assert not [i for i in ins if i.startswith("scratch_")], f"{unit} {fn}"
+        if unit == "rows8":
+            continue
         exact = "ILi1ELb1E" in fn or "ILi0ELb1E" in fn
         stage = {"0": 32, "1": 16, "2": 8}[unit[9]] * (4 if exact else 1)
         assert sum("mfma" in i for i in ins) == stage, f"{unit} {fn}"
