@@ -272,7 +272,9 @@ int gt_quantise(const gt_quantise_args* a, void* stream);
 /* Y = act(X·Wᵀ + bias) + R of codes: X M×K, W N×K (gated: 2N×K, the gate's rows, then the
  * up's), K along the rows of both, so that blocks of 128 lie along the sum:
  *   (X·Wᵀ)[m][n] = Σ_b sx[m][b]·sw[n][b]·Σ_{k in block b} X[m][k]·W[n][k].
- * A block's sum and the sum over blocks are fp32. The gradients are the same product of
+ * The sum over blocks is fp32, and so is a block's where Y is fp32. Where Y is bf16, a block's sum
+ * is the 8-bit matrix instructions': of up to 8 products that they add at once they drop what lies
+ * more than about 2^13 below the largest. The gradients are the same product of
  * other codes: dX = dY·W takes codes of dY and of W's transpose, dW = dYᵀ·X codes of both
  * transposes. bias: N (2N) or NULL, R: M×N or NULL, both in dtype; Y in dtype or fp32, and it may be R
  * (dW += …). Rows of X and W at 16-byte aligned addresses are the fast case. */

@@ -60,7 +60,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // 8 codes as bf16, which holds every one of them exactly. The matrix instructions that take
 // codes keep some 13 bits below the largest of the products they add at once (a 1 beside
-// 2^13 and −2^13 vanishes), 1.7e-5 of a product's norm; of bf16 operands they keep all that fp32
+// 2^14 and −2^14 vanishes), 1.7e-5 of a product's norm; of bf16 operands they keep all that fp32
 // holds.
 template <int CODE>
 __device__ __forceinline__ bf16x8 widen8(int lo, int hi) {

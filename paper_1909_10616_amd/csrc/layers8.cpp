@@ -182,8 +182,9 @@ struct Form {
 
 // What a stage (128 k) of a tile takes, in µs, where few tiles run (alone) and where they fill the
 // chip (full), the launch and epilogue of such rounds, and how many tiles fill it. Fitted to
-// 100 shapes from 1×1024×1024 to 4096×11008×4096, each in every form (bf16, K = 4096: 256×256 tiles 53 µs for 16 of them, 73 for 256; 128×128 29 for 32,
-// 45 for 512; 64×64 25 for 64, 34 for 1024): 94 choices are within 5 % of the best form.
+// 100 shapes from 1×1024×1024 to 4096×11008×4096, each in every form (bf16, K = 4096: 256×256
+// tiles 53 µs for 16 of them, 73 for 256; 128×128 29 for 32, 45 for 512; 64×64 25 for 64, 34
+// for 1024): 93 choices are within 5 % of the best form, 98 within 10 %.
 struct Cost8 {
   double alone, full, fixed, fixed_full;
   int64_t fill;
@@ -250,7 +251,6 @@ void choose(Linear8* l) {
   l->rows = best.rows;
   l->staged = staged;
   l->tile = best.tile;
-  /*FORCE*/
   a.splits = best.cost > 0.0 ? best.splits : 0;   // (0: no form serves)
   a.tilesM = static_cast<int>(best.tm);
   a.tilesN = static_cast<int>(best.tn);

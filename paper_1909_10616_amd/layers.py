@@ -566,8 +566,8 @@ def gt_linear_fp8(X, W, bias=None, residual=None, act="none", gated=False, Y=Non
         (like, _), (values, _) = X, W
         wide, K = values.shape
     except (TypeError, ValueError, AttributeError):
-        like = X = None
-    if X is None or isinstance(X, torch.Tensor) or isinstance(W, torch.Tensor):
+        like = None
+    if not isinstance(like, torch.Tensor) or isinstance(X, torch.Tensor) or isinstance(W, torch.Tensor):
         raise ValueError("X and W must be Codes of matrices: values and their scales")
     _gpu(like, "X", 2)
     M = like.shape[0]

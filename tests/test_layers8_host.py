@@ -194,6 +194,7 @@ def test_cpu_tensors_are_refused(L):
 
 def test_codes_are_asked_for(L):
     X = torch.zeros(4, 128)
-    for x, w in ((X, X), (None, None), (L.Codes(X, X), 3), (3, L.Codes(X, X)), ((), ())):
+    for x, w in ((X, X), (None, None), (L.Codes(X, X), 3), (3, L.Codes(X, X)), ((), ()), ((3, 4), L.Codes(X, X)),
+                 (L.Codes(X, X), X)):
         with pytest.raises(ValueError):
             L.gt_linear_fp8(x, w)
