@@ -4,7 +4,8 @@
 // mean costs no digits, then the outputs: each row is read once and written once.
 // Backward: both means of a row in one exchange; every thread keeps the column sums of dw
 // and db for its own columns over all rows that its workgroup takes, and a second launch
-// adds the workgroups' sums in their order.
+// adds the workgroups' sums in their order. Up to 1024 rows other workgroups of the same
+// launch take the columns' sums.
 // Bound by memory: 16384×4096 in bf16 with mean and rstd 49 µs, 5.5 TB/s; its gradients with
 // R 104 µs, 5.2 TB/s. One row of 4096 in bf16 is latency, 2.7 µs on the GPU.
 // Thread t of a row has the octets t, t + TH, …, so that 16 neighbours hold 128 columns, a
@@ -164,16 +165,16 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const gt_norm_args a) {
 
 // ---- backward
 
-// dw and db of a thread's columns, from its workgroup's rows, to the workgroup's partial row.
+// Workgroup `block` of `blocks` (TH, at least 256 threads). dw and db of a thread's columns, from
+// its workgroup's rows, to the workgroup's partial row.
 template <typename T, typename W, int TH, int NV, bool SUMS>
-__global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_grad_kernel(const gt_norm_grad_args a,
-                                                                        float* part) {
+__device__ __forceinline__ void grad_rows(const gt_norm_grad_args& a, float* part, int block, int blocks) {
   constexpr int RB = TH < 256 ? 256 / TH : 1;
   __shared__ float box[2][2][16];
   __shared__ f32x4 join[SUMS && RB > 1 ? RB : 1][SUMS && RB > 1 ? 2 * TH : 1];
   const int t = threadIdx.x % TH, rb = threadIdx.x / TH;
   const W* wp = static_cast<const W*>(a.w);
-  const int64_t step = int64_t{gridDim.x} * RB;
+  const int64_t step = static_cast<int64_t>(blocks) * RB;
   auto col = [&](int v) { return (static_cast<int64_t>(v) * TH + t) * 8; };
   raw8<W> w[NV];
   raw8<T> nx[NV], ny[NV];
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_grad_kernel(const gt
     nmean = row < a.M ? a.mean[row] : 0.0f;
     nrstd = row < a.M ? a.rstd[row] : 0.0f;
   };
-  int64_t row = int64_t{blockIdx.x} * RB + rb;
+  int64_t row = static_cast<int64_t>(block) * RB + rb;
   load(row);
 #pragma unroll
   for (int v = 0; v < NV; ++v) w[v] = raw_of<W>(wp + col(v), wp ? a.N - col(v) : 0);
@@ -267,7 +268,7 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_grad_kernel(const gt
     }
   }
   if constexpr (SUMS) {
-    float* out = part + int64_t{blockIdx.x} * 2 * a.N;
+    float* out = part + static_cast<int64_t>(block) * 2 * a.N;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
 #pragma unroll
@@ -289,6 +290,62 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_grad_kernel(const gt
       }
     }
   }
+}
+
+template <typename T, typename W, int TH, int NV, bool SUMS>
+__global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_grad_kernel(const gt_norm_grad_args a, float* part) {
+  grad_rows<T, W, TH, NV, SUMS>(a, part, static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
+}
+
+// dw and db of 32 columns over all rows, 4 threads a row.
+template <typename T, int NT>
+__device__ __forceinline__ void grad_columns(const gt_norm_grad_args& a, int block) {
+  constexpr int RL = NT / 4, PARTS = NT / 64;
+  __shared__ __align__(16) float sums[RL][68];   // [row lane][dw, then db, 32 columns each]
+  __shared__ float parts[PARTS][64];
+  const int q = threadIdx.x & 3, rl = threadIdx.x >> 2;
+  const int64_t c = static_cast<int64_t>(block) * 32 + q * 8, left = a.N - c;
+  oct dw{}, db{};
+#pragma unroll 8
+  for (int64_t row = rl; row < a.M; row += RL) {
+    const oct x = open8<T>(raw_of<T>(static_cast<const T*>(a.X) + row * a.ldx + c, left));
+    const oct y = open8<T>(raw_of<T>(static_cast<const T*>(a.dY) + row * a.lddy + c, left));
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    dw.a += y.a * ((x.a - mean) * rstd);
+    dw.b += y.b * ((x.b - mean) * rstd);
+    db.a += y.a;
+    db.b += y.b;
+  }
+  f32x4* mine = reinterpret_cast<f32x4*>(&sums[rl][q * 8]);
+  mine[0] = dw.a;
+  mine[1] = dw.b;
+  mine[8] = db.a;
+  mine[9] = db.b;
+  __syncthreads();
+  const int j = threadIdx.x & 63, p = threadIdx.x >> 6;
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < RL / PARTS; ++i) s += sums[p * (RL / PARTS) + i][j];
+  parts[p][j] = s;
+  __syncthreads();
+  const int64_t n = static_cast<int64_t>(block) * 32 + (j & 31);
+  float* out = j < 32 ? a.dw : a.db;
+  if (p > 0 || n >= a.N || !out) return;
+  s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) s += parts[i][j];
+  out[n] = s;
+}
+
+// Few rows: their statistics are given, so that the columns' sums need not wait for the rows. The
+// first `columns` workgroups take 32 columns each, the others rows: one launch, no scratch.
+template <typename T, typename W, int TH, int NV>
+__global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_grad_few_kernel(const gt_norm_grad_args a, int columns) {
+  const int block = static_cast<int>(blockIdx.x);
+  if (block < columns)
+    grad_columns<T, TH < 256 ? 256 : TH>(a, block);
+  else
+    grad_rows<T, W, TH, NV, false>(a, nullptr, block - columns, static_cast<int>(gridDim.x) - columns);
 }
 
 // Long rows: dX alone, read twice.
@@ -442,7 +499,7 @@ unsigned grad_grid(int64_t M, const Rows& r) {
 // Rows too wide for the sums' registers beside their own: the sums by a kernel of their own, which
 // reads X and dY again (2048×16384 in bf16 78 µs, 124 with spilled sums in one).
 bool sums_apart(const Rows& r) { return r.threads == 0 || r.octets == 4; }
-unsigned apart_parts(int64_t M) { return static_cast<unsigned>(std::min<int64_t>((M + 3) / 4, 64)); }
+unsigned sums_parts(int64_t M) { return static_cast<unsigned>(std::min<int64_t>((M + 3) / 4, 64)); }
 
 template <typename T, typename W, bool SUMS>
 hipError_t grad_by(const gt_norm_grad_args& a, float* part, hipStream_t s) {
@@ -458,16 +515,50 @@ hipError_t grad_by(const gt_norm_grad_args& a, float* part, hipStream_t s) {
   return hipGetLastError();
 }
 
+// The columns' own pass reads X and dY again, 32 columns a workgroup: faster than the sums' way
+// through memory and their launch while its rows are few (bf16, with R, in a graph: 128×4096
+// 4.3 µs, 8.6 in two launches; 1024×1000 7.9, 9.0; 1024×4096 12.5, 19.9; 1024×8192 21.7, 19.8;
+// 2048×4096 21.6, 20.4), and a launch and an allocation less for the host (5 µs).
+constexpr int64_t kFewRows = 1024;
+bool few_rows(int64_t M, const Rows& r) { return r.threads > 0 && M <= kFewRows; }
+
+template <typename T, typename W>
+hipError_t few_by(const gt_norm_grad_args& a, int columns, bool rows, hipStream_t s) {
+  const Rows r = rows_of(a.N);
+  const unsigned grid = columns + (rows ? grad_grid(a.M, r) : 0);
+  if (r.threads == 64 && r.octets == 1) norm_grad_few_kernel<T, W, 64, 1><<<grid, 256, 0, s>>>(a, columns);
+  else if (r.threads == 64) norm_grad_few_kernel<T, W, 64, 2><<<grid, 256, 0, s>>>(a, columns);
+  else if (r.threads == 256 && r.octets == 1) norm_grad_few_kernel<T, W, 256, 1><<<grid, 256, 0, s>>>(a, columns);
+  else if (r.threads == 256) norm_grad_few_kernel<T, W, 256, 2><<<grid, 256, 0, s>>>(a, columns);
+  else if (r.octets == 2) norm_grad_few_kernel<T, W, 512, 2><<<grid, 512, 0, s>>>(a, columns);
+  else norm_grad_few_kernel<T, W, 512, 4><<<grid, 512, 0, s>>>(a, columns);
+  return hipGetLastError();
+}
+// The bytes from p on of rows ld apart, and others: do they share any?
+bool apart(const void* p, int64_t ldp, const void* q, int64_t ldq, int64_t M, int64_t N, int64_t size) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a + ((M - 1) * ldp + N) * size <= b || b + ((M - 1) * ldq + N) * size <= a;
+}
+template <typename T, typename W>
+hipError_t few(const gt_norm_grad_args& a, hipStream_t s) {
+  const int columns = static_cast<int>((a.N + 31) / 32);
+  const bool one = !a.dX || (apart(a.dX, a.lddx, a.dY, a.lddy, a.M, a.N, sizeof(T)) &&
+                             apart(a.dX, a.lddx, a.X, a.ldx, a.M, a.N, sizeof(T)));
+  const hipError_t e = few_by<T, W>(a, columns, a.dX && one, s);
+  return e != hipSuccess || one ? e : few_by<T, W>(a, 0, true, s);   // (dX over dY: when its sums are taken)
+}
+
 template <typename T, typename W>
 hipError_t grad(const gt_norm_grad_args& a, float* part, hipStream_t s) {
   hipError_t e = hipSuccess;
-  const bool apart = sums_apart(rows_of(a.N));
-  if (a.M > 0 && part && apart) {   // (before dX, which may be dY)
-    norm_sums_kernel<T><<<dim3(static_cast<unsigned>((a.N + 511) / 512), apart_parts(a.M)), 256, 0, s>>>(a, part);
+  if (a.M > 0 && (a.dw || a.db) && few_rows(a.M, rows_of(a.N))) return few<T, W>(a, s);
+  const bool own = sums_apart(rows_of(a.N));
+  if (a.M > 0 && part && own) {   // (before dX, which may be dY)
+    norm_sums_kernel<T><<<dim3(static_cast<unsigned>((a.N + 511) / 512), sums_parts(a.M)), 256, 0, s>>>(a, part);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && a.M > 0 && (a.dX || (part && !apart)))
-    e = part && !apart ? grad_by<T, W, true>(a, part, s) : grad_by<T, W, false>(a, part, s);
+  if (e == hipSuccess && a.M > 0 && (a.dX || (part && !own)))
+    e = part && !own ? grad_by<T, W, true>(a, part, s) : grad_by<T, W, false>(a, part, s);
   if (e != hipSuccess || (!a.dw && !a.db)) return e;
   const unsigned columns = static_cast<unsigned>(std::min<int64_t>((a.N + 63) / 64, int64_t{1} << 20));
   norm_join_kernel<<<dim3(columns, 2), 1024, 0, s>>>(part, norm_parts(a), a.N, a.dw, a.db);
@@ -484,7 +575,8 @@ hipError_t launch_norm(const gt_norm_args& a, hipStream_t s) {
 int64_t norm_parts(const gt_norm_grad_args& a) {
   if (a.M == 0 || (!a.dw && !a.db)) return 0;
   const Rows r = rows_of(a.N);
-  return sums_apart(r) ? apart_parts(a.M) : grad_grid(a.M, r);
+  if (few_rows(a.M, r)) return 0;
+  return sums_apart(r) ? sums_parts(a.M) : grad_grid(a.M, r);
 }
 
 hipError_t launch_norm_grad(const gt_norm_grad_args& a, float* part, hipStream_t s) {

@@ -241,6 +241,50 @@ def test_norm_backward(L, dtype, shape):
         assert torch.equal(both.dX, g.dX) and torch.equal(both.dweight, g.dweight)
 
 
+@pytest.mark.parametrize("shape", [(1024, 40), (1025, 40), (1040, 1000), (1030, 2050), (1026, 4100), (1025, 8200)], ids=str)
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=IDS.get)
+def test_norm_backward_past_few_rows(L, dtype, shape):
+    """Either side of the rows up to which one launch takes the columns' sums."""
+    M, N = shape
+    f = Frame(5, 3)
+    X, dY = f.place(rows(f.gen, M, N, dtype)), f.normal(dtype, M, N)
+    w = f.normal(F32, N)
+    dX = f.output(dtype, M, N)
+    mean, rstd = torch.empty(2, M, device="cuda")
+    L.gt_norm(X, w, mean=mean, rstd=rstd)
+    note(f"norm backward {dtype} {shape}")
+    g = L.gt_norm_backward(dY, X, mean, rstd, weight=w, dX=dX)
+    torch.cuda.synchronize()
+    want = ref8.norm_backward(dY, X, mean, rstd, w, None, dtype)
+    for have, (v, err), name in zip(g, want, ("dX", "dw", "db")):
+        ref.check(have, (v, err), name)
+    f.untouched()
+    assert torch.equal(L.gt_norm_backward(dY, X, mean, rstd, weight=w, need=("dweight",), bias=False).dweight, g.dweight)
+    both = L.gt_norm_backward(dY, X, mean, rstd, weight=w, dX=dY)
+    torch.cuda.synchronize()
+    assert torch.equal(both.dX, g.dX) and torch.equal(both.dweight, g.dweight) and torch.equal(both.dbias, g.dbias)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=IDS.get)
+def test_norm_backward_where_dx_lies(L, dtype):
+    """dX over all of dY, in the other columns of dY's rows, and over X: the sums are of what was there."""
+    M, N = 300, 520
+    gen = torch.Generator().manual_seed(2)
+    x, y = rows(gen, M, N, dtype).cuda(), rows(gen, M, N, dtype).cuda()
+    mean, rstd = torch.empty(2, M, device="cuda")
+    L.gt_norm(x, mean=mean, rstd=rstd)
+    want = L.gt_norm_backward(y, x, mean, rstd)
+    wide = torch.empty(M, 2 * N, dtype=dtype, device="cuda")
+    wide[:, :N] = y
+    over, beside, X = y.clone(), wide[:, N:], x.clone()
+    got = [L.gt_norm_backward(over, x, mean, rstd, dX=over), L.gt_norm_backward(wide[:, :N], x, mean, rstd, dX=beside),
+           L.gt_norm_backward(y, X, mean, rstd, dX=X)]
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g, want))
+    assert torch.equal(wide[:, :N], y)
+
+
 def test_norm_gradients_against_differences(L):
     """The directional derivative of Σ c·Y by central differences in 64 bits."""
     gen = torch.Generator().manual_seed(4)

@@ -88,7 +88,7 @@ def test_null_arguments_are_refused(L, name):
 @pytest.mark.parametrize("name,change", [
     ("gt_linear_fp8", dict(M=256, N=2048, K=8192, ldx=8192, ldw=8192, ldsx=64, ldsw=64, act=0, ldr=2048, ldy=2048)),
     ("gt_linear_fp8", dict(M=3000, N=2048, K=4099, ldx=4099, ldw=4099, ldsx=33, ldsw=33, act=0, ldr=2048, ldy=2048)),
-    ("gt_norm_backward", {})])
+    ("gt_norm_backward", dict(M=1025))])
 def test_scratch_too_small_or_misaligned(L, name, change):
     a = args(L, name, **change)
     need = L.workspace_bytes(name, a)
@@ -97,6 +97,14 @@ def test_scratch_too_small_or_misaligned(L, name, change):
     assert call(L, name, a, AT, 0) == GT_ESMALL
     assert call(L, name, a, None, need) == GT_EINVAL
     assert call(L, name, a, AT + 16, need) == GT_EINVAL
+
+
+def test_sums_of_few_rows_need_no_scratch(L):
+    """Whatever is wanted and wherever dX lies."""
+    for change in ({}, dict(dX=AT), dict(dX=None), dict(dw=None), dict(M=1024), dict(N=16384)):
+        n = dict(N=16384, lddy=16384, ldx=16384, ldr=16384, lddx=16384) if "N" in change else {}
+        assert L.workspace_bytes("gt_norm_backward", args(L, "gt_norm_backward", **{**change, **n})) == 0
+    assert L.workspace_bytes("gt_norm_backward", args(L, "gt_norm_backward", M=1025)) > 0
 
 
 def test_copies_are_as_large_as_the_rows(L):
