@@ -174,13 +174,15 @@ def _tensor(t, name, like, shape, dtype=None):
     contiguous; its pointer and row stride."""
     if t.dtype is not (dtype or like.dtype):
         raise ValueError(f"{name} must be {dtype or like.dtype}")
-    if t.device != like.device:
+    if t.get_device() != like.get_device():
         raise ValueError(f"{name} must be a GPU tensor on {like.device}")
     have = t.shape
     if have != shape:
         raise ValueError(f"{name} has shape {tuple(have)}, not {tuple(shape)}")
     st = t.stride()
     n = len(st)
+    if n == 2 and st[1] == 1 and st[0] >= have[1] > 0:   # (nearly every call)
+        return t.data_ptr(), st[0]
     if n == 0 or (st[-1] != 1 and have[-1] != 1):
         raise ValueError(f"the rows of {name} must be contiguous")
     cols = have[-1]
@@ -227,41 +229,49 @@ def _call(name, a, like, workspace, stream):
     import torch
     if _lib is None:
         lib()
-    if like.device.index == torch._C._cuda_getDevice():
-        _launch(name, a, like, workspace, stream)
+    device = like.get_device()
+    if device == torch._C._cuda_getDevice():
+        # (the current stream's handle alone, as _stream gives it)
+        on = torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
+        _launch(name, a, like, workspace, stream, on)
         return
-    with torch.cuda.device(like.device):
-        _launch(name, a, like, workspace, stream)
+    with torch.cuda.device(device):
+        _launch(name, a, like, workspace, stream, _stream(stream))
 
 
-def _launch(name, a, like, workspace, stream):
+def _launch(name, a, like, workspace, stream, on):
     run, query = _calls[name]
     ref = ctypes.byref(a)
     if query is None:
-        _check(run(ref, _stream(stream)), name)
-        return
-    need = _i64()
-    _check(query(ref, ctypes.byref(need)), name)
-    n = need.value
-    if n == 0:
-        _check(run(ref, None, 0, _stream(stream)), name)
-        return
-    if workspace is None:
-        import torch
-        workspace = _empty((n,), torch.uint8, like.device, stream)
-    elif workspace.device != like.device or not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous, on the operands' device")
-    _check(run(ref, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)), name)
+        rc = run(ref, on)
+    else:
+        need = _i64()
+        _check(query(ref, ctypes.byref(need)), name)
+        n = need.value
+        if n == 0:
+            rc = run(ref, None, 0, on)
+        else:
+            if workspace is None:
+                import torch
+                workspace = _empty((n,), torch.uint8, like.device, stream)
+            elif workspace.device != like.device or not workspace.is_contiguous():
+                raise ValueError("workspace must be contiguous, on the operands' device")
+            rc = run(ref, workspace.data_ptr(), workspace.numel() * workspace.element_size(), on)
+    if rc != 0:
+        _check(rc, name)
 
 
 def _empty(shape, dtype, device, stream, ld=None):
     """Memory for the stream the call runs on (PyTorch's allocator gives memory that is
     free in the order of one stream); ld: elements between rows."""
     import torch
-    if stream is None:
-        if ld is None or ld == shape[1]:
-            return torch.empty(shape, dtype=dtype, device=device)
-        return torch.empty_strided(shape, (ld, 1), dtype=dtype, device=device)
+    if stream is None:   # (strides given: a third of a microsecond less than torch.empty)
+        n = len(shape)
+        if n == 2:
+            return torch.empty_strided(shape, (ld or shape[1] or 1, 1), dtype=dtype, device=device)
+        if n == 1:
+            return torch.empty_strided(shape, (1,), dtype=dtype, device=device)
+        return torch.empty(shape, dtype=dtype, device=device)
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
     with torch.cuda.stream(stream):
@@ -579,12 +589,14 @@ def gt_linear_fp8(X, W, bias=None, residual=None, act="none", gated=False, Y=Non
     typed = bias if bias is not None else residual
     if Y is None:
         Y = _empty((M, N), torch.bfloat16 if typed is None else typed.dtype, like.device, stream)
+        y, ldy = Y.data_ptr(), N
+    else:
+        y, ldy = _tensor(Y, "Y", like, (M, N), Y.dtype)
     typed = Y if typed is None else typed
     dt = _type(typed, "Y" if typed is Y else "bias" if typed is bias else "residual")
     b = _one(bias, "bias", like, (wide,), typed.dtype)
     r, ldr = _pair(residual, "residual", like, (M, N), typed.dtype)
     out = _result_type(Y, "Y", typed)
-    y, ldy = _tensor(Y, "Y", like, (M, N), Y.dtype)
     _call("gt_linear_fp8",
           gt_linear_fp8_args(M, N, K, dt, _act(act, gated), out, xc, wc, xb, wb, 0, x, ldx, sx, ldsx, w, ldw,
                              sw, ldsw, b, r, ldr, y, ldy), like, workspace, stream)
@@ -647,8 +659,13 @@ def gt_norm_backward(dY, X, mean, rstd, weight=None, residual=None, bias=True, d
     _gpu(X, "X", 2)
     M, N = X.shape
     dt = _type(X, "X")
-    if dX is None and "dX" in need:
+    if dX is not None:
+        dx, lddx = _tensor(dX, "dX", X, (M, N))
+    elif "dX" in need:
         dX = _empty((M, N), X.dtype, X.device, stream)
+        dx, lddx = dX.data_ptr(), N
+    else:
+        dx, lddx = None, 0
     dw = _empty((N,), torch.float32, X.device, stream) if "dweight" in need else None
     db = _empty((N,), torch.float32, X.device, stream) if bias else None
     dy, lddy = _tensor(dY, "dY", X, (M, N))
@@ -656,7 +673,6 @@ def gt_norm_backward(dY, X, mean, rstd, weight=None, residual=None, bias=True, d
     wt = dt if weight is None else _result_type(weight, "weight", X)
     w = None if weight is None else _whole(weight, "weight", X, (N,), weight.dtype)
     r, ldr = _pair(residual, "residual", X, (M, N))
-    dx, lddx = _pair(dX, "dX", X, (M, N))
     _call("gt_norm_backward",
           gt_norm_grad_args(M, N, dt, wt, dy, lddy, x, ldx, w, _whole(mean, "mean", X, (M,), torch.float32),
                             _whole(rstd, "rstd", X, (M,), torch.float32), r, ldr, dx, lddx,
