@@ -4,7 +4,7 @@
 // mean costs no digits, then the outputs: each row is read once and written once.
 // Backward: both means of a row in one exchange; every thread keeps the column sums of dw
 // and db for its own columns over all rows that its workgroup takes, and a second launch
-// adds the workgroups' sums in their order. Up to 1024 rows other workgroups of the same
+// adds the workgroups' sums in their order. Of few rows other workgroups of the same
 // launch take the columns' sums.
 // Bound by memory: 16384×4096 in bf16 with mean and rstd 49 µs, 5.5 TB/s; its gradients with
 // R 104 µs, 5.2 TB/s. One row of 4096 in bf16 is latency, 2.7 µs on the GPU.
@@ -297,39 +297,67 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_grad_kernel(const gt
   grad_rows<T, W, TH, NV, SUMS>(a, part, static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
 }
 
-// dw and db of 32 columns over all rows, 4 threads a row.
-template <typename T, int NT>
+// dw and db of 8·QL columns over all rows, QL of the NT threads a row.
+template <typename T, int NT, int QL>
 __device__ __forceinline__ void grad_columns(const gt_norm_grad_args& a, int block) {
-  constexpr int RL = NT / 4, PARTS = NT / 64;
-  __shared__ __align__(16) float sums[RL][68];   // [row lane][dw, then db, 32 columns each]
-  __shared__ float parts[PARTS][64];
-  const int q = threadIdx.x & 3, rl = threadIdx.x >> 2;
-  const int64_t c = static_cast<int64_t>(block) * 32 + q * 8, left = a.N - c;
+  constexpr int C = 8 * QL, RL = NT / QL, PARTS = NT / (2 * C);
+  __shared__ __align__(16) float sums[RL][2 * C + 4];   // [row lane][dw, then db, of C columns]
+  __shared__ float parts[PARTS][2 * C];
+  const int q = threadIdx.x % QL, rl = threadIdx.x / QL;
+  const int64_t c = static_cast<int64_t>(block) * C + q * 8, left = a.N - c;
+  const T* X = static_cast<const T*>(a.X) + c;
+  const T* Y = static_cast<const T*>(a.dY) + c;
   oct dw{}, db{};
-#pragma unroll 8
-  for (int64_t row = rl; row < a.M; row += RL) {
-    const oct x = open8<T>(raw_of<T>(static_cast<const T*>(a.X) + row * a.ldx + c, left));
-    const oct y = open8<T>(raw_of<T>(static_cast<const T*>(a.dY) + row * a.lddy + c, left));
-    const float mean = a.mean[row], rstd = a.rstd[row];
+  auto add = [&](const raw8<T>& xr, const raw8<T>& yr, float mean, float rstd) __attribute__((always_inline)) {
+    const oct x = open8<T>(xr), y = open8<T>(yr);
     dw.a += y.a * ((x.a - mean) * rstd);
     dw.b += y.b * ((x.b - mean) * rstd);
     db.a += y.a;
     db.b += y.b;
+  };
+  if (left >= 8) {   // U rows' loads at once; rows past the last count as zeros
+    constexpr int U = 4;
+    for (int64_t row = rl; row < a.M; row += U * RL) {
+      raw8<T> x[U], y[U];
+      float mean[U], rstd[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int64_t at = row + i * RL < a.M ? row + i * RL : a.M - 1;
+        __builtin_memcpy(&x[i], X + at * a.ldx, sizeof(x[i]));
+        __builtin_memcpy(&y[i], Y + at * a.lddy, sizeof(y[i]));
+        mean[i] = a.mean[at];
+        rstd[i] = a.rstd[at];
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const bool live = row + i * RL < a.M;
+        raw8<T> xs, ys;
+#pragma unroll
+        for (size_t k = 0; k < sizeof(xs.w) / sizeof(xs.w[0]); ++k) {
+          xs.w[k] = live ? x[i].w[k] : u32x4{};
+          ys.w[k] = live ? y[i].w[k] : u32x4{};
+        }
+        add(xs, ys, live ? mean[i] : 0.0f, live ? rstd[i] : 0.0f);
+      }
+    }
+  } else if (left > 0) {
+    for (int64_t row = rl; row < a.M; row += RL)
+      add(raw_of<T>(X + row * a.ldx, left), raw_of<T>(Y + row * a.lddy, left), a.mean[row], a.rstd[row]);
   }
   f32x4* mine = reinterpret_cast<f32x4*>(&sums[rl][q * 8]);
   mine[0] = dw.a;
   mine[1] = dw.b;
-  mine[8] = db.a;
-  mine[9] = db.b;
+  mine[C / 4] = db.a;
+  mine[C / 4 + 1] = db.b;
   __syncthreads();
-  const int j = threadIdx.x & 63, p = threadIdx.x >> 6;
+  const int j = threadIdx.x % (2 * C), p = threadIdx.x / (2 * C);
   float s = 0.0f;
 #pragma unroll
   for (int i = 0; i < RL / PARTS; ++i) s += sums[p * (RL / PARTS) + i][j];
   parts[p][j] = s;
   __syncthreads();
-  const int64_t n = static_cast<int64_t>(block) * 32 + (j & 31);
-  float* out = j < 32 ? a.dw : a.db;
+  const int64_t n = static_cast<int64_t>(block) * C + j % C;
+  float* out = j < C ? a.dw : a.db;
   if (p > 0 || n >= a.N || !out) return;
   s = 0.0f;
 #pragma unroll
@@ -338,12 +366,12 @@ __device__ __forceinline__ void grad_columns(const gt_norm_grad_args& a, int blo
 }
 
 // Few rows: their statistics are given, so that the columns' sums need not wait for the rows. The
-// first `columns` workgroups take 32 columns each, the others rows: one launch, no scratch.
-template <typename T, typename W, int TH, int NV>
+// first `columns` workgroups take 8·QL columns each, the others rows: one launch, no scratch.
+template <typename T, typename W, int TH, int NV, int QL>
 __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_grad_few_kernel(const gt_norm_grad_args a, int columns) {
   const int block = static_cast<int>(blockIdx.x);
   if (block < columns)
-    grad_columns<T, TH < 256 ? 256 : TH>(a, block);
+    grad_columns<T, TH < 256 ? 256 : TH, QL>(a, block);
   else
     grad_rows<T, W, TH, NV, false>(a, nullptr, block - columns, static_cast<int>(gridDim.x) - columns);
 }
@@ -515,23 +543,36 @@ hipError_t grad_by(const gt_norm_grad_args& a, float* part, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The columns' own pass reads X and dY again, 32 columns a workgroup: faster than the sums' way
-// through memory and their launch while its rows are few (bf16, with R, in a graph: 128×4096
-// 4.3 µs, 8.6 in two launches; 1024×1000 7.9, 9.0; 1024×4096 12.5, 19.9; 1024×8192 21.7, 19.8;
-// 2048×4096 21.6, 20.4), and a launch and an allocation less for the host (5 µs).
-constexpr int64_t kFewRows = 1024;
-bool few_rows(int64_t M, const Rows& r) { return r.threads > 0 && M <= kFewRows; }
+// The columns' own pass reads X and dY again, few columns a workgroup: faster than the sums' way
+// through memory and their launch while its rows are few (with R, in a graph, two launches in
+// brackets: bf16 100×4096 4.1 µs (9.3), 1000×1024 8.1 (10.3), 1000×4096 11.9 (19.4), 500×8192
+// 13.1 (17.8), 1000×8192 21.2 (18.9); fp32 1000×4096 16.6 (18.4)), and a launch and an
+// allocation less for the host (5 µs).
+bool few_rows(int64_t M, int64_t N) { return rows_of(N).threads > 0 && M <= (N <= 4096 ? 1024 : 512); }
+// Threads a row: 4 take 64 or 128 bytes of it. Unaligned accesses are slower in a unit's memory
+// pipeline, for which narrow rows get more workgroups (bf16, 1000×1021 9.7 µs, with 4 threads
+// 16.6; 1000×4095 31.8 and 21.0; aligned 1000×1024 9.4 and 8.1).
+int column_threads(const gt_norm_grad_args& a) {
+  const int64_t size = a.dtype == GT_F32 ? 4 : 2;
+  const uint64_t bits = reinterpret_cast<uintptr_t>(a.X) | reinterpret_cast<uintptr_t>(a.dY) |
+                        static_cast<uint64_t>(a.ldx * size) | static_cast<uint64_t>(a.lddy * size);
+  return bits % 16 == 0 || a.N > 2048 ? 4 : 1;
+}
 
-template <typename T, typename W>
+template <typename T, typename W, int QL>
 hipError_t few_by(const gt_norm_grad_args& a, int columns, bool rows, hipStream_t s) {
   const Rows r = rows_of(a.N);
   const unsigned grid = columns + (rows ? grad_grid(a.M, r) : 0);
-  if (r.threads == 64 && r.octets == 1) norm_grad_few_kernel<T, W, 64, 1><<<grid, 256, 0, s>>>(a, columns);
-  else if (r.threads == 64) norm_grad_few_kernel<T, W, 64, 2><<<grid, 256, 0, s>>>(a, columns);
-  else if (r.threads == 256 && r.octets == 1) norm_grad_few_kernel<T, W, 256, 1><<<grid, 256, 0, s>>>(a, columns);
-  else if (r.threads == 256) norm_grad_few_kernel<T, W, 256, 2><<<grid, 256, 0, s>>>(a, columns);
-  else if (r.octets == 2) norm_grad_few_kernel<T, W, 512, 2><<<grid, 512, 0, s>>>(a, columns);
-  else norm_grad_few_kernel<T, W, 512, 4><<<grid, 512, 0, s>>>(a, columns);
+  if (r.threads == 64 && r.octets == 1) norm_grad_few_kernel<T, W, 64, 1, QL><<<grid, 256, 0, s>>>(a, columns);
+  else if (r.threads == 64) norm_grad_few_kernel<T, W, 64, 2, QL><<<grid, 256, 0, s>>>(a, columns);
+  else if (r.threads == 256 && r.octets == 1) norm_grad_few_kernel<T, W, 256, 1, QL><<<grid, 256, 0, s>>>(a, columns);
+  else if constexpr (QL == 4) {
+    if (r.threads == 256) norm_grad_few_kernel<T, W, 256, 2, QL><<<grid, 256, 0, s>>>(a, columns);
+    else if (r.octets == 2) norm_grad_few_kernel<T, W, 512, 2, QL><<<grid, 512, 0, s>>>(a, columns);
+    else norm_grad_few_kernel<T, W, 512, 4, QL><<<grid, 512, 0, s>>>(a, columns);
+  } else {
+    return hipErrorInvalidValue;   // (column_threads: not above 2048 columns)
+  }
   return hipGetLastError();
 }
 // The bytes from p on of rows ld apart, and others: do they share any?
@@ -541,17 +582,18 @@ bool apart(const void* p, int64_t ldp, const void* q, int64_t ldq, int64_t M, in
 }
 template <typename T, typename W>
 hipError_t few(const gt_norm_grad_args& a, hipStream_t s) {
-  const int columns = static_cast<int>((a.N + 31) / 32);
+  const int ql = column_threads(a), columns = static_cast<int>((a.N + 8 * ql - 1) / (8 * ql));
   const bool one = !a.dX || (apart(a.dX, a.lddx, a.dY, a.lddy, a.M, a.N, sizeof(T)) &&
                              apart(a.dX, a.lddx, a.X, a.ldx, a.M, a.N, sizeof(T)));
-  const hipError_t e = few_by<T, W>(a, columns, a.dX && one, s);
-  return e != hipSuccess || one ? e : few_by<T, W>(a, 0, true, s);   // (dX over dY: when its sums are taken)
+  auto go = ql == 1 ? few_by<T, W, 1> : few_by<T, W, 4>;
+  const hipError_t e = go(a, columns, a.dX && one, s);
+  return e != hipSuccess || one ? e : go(a, 0, true, s);   // (dX over dY: when its sums are taken)
 }
 
 template <typename T, typename W>
 hipError_t grad(const gt_norm_grad_args& a, float* part, hipStream_t s) {
   hipError_t e = hipSuccess;
-  if (a.M > 0 && (a.dw || a.db) && few_rows(a.M, rows_of(a.N))) return few<T, W>(a, s);
+  if (a.M > 0 && (a.dw || a.db) && few_rows(a.M, a.N)) return few<T, W>(a, s);
   const bool own = sums_apart(rows_of(a.N));
   if (a.M > 0 && part && own) {   // (before dX, which may be dY)
     norm_sums_kernel<T><<<dim3(static_cast<unsigned>((a.N + 511) / 512), sums_parts(a.M)), 256, 0, s>>>(a, part);
@@ -575,7 +617,7 @@ hipError_t launch_norm(const gt_norm_args& a, hipStream_t s) {
 int64_t norm_parts(const gt_norm_grad_args& a) {
   if (a.M == 0 || (!a.dw && !a.db)) return 0;
   const Rows r = rows_of(a.N);
-  if (few_rows(a.M, r)) return 0;
+  if (few_rows(a.M, a.N)) return 0;
   return sums_apart(r) ? sums_parts(a.M) : grad_grid(a.M, r);
 }
 
