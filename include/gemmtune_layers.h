@@ -334,7 +334,8 @@ int gt_norm(const gt_norm_args* a, void* stream);
 /* Gradients of gt_norm. With h = (X − mean)·rstd and g = dY·w: dX = rstd·(g − mean of g −
  * h·mean of g·h) + R (the means over the row; M×N, dtype), dw = Σ over rows of dY·h and db = Σ of dY
  * (N, fp32). Any of the three may be NULL. R (M×N in dtype or NULL): the gradient that
- * reaches X by another way; dX may be R, or dY. mean, rstd as gt_norm gave them. */
+ * reaches X by another way; dX may be R, or dY. mean, rstd as gt_norm gave them: h is off by what the mean's
+ * rounding to fp32 is of a deviation, up to 2^-24·|mean|·rstd. */
 typedef struct gt_norm_grad_args {
   int64_t M, N;
   int32_t dtype, wtype;

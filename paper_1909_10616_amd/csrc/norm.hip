@@ -1,7 +1,9 @@
 // Layer norm and its gradients, a row in the registers of 64 to 512 threads.
 //
-// Forward: the mean, then Σ(X − mean)² of the values that the registers hold, so that a large
-// mean costs no digits, then the outputs: each row is read once and written once.
+// Forward: the mean, then in one exchange Σ(X − mean) and Σ(X − mean)² of the values that the registers
+// hold, then the outputs: each row is read once and written once. The first of the two sums is what
+// the mean has lost to rounding (4096 values with a mean of 10^5 deviations: 1 % of a deviation); it is
+// taken off the deviations, their variance and the mean, so that a large mean costs no digits.
 // Backward: both means of a row in one exchange; every thread keeps the column sums of dw
 // and db for its own columns over all rows that its workgroup takes, and a second launch
 // adds the workgroups' sums in their order. Of few rows other workgroups of the same
@@ -38,6 +40,26 @@ __device__ __forceinline__ float row_sum(float s, float* box) {
   return s;
 }
 
+// Two sums in one exchange.
+template <int TH>
+__device__ __forceinline__ void row_sums(float* s, float* q, float (*box)[16]) {
+  *s = wave_sum(*s);
+  *q = wave_sum(*q);
+  if constexpr (TH > 64) {
+    if ((threadIdx.x & 63) == 0) {
+      box[0][threadIdx.x >> 6] = *s;
+      box[1][threadIdx.x >> 6] = *q;
+    }
+    __syncthreads();
+    *s = *q = 0.0f;
+#pragma unroll
+    for (int i = 0; i < TH / 64; ++i) {
+      *s += box[0][i];
+      *q += box[1][i];
+    }
+  }
+}
+
 template <typename W>
 __device__ __forceinline__ oct open_or(const void* p, const raw8<W>& r, float none) {
   return p ? open8<W>(r) : oct{f32x4{none, none, none, none}, f32x4{none, none, none, none}};
@@ -60,16 +82,30 @@ __device__ __forceinline__ oct centred(const oct& v, float m, int64_t n) {
 
 // ---- forward
 
-// An octet of a row's outputs from X − mean.
+// The reciprocal deviation of a row from the mean square of its deviations from a mean that is off by `off`.
+// (Fused, so that an infinite square stays one; rounding may leave less than nothing of a constant row.)
+__device__ __forceinline__ float deviation(float square, float off, float eps) {
+  const float v = fmaf(-off, off, square);
+  return 1.0f / sqrtf((v < 0.0f ? 0.0f : v) + eps);
+}
+
+// An octet of a row's outputs from its deviations from a mean that is off by `off`.
 template <typename T, int CODE>
-__device__ __forceinline__ void norm_out(const gt_norm_args& a, int64_t row, int64_t c, const oct& d,
+__device__ __forceinline__ void norm_out(const gt_norm_args& a, int64_t row, int64_t c, const oct& d, float off,
                                          float rstd, const oct& w, const oct& b) {
   const int64_t left = a.N - c;
   oct y;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    y.a[i] = fmaf(d.a[i] * rstd, w.a[i], b.a[i]);
-    y.b[i] = fmaf(d.b[i] * rstd, w.b[i], b.b[i]);
+    y.a[i] = fmaf((d.a[i] - off) * rstd, w.a[i], b.a[i]);
+    y.b[i] = fmaf((d.b[i] - off) * rstd, w.b[i], b.b[i]);
+  }
+  if (CODE >= 0 && left < 8) {   // (what is behind the row is not among a block's values)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y.a[i] = i < left ? y.a[i] : 0.0f;
+      y.b[i] = i + 4 < left ? y.b[i] : 0.0f;
+    }
   }
   if (a.Y && left > 0) store8n(static_cast<T*>(a.Y) + row * a.ldy + c, y, left);
   if constexpr (CODE >= 0) {
@@ -83,7 +119,7 @@ __device__ __forceinline__ void norm_out(const gt_norm_args& a, int64_t row, int
 template <typename T, typename W, int TH, int NV, int CODE>
 __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_kernel(const gt_norm_args a) {
   constexpr int RB = TH < 256 ? 256 / TH : 1;   // rows of a workgroup
-  __shared__ float box[2][16];
+  __shared__ float box[3][16];
   const int t = threadIdx.x % TH, rb = threadIdx.x / TH;
   const W* wp = static_cast<const W*>(a.w);
   const W* bp = static_cast<const W*>(a.b);
@@ -103,7 +139,7 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_kernel(const gt_norm
     w[v] = raw_of<W>(wp + col(v), wp ? a.N - col(v) : 0);
     b[v] = raw_of<W>(bp + col(v), bp ? a.N - col(v) : 0);
   }
-  const float n = static_cast<float>(a.N);
+  const float each = 1.0f / static_cast<float>(a.N);   // (what its rounding costs the mean goes off with the rest)
   for (; row < a.M; row += step) {
     oct x[NV];
     float s = 0.0f;
@@ -113,21 +149,24 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_kernel(const gt_norm
       s += sum8(x[v]);
     }
     load(row + step);
-    const float mean = row_sum<TH>(s, box[0]) / n;
+    const float mean = row_sum<TH>(s, box[0]) * each;
+    float squares = 0.0f;
     s = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       x[v] = centred(x[v], mean, a.N - col(v));
-      s += sum8(oct{x[v].a * x[v].a, x[v].b * x[v].b});
+      s += sum8(x[v]);
+      squares += sum8(oct{x[v].a * x[v].a, x[v].b * x[v].b});
     }
-    const float rstd = 1.0f / sqrtf(row_sum<TH>(s, box[1]) / n + a.eps);
+    row_sums<TH>(&s, &squares, box + 1);
+    const float off = s * each, rstd = deviation(squares * each, off, a.eps);
     if (t == 0) {
-      if (a.mean) a.mean[row] = mean;
+      if (a.mean) a.mean[row] = mean + off;
       if (a.rstd) a.rstd[row] = rstd;
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v)
-      norm_out<T, CODE>(a, row, col(v), x[v], rstd, open_or<W>(wp, w[v], 1.0f), open_or<W>(bp, b[v], 0.0f));
+      norm_out<T, CODE>(a, row, col(v), x[v], off, rstd, open_or<W>(wp, w[v], 1.0f), open_or<W>(bp, b[v], 0.0f));
   }
 }
 
@@ -135,28 +174,31 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_kernel(const gt_norm
 template <typename T, typename W, int CODE>
 __global__ __launch_bounds__(1024) void norm_long_kernel(const gt_norm_args a) {
   constexpr int TH = 1024;
-  __shared__ float box[2][16];
+  __shared__ float box[3][16];
   const W* wp = static_cast<const W*>(a.w);
   const W* bp = static_cast<const W*>(a.b);
-  const float n = static_cast<float>(a.N);
+  const float each = 1.0f / static_cast<float>(a.N);
   for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
     const T* x = static_cast<const T*>(a.X) + row * a.ldx;
     float s = 0.0f;
     for (int64_t c = threadIdx.x * 8; c < a.N; c += TH * 8) s += sum8(open8<T>(raw_of<T>(x + c, a.N - c)));
-    const float mean = row_sum<TH>(s, box[0]) / n;
+    const float mean = row_sum<TH>(s, box[0]) * each;
+    float squares = 0.0f;
     s = 0.0f;
     for (int64_t c = threadIdx.x * 8; c < a.N; c += TH * 8) {
       const oct d = centred(open8<T>(raw_of<T>(x + c, a.N - c)), mean, a.N - c);
-      s += sum8(oct{d.a * d.a, d.b * d.b});
+      s += sum8(d);
+      squares += sum8(oct{d.a * d.a, d.b * d.b});
     }
-    const float rstd = 1.0f / sqrtf(row_sum<TH>(s, box[1]) / n + a.eps);
+    row_sums<TH>(&s, &squares, box + 1);
+    const float off = s * each, rstd = deviation(squares * each, off, a.eps);
     if (threadIdx.x == 0) {
-      if (a.mean) a.mean[row] = mean;
+      if (a.mean) a.mean[row] = mean + off;
       if (a.rstd) a.rstd[row] = rstd;
     }
     for (int64_t c0 = 0; c0 < a.N; c0 += TH * 8) {   // (all lanes, for the blocks' maxima)
       const int64_t c = c0 + threadIdx.x * 8, left = a.N - c;
-      norm_out<T, CODE>(a, row, c, centred(open8<T>(raw_of<T>(x + c, left)), mean, left), rstd,
+      norm_out<T, CODE>(a, row, c, centred(open8<T>(raw_of<T>(x + c, left)), mean, left), off, rstd,
                         open_or<W>(wp, raw_of<W>(wp + c, wp ? left : 0), 1.0f),
                         open_or<W>(bp, raw_of<W>(bp + c, bp ? left : 0), 0.0f));
     }
