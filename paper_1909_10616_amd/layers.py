@@ -130,6 +130,9 @@ class NormGrads(typing.NamedTuple):
     dbias: typing.Any
 
 
+_NORM_GRADS = frozenset(NormGrads._fields)
+
+
 _lib = None
 _calls = {}   # entry point → its function and its scratch query (None: no scratch)
 
@@ -652,9 +655,13 @@ def gt_norm_backward(dY, X, mean, rstd, weight=None, residual=None, bias=True, d
                      need=("dX", "dweight"), workspace=None, stream=None) -> NormGrads:
     """The gradients of gt_norm from dY [M, N] and the statistics it kept: dX in X's type, dweight
     and dbias (None unless bias) [N] in float32. residual [M, N]: a gradient that reaches X by
-    another way, added to dX. dX may be the residual or dY itself. need: which of dX and
-    dweight are wanted."""
+    another way, added to dX. dX may be the residual or dY itself. need: which of "dX" and "dweight" are
+    wanted; dbias is wanted with bias, or where it is named there. The sums over the columns read X and dY a
+    second time or take scratch: of dX alone, need="dX", bias=False leaves them out."""
     import torch
+    need = (need,) if isinstance(need, str) else tuple(need)
+    if not _NORM_GRADS.issuperset(need):
+        raise ValueError('need is "dX", "dweight", "dbias" or several of them')
     _gpu(dY, "dY", 2)
     _gpu(X, "X", 2)
     M, N = X.shape
@@ -667,7 +674,7 @@ def gt_norm_backward(dY, X, mean, rstd, weight=None, residual=None, bias=True, d
     else:
         dx, lddx = None, 0
     dw = _empty((N,), torch.float32, X.device, stream) if "dweight" in need else None
-    db = _empty((N,), torch.float32, X.device, stream) if bias else None
+    db = _empty((N,), torch.float32, X.device, stream) if bias or "dbias" in need else None
     dy, lddy = _tensor(dY, "dY", X, (M, N))
     x, ldx = _tensor(X, "X", X, (M, N))
     wt = dt if weight is None else _result_type(weight, "weight", X)
