@@ -48,3 +48,7 @@ hipError_t launch_product8(int dtype, int tile, bool exact, bool uni, const Prod
 hipError_t launch_rows8(int dtype, int rows, bool staged, const Product8& a, hipStream_t s);
 
 }  // namespace gt
+
+// The form that a call takes, so that tests can hold every one: rows a workgroup of the kernels of a few
+// rows (0: tiles), the tile (−1), K slices (0: no form serves), whether all of its sums are fp32's.
+extern "C" int gt_linear_fp8_form(const gt_linear_fp8_args* a, int32_t form[4]);

@@ -312,6 +312,17 @@ int linear_fp8_workspace_impl(const gt_linear_fp8_args* a, int64_t* bytes) {
   return GT_OK;
 }
 
+int linear_fp8_form_impl(const gt_linear_fp8_args* a, int32_t* form) {
+  if (!form) return fail("gt_linear_fp8_form: null argument");
+  GT_CHECK(linear8_checks(a, false));
+  const Linear8 l = linear8(*a);
+  form[0] = l.rows;
+  form[1] = l.rows > 0 ? -1 : l.tile;
+  form[2] = l.q.p.splits;
+  form[3] = l.rows > 0 || l.exact;
+  return GT_OK;
+}
+
 int linear_fp8_impl(const gt_linear_fp8_args* a, void* ws, int64_t ws_bytes, void* stream) {
   GT_CHECK(linear8_checks(a, true));
   if (a->M == 0) return GT_OK;
@@ -358,6 +369,9 @@ int gt_linear_fp8_workspace(const gt_linear_fp8_args* a, int64_t* bytes) {
 }
 int gt_linear_fp8(const gt_linear_fp8_args* a, void* ws, int64_t ws_bytes, void* stream) {
   return guarded([&] { return linear_fp8_impl(a, ws, ws_bytes, stream); });
+}
+int gt_linear_fp8_form(const gt_linear_fp8_args* a, int32_t* form) {
+  return guarded([&] { return linear_fp8_form_impl(a, form); });
 }
 int gt_norm(const gt_norm_args* a, void* stream) {
   return guarded([&] { return norm_impl(a, stream); });
