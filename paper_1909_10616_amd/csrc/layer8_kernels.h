@@ -39,8 +39,8 @@ constexpr Tile8 tile8(int tile) {
   return tile == 0 ? Tile8{256, 256, 2, 4} : tile == 1 ? Tile8{128, 128, 2, 2} : Tile8{64, 64, 2, 1};
 }
 constexpr unsigned kStage8(int tile) { return (tile8(tile).BM + tile8(tile).BN) * 132u; }
-// exact: sums of all that fp32 holds (not tile 0), else a bf16 Y's; uni: the rows of B in
-// either half of a wavefront's columns share their scales.
+// exact: sums of all that fp32 holds (not tile 0), else what the 8-bit instructions keep, of a bf16 Y;
+// uni: the rows of B in either half of a wavefront's columns share their scales.
 hipError_t launch_product8(int dtype, int tile, bool exact, bool uni, const Product8& a, hipStream_t s);
 
 // Few rows: `rows` (16, 32 or 64) a workgroup; staged: both operands at 16-byte aligned rows that

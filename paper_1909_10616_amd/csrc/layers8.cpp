@@ -299,7 +299,7 @@ Linear8 linear8(const gt_linear_fp8_args& g) {
   e.R = g.R;
   e.ldr = g.ldr;
   e.ldpart = up(a.N, 4) * (e.gated ? 2 : 1);
-  l.exact = g.out_dtype == GT_F32;
+  l.exact = g.out_dtype == GT_F32 || g.exact != 0;
   l.uni = g.wblock == 128 && (!e.gated || a.N % 128 == 0);
   choose(&l);
   return l;

@@ -71,7 +71,7 @@ class gt_quantise_args(ctypes.Structure):
 
 
 class gt_linear_fp8_args(ctypes.Structure):
-    _fields_ = _fields("l:M N K;i:dtype act out_dtype xcode wcode xblock wblock reserved;p:X;l:ldx;p:sx;"
+    _fields_ = _fields("l:M N K;i:dtype act out_dtype xcode wcode xblock wblock exact;p:X;l:ldx;p:sx;"
                        "l:ldsx;p:W;l:ldw;p:sw;l:ldsw;p:bias R;l:ldr;p:Y;l:ldy")
 
 
@@ -566,12 +566,14 @@ def _places(c):
 
 
 def gt_linear_fp8(X, W, bias=None, residual=None, act="none", gated=False, Y=None, workspace=None,
-                  stream=None):
+                  stream=None, exact=False):
     """Y = act(X·Wᵀ + bias) + residual of Codes X [M, K] and W [N, K], fused into the product: K
     lies along the rows of both, blocks of 128 of it are summed and scaled in fp32. gated: W [2N, K]
     and bias [2N] hold a gate's rows, then the up's, Y = act(gate)·up + residual. bias and residual
     [M, N] float32 or bfloat16, of one type; Y in that type (bfloat16 without either) unless given,
-    in float32 or in theirs; it may be the residual itself. The gradients are products of
+    in float32 or in theirs; it may be the residual itself. A bfloat16 Y lets the 8-bit matrix instructions
+    add a block's products, which keep some 13 bits below the largest of 8; a float32 Y and exact=True
+    have them added in fp32, at about half the rate. The gradients are products of
     codes too: dX = gt_linear_fp8(codes of dY, transposed codes of W), dW [N, K] =
     gt_linear_fp8(transposed codes of dY, transposed codes of X)."""
     import torch
@@ -601,8 +603,8 @@ def gt_linear_fp8(X, W, bias=None, residual=None, act="none", gated=False, Y=Non
     r, ldr = _pair(residual, "residual", like, (M, N), typed.dtype)
     out = _result_type(Y, "Y", typed)
     _call("gt_linear_fp8",
-          gt_linear_fp8_args(M, N, K, dt, _act(act, gated), out, xc, wc, xb, wb, 0, x, ldx, sx, ldsx, w, ldw,
-                             sw, ldsw, b, r, ldr, y, ldy), like, workspace, stream)
+          gt_linear_fp8_args(M, N, K, dt, _act(act, gated), out, xc, wc, xb, wb, int(bool(exact)), x, ldx, sx, ldsx,
+                             w, ldw, sw, ldsw, b, r, ldr, y, ldy), like, workspace, stream)
     return Y
 
 
