@@ -82,6 +82,9 @@ __device__ __forceinline__ oct centred(const oct& v, float m, int64_t n) {
 
 // ---- forward
 
+// What a mean is off by, from the mean of the deviations from it; nothing where that is no number (of a row with
+// an infinity, which is its mean, or where the deviations' sum overflows).
+__device__ __forceinline__ float offset(float mean) { return fabsf(mean) < __builtin_inff() ? mean : 0.0f; }
 // The reciprocal deviation of a row from the mean square of its deviations from a mean that is off by `off`.
 // (Fused, so that an infinite square stays one; rounding may leave less than nothing of a constant row.)
 __device__ __forceinline__ float deviation(float square, float off, float eps) {
@@ -159,7 +162,7 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_kernel(const gt_norm
       squares += sum8(oct{x[v].a * x[v].a, x[v].b * x[v].b});
     }
     row_sums<TH>(&s, &squares, box + 1);
-    const float off = s * each, rstd = deviation(squares * each, off, a.eps);
+    const float off = offset(s * each), rstd = deviation(squares * each, off, a.eps);
     if (t == 0) {
       if (a.mean) a.mean[row] = mean + off;
       if (a.rstd) a.rstd[row] = rstd;
@@ -191,7 +194,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const gt_norm_args a) {
       squares += sum8(oct{d.a * d.a, d.b * d.b});
     }
     row_sums<TH>(&s, &squares, box + 1);
-    const float off = s * each, rstd = deviation(squares * each, off, a.eps);
+    const float off = offset(s * each), rstd = deviation(squares * each, off, a.eps);
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[row] = mean + off;
       if (a.rstd) a.rstd[row] = rstd;

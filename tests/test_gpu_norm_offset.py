@@ -117,3 +117,23 @@ def test_variance_past_the_largest_value(L):
         Y = L.gt_norm(x.cuda(), None, b.cuda(), mean=mean, rstd=rstd)
         torch.cuda.synchronize()
         assert not bool(rstd.any()) and torch.equal(Y.cpu(), b.expand(3, N))
+
+
+def test_sums_that_are_not_finite(L):
+    """An infinity leaves its row an infinite mean and no numbers; deviations whose sum overflows, where the
+    values' does not, leave rstd 0 and Y = b."""
+    for N in (24, 700, 1500, 3000, 6000, 12000, 20000):
+        x = torch.randn(4, N, generator=torch.Generator().manual_seed(N))
+        x[0, 5], x[1, N - 1] = math.inf, -math.inf
+        x[2] = 0
+        # octets of a wavefront's first lanes, whose sums meet two lanes apart first: −3.3e38, 3.3e38, 3.3e38
+        x[2, :8], x[2, 8:24] = -3.3e38 / 8, 3.3e38 / 8
+        b = torch.linspace(-1, 1, N)
+        mean, rstd = torch.empty(2, 4, device="cuda")
+        Y = L.gt_norm(x.cuda(), None, b.cuda(), mean=mean, rstd=rstd)
+        torch.cuda.synchronize()
+        assert mean[:2].tolist() == [math.inf, -math.inf]
+        assert bool(torch.isnan(rstd[:2]).all()) and bool(torch.isnan(Y[:2]).all())
+        assert rstd[2].item() == 0 and torch.equal(Y[2].cpu(), b)
+        assert abs(mean[2].item() / (3.3e38 / N) - 1) < 2.0 ** -20
+        assert bool(torch.isfinite(Y[3]).all())
