@@ -8,8 +8,8 @@
 // and db for its own columns over all rows that its workgroup takes, and a second launch
 // adds the workgroups' sums in their order. Of few rows other workgroups of the same
 // launch take the columns' sums.
-// Bound by memory: 16384×4096 in bf16 with mean and rstd 49 µs, 5.5 TB/s; its gradients with
-// R 104 µs, 5.2 TB/s. One row of 4096 in bf16 is latency, 2.7 µs on the GPU.
+// Bound by memory: 16384×4096 in bf16 with mean and rstd 47 to 50 µs, 5.4 to 5.7 TB/s; its gradients with
+// R 104 µs, 5.2 TB/s. One row of 4096 in bf16 is latency, 2.8 µs on the GPU.
 // Thread t of a row has the octets t, t + TH, …, so that 16 neighbours hold 128 columns, a
 // block of codes.
 #include <hip/hip_runtime.h>
@@ -534,7 +534,8 @@ Rows rows_of(int64_t N) {
   return Rows{0, 0};
 }
 // As many workgroups as are resident at once, each with the parameters in its registers for all its
-// rows (16384×4096 in bf16: 5 a unit 48.8 µs, 4 49.1, 6 52.7; 2048×16384: 1 25.5, 2 28.7, 4 34.6).
+// rows (bf16 with fp32 parameters, 16384×4096: 2 a unit 53.2 µs, 4 45.4, 5 46.7, 6 50.2; 2048×16384: 1 27.1,
+// 2 30.6, 4 37.4; 4096×4096 to codes: 2 20.3, 4 17.5, 5 17.2, 8 16.6).
 unsigned grid_of(int64_t M, const Rows& r) {
   const int each = r.threads == 64 ? 4 : 1;
   const int a_unit = r.threads == 512 ? (r.octets == 4 ? 1 : 2) : r.octets == 2 && r.threads == 256 ? 5 : 8;
